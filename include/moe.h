@@ -86,6 +86,8 @@ extern "C" {
 
 #define MOE_DTYPE_BF16 0     /* hidden rows of H bf16 values (2H bytes) */
 #define MOE_DTYPE_FP8_E4M3 1 /* H OCP E4M3FN bytes + H/128 float32 block scales */
+#define MOE_DTYPE_F32 2      /* float32 (router logits, residuals, norm weights) */
+#define MOE_DTYPE_INT8 3     /* H int8 values + one float32 scale per row */
 
 #define MOE_STATUS_BAD_INDEX 1u
 #define MOE_STATUS_DUP_INDEX 2u
@@ -507,6 +509,189 @@ int moe_expert_scale(const uint64_t* recv_x, const uint64_t* recv_scales, int sc
                      const int32_t* expert_offset,
                      const int32_t* rank_offset, const int32_t* recv_cap,
                      const uint64_t* out_y, int64_t max_rows, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The layer around the exchange: routing (what moe_layout and moe_combine
+ * take), RMS norm with 8-bit output (what moe_dispatch carries) and the
+ * experts' products on the rows that arrive.
+ *
+ * Conventions as above; further: rows are packed unless the call takes a
+ * pitch (elements from one row to the next, 0 = packed).  Outputs may not
+ * overlap inputs unless the call says so.  T = 0 (rows = 0) is allowed.
+ * --------------------------------------------------------------------- */
+
+#define MOE_MAX_GROUPS 64 /* blocks of experts in moe_route */
+#define MOE_SCORE_SOFTMAX 0 /* s_e = exp(x_e - max) / sum over the token's experts */
+#define MOE_SCORE_SIGMOID 1 /* s_e = 1 / (1 + exp(-x_e)) */
+
+/*
+ * moe_route -- the k experts of each token and their combine weights.
+ *
+ * Of a token's logits x[E] an expert is eligible unless its logit is -inf or
+ * NaN (softmax sums over the eligible ones).  Each eligible expert has a key:
+ * the score plus bias[e], in float32; where neither a bias nor group_top = 2
+ * asks for scores, the logit itself, which orders as the score does.  A NaN or
+ * -inf key makes the expert ineligible as well.  The k highest keys win, equal keys
+ * in the order of their index.  The bias (load balance) takes part in the
+ * choice only.
+ *
+ * groups > 1: the experts form `groups` blocks of E/groups neighbours; a
+ * block's key is the sum of its group_top (1 or 2) highest keys (of those it
+ * has; a block without eligible experts is never kept), and the experts of the
+ * top_groups best blocks, equal ones in the order of their index, take part.
+ *
+ * w = s (renorm 0), or s divided by the sum over the chosen (renorm 1; 0 if
+ * that sum is 0), times scale.  A slot without an eligible expert, and every
+ * slot of a token whose token_mask byte is 0, gets topk_idx = -1 and weight 0,
+ * which moe_layout takes as unused.
+ *
+ * A softmax's sum adds the upper half of the terms (E padded with zeros to a
+ * power of two) to the lower half until one is left, whatever the launch, so
+ * that replicas that route the same logits agree to the bit.
+ *
+ * logits     [T,E] float32 or bf16 (dtype MOE_DTYPE_F32 / MOE_DTYPE_BF16), rows
+ *            logits_pitch elements apart.
+ * bias       [E] float32 or NULL.
+ * token_mask [T] uint8 or NULL (every token routed).
+ * Out:       topk_idx [T,k] int32, topk_w [T,k] float32, keys descending.
+ * Errors: MOE_EINVAL also for groups > MOE_MAX_GROUPS, E % groups, top_groups outside [1, groups],
+ * group_top outside [1, 2], k > top_groups * E/groups, or a pitch below E.
+ */
+int moe_route(const void* logits, int dtype, int64_t logits_pitch, int64_t T, int k, int E,
+              int score, const float* bias, int groups, int top_groups, int group_top,
+              int renorm, float scale, const uint8_t* token_mask, int32_t* topk_idx,
+              float* topk_w, void* stream);
+
+/*
+ * moe_route_backward -- gradient of the logits from grad_w [T,k], that of
+ * topk_w, with topk_idx as moe_route chose it (the choice itself has no
+ * gradient, nor has the bias).  With c = scale, g = grad_w, s the scores and q
+ * the renormalised ones, over the used slots j:
+ *      softmax              dx_e = c s_e (g_e - sum_j g_j s_j)   for every expert
+ *      softmax, renorm      dx_j = c q_j (g_j - sum_i g_i q_i)
+ *      sigmoid              dx_j = c g_j s_j (1 - s_j)
+ *      sigmoid, renorm      dx_j = c q_j (1 - s_j) (g_j - sum_i g_i q_i)
+ * and 0 elsewhere.  grad_logits [T,E] (packed, type of the logits) is written
+ * whole.  An expert of topk_idx outside [0, E) counts as unused; one repeated
+ * within a row is not supported (moe_route never makes one).
+ */
+int moe_route_backward(const void* logits, int dtype, int64_t logits_pitch, int64_t T, int k,
+                       int E, int score, int renorm, float scale, const int32_t* topk_idx,
+                       const float* grad_w, void* grad_logits, void* stream);
+
+/* Widest row of moe_rmsnorm, moe_rmsnorm_backward and moe_quantize: a workgroup holds one
+ * row in registers, so that it is read once. */
+#define MOE_MAX_ROW 16384
+
+/*
+ * moe_rmsnorm -- residual addition, RMS norm and the rounding to what the next
+ * step takes, in one pass over the rows (float32 throughout, one rounding per
+ * output):
+ *      h = x + residual           sum_out = h
+ *      rstd = 1 / sqrt(mean(h^2) + eps)
+ *      v = h * rstd * weight      y = bf16(v), q = 8-bit codes of v
+ * The norm reads the unrounded h.
+ *
+ * x         [T,H] bf16, rows x_pitch elements apart, 16-byte aligned rows.
+ * residual  [T,H] of residual_dtype (BF16 or F32), rows residual_pitch apart, or
+ *           NULL (h = x; sum_out must then be NULL).
+ * weight    [H] of weight_dtype (BF16 or F32).
+ * sum_out   [T,H] of residual_dtype, packed, or NULL.  May be the residual itself if that is
+ *           packed.
+ * y         [T,H] bf16 or NULL.
+ * q         [T,H] bytes or NULL; q_dtype MOE_DTYPE_FP8_E4M3 or MOE_DTYPE_INT8
+ *           (ignored when q is NULL).
+ * q_scales  [T,scale_cols] float32.  FP8: one scale per MOE_FP8_BLOCK values,
+ *           scale_cols = H/128 (or 0): the x and x_scales of moe_dispatch.
+ *           INT8: one scale per row, written scale_cols times (0 = once);
+ *           scale_cols = H/128 makes rows and scales that moe_dispatch carries
+ *           as MOE_DTYPE_FP8_E4M3 (it copies bytes).
+ *           With a = max |v| of the block or row and M = 448 or 127:
+ *           scale = max(a, 2^-100) / M (1 if a = 0), code = v * (M / max(a,
+ *           2^-100)) rounded to nearest even, at most M.  NaN or infinity in a
+ *           block or row makes its scale NaN or infinite, so that it shows.
+ * rstd      [T] float32 or NULL (moe_rmsnorm_backward takes it).
+ * Errors: MOE_EINVAL for H > MOE_MAX_ROW, no output at all, eps < 0 or NaN;
+ * MOE_EALIGN for H % 8, H % 16 with INT8 codes, H % 128 with FP8, pitches that
+ * break the 16-byte alignment of rows, misaligned pointers.
+ */
+int moe_rmsnorm(const uint16_t* x, int64_t x_pitch, const void* residual, int residual_dtype,
+                int64_t residual_pitch, const void* weight, int weight_dtype, float eps,
+                int64_t T, int H, void* sum_out, uint16_t* y, int q_dtype, void* q,
+                float* q_scales, int scale_cols, float* rstd, void* stream);
+
+/* Workspace of moe_rmsnorm_backward (written to *out_bytes, a HOST pointer). */
+int moe_rmsnorm_backward_workspace_bytes(int64_t T, int H, size_t* out_bytes);
+
+/*
+ * moe_rmsnorm_backward -- gradients of moe_rmsnorm's bf16 path.  With u =
+ * grad_y * weight:
+ *      grad_x = rstd * u - h * rstd^3 * mean(u * h) + grad_sum
+ *      grad_weight = sum over tokens of grad_y * h * rstd
+ * grad_x is the gradient of x and of the residual alike.
+ *
+ * grad_y     [T,H] bf16.
+ * h          [T,H] of h_dtype (BF16 or F32): sum_out, or x without a residual.
+ * rstd       [T] float32, as moe_rmsnorm left it.
+ * grad_sum   [T,H] of h_dtype, the gradient that reaches sum_out from later
+ *            layers, or NULL.
+ * grad_x     [T,H] of h_dtype; may be grad_sum.
+ * grad_weight [H] float32, or NULL (then no workspace is needed).
+ * workspace  256-byte aligned, moe_rmsnorm_backward_workspace_bytes.
+ * Tokens are summed in an order that depends on T and H alone: equal calls give
+ * equal bits.
+ */
+int moe_rmsnorm_backward(const uint16_t* grad_y, const void* h, int h_dtype, const float* rstd,
+                         const void* weight, int weight_dtype, const void* grad_sum, int64_t T,
+                         int H, void* grad_x, float* grad_weight, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * moe_quantize -- 8-bit codes and scales of bf16 rows, as moe_rmsnorm makes them
+ * (v = x): between the two products of an expert, or before moe_dispatch.
+ *
+ * row_src   [rows] int32 or NULL: rows whose entry is negative are skipped
+ *           (moe_layout's row_src: rows that no slot fills; a rank's region
+ *           starts at its rank_offset).
+ * q, q_scales, scale_cols, q_dtype: as for moe_rmsnorm.
+ */
+int moe_quantize(const uint16_t* x, int64_t x_pitch, int64_t rows, int H,
+                 const int32_t* row_src, int q_dtype, void* q, float* q_scales, int scale_cols,
+                 void* stream);
+
+#define MOE_MAX_DEPTH 131056 /* deepest product whose sums stay in int32 */
+#define MOE_ACT_NONE 0
+#define MOE_ACT_SWIGLU 1
+
+/*
+ * moe_expert_matmul -- the experts' products on 8-bit integers, scales for each
+ * row and each channel:
+ *      v[r,n] = (sum_k a[r,k] * w[e,n,k]) * a_scales[r] * w_scales[e,n]
+ * for the rows r of expert e's window, summed exactly in int32.
+ *      MOE_ACT_NONE    y[r,n] = bf16(v[r,n])                    n < N
+ *      MOE_ACT_SWIGLU  y[r,i] = bf16(silu(v[r,i]) * v[r,N/2+i])  i < N/2
+ *
+ * a         [rows,K] int8, 16-byte aligned, K % 16 == 0, K <= MOE_MAX_DEPTH.
+ * a_scales  a row's scale at a_scales[r * a_scale_pitch] (0 = 1).
+ * w         [E,N,K] int8, 16-byte aligned: channel by channel, the depth innermost.
+ * w_scales  [E,N] float32.
+ * expert_offset, expert_count: expert e's window is the expert_count[e] rows
+ *           from expert_offset[e] - expert_offset[0], clipped to [0, rows).
+ *           expert_count NULL: up to expert_offset[e+1].  Both as moe_layout or
+ *           moe_layout_fixed leave them; a rank passes expert_offset + r*L and
+ *           expert_count + r*L with its own region.  Windows may not overlap.
+ *           expert_offset NULL (E = 1 only): one window of all rows, a plain
+ *           matrix product.
+ * y         [rows,N] or [rows,N/2] bf16, 16-byte aligned, row bytes % 16 == 0; rows of no
+ *           window are left untouched.
+ * Errors: MOE_EALIGN for K % 16, N % 8 (SWIGLU: N % 16), misaligned pointers;
+ * MOE_EINVAL for K > MOE_MAX_DEPTH, rows > INT32_MAX,
+ * E > MOE_MAX_EXPERTS.
+ */
+int moe_expert_matmul(const int8_t* a, const float* a_scales, int a_scale_pitch, int64_t rows,
+                      const int8_t* w, const float* w_scales, int E, int N, int K,
+                      const int32_t* expert_offset, const int32_t* expert_count, int act,
+                      uint16_t* y, void* stream);
 
 #ifdef __cplusplus
 }

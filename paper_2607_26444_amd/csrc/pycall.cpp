@@ -36,8 +36,14 @@ PyObject* g_get_stream;       // (index) -> address of its current stream
 #define MOE_CALLS(X)                                                                     \
   X(moe_layout) X(moe_layout_fixed) X(moe_dispatch) X(moe_combine) X(moe_layout_dedup) \
   X(moe_dispatch_dedup) X(moe_expand) X(moe_combine_local) X(moe_combine_dedup)
+// Calls of the layer around the exchange: a library without one of them binds
+// all the same, and that call raises.
+#define MOE_LAYER_CALLS(X)                                                       \
+  X(moe_route) X(moe_route_backward) X(moe_rmsnorm) X(moe_rmsnorm_backward)      \
+  X(moe_quantize) X(moe_expert_matmul)
 #define X(name) decltype(&name) f_##name;
 MOE_CALLS(X)
+MOE_LAYER_CALLS(X)
 #undef X
 
 // Reads one call's arguments in order; after the first failure (a Python
@@ -75,6 +81,15 @@ class Args {
   }
 
   int i32() { return ok_ ? (int)integer(args_[at_++]) : 0; }
+  int64_t i64() { return ok_ ? (int64_t)integer(args_[at_++]) : 0; }
+
+  float f32() {
+    if (!ok_) return 0.0f;
+    PyObject* o = args_[at_++];
+    const double v = PyFloat_CheckExact(o) ? PyFloat_AS_DOUBLE(o) : PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) ok_ = false;
+    return (float)v;
+  }
 
   // Truth of an attribute, or a method's integer result.
   long long method(PyObject* o, PyObject* name) {
@@ -129,8 +144,14 @@ class Args {
     return ptr<const int32_t>();
   }
 
-  void* workspace(size_t& bytes) {
+  // A workspace; `optional`: None is a null pointer of no bytes.
+  void* workspace(size_t& bytes, bool optional = false) {
     PyObject* o = ok_ ? args_[at_] : nullptr;
+    if (o == Py_None && optional) {
+      ++at_;
+      bytes = 0;
+      return nullptr;
+    }
     void* p = ptr<void>();
     bytes = ok_ ? (size_t)(method(o, s_numel) * method(o, s_element_size)) : 0;
     return p;
@@ -346,6 +367,147 @@ PyObject* combine_dedup(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// The entry point of a call of the layer, or null with the error set.
+template <typename F>
+bool present(F* f, const char* name) {
+  if (f) return true;
+  PyErr_Format(PyExc_RuntimeError, "libmoe.so has no %s: build it again", name);
+  return false;
+}
+
+PyObject* route(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_route, "moe_route")) return nullptr;
+  Args a(args, n);
+  a.expect(15);
+  const void* x = a.ptr<const void>();
+  const int dtype = a.i32(), E = a.i32();
+  const float* bias = a.ptr<const float>();
+  const uint8_t* mask = a.ptr<const uint8_t>();
+  int64_t T;
+  int k;
+  int32_t* idx = const_cast<int32_t*>(a.table(T, k));
+  float* w = a.ptr<float>();
+  const int score = a.i32(), groups = a.i32(), top = a.i32(), two = a.i32(), renorm = a.i32();
+  const float scale = a.f32();
+  void* stream = a.stream();
+  const int64_t pitch = a.i64();
+  return finish(a, [&] {
+    return f_moe_route(x, dtype, pitch, T, k, E, score, bias, groups, top, two, renorm, scale,
+                       mask, idx, w, stream);
+  });
+}
+
+PyObject* route_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_route_backward, "moe_route_backward")) return nullptr;
+  Args a(args, n);
+  a.expect(11);
+  const void* x = a.ptr<const void>();
+  const int dtype = a.i32(), E = a.i32();
+  int64_t T;
+  int k;
+  const int32_t* idx = a.table(T, k);
+  const float* gw = a.ptr<const float>();
+  void* gx = a.ptr<void>();
+  const int score = a.i32(), renorm = a.i32();
+  const float scale = a.f32();
+  void* stream = a.stream();
+  const int64_t pitch = a.i64();
+  return finish(a, [&] {
+    return f_moe_route_backward(x, dtype, pitch, T, k, E, score, renorm, scale, idx, gw, gx,
+                                stream);
+  });
+}
+
+PyObject* rmsnorm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_rmsnorm, "moe_rmsnorm")) return nullptr;
+  Args a(args, n);
+  a.expect(18);
+  const uint16_t* x = a.ptr<const uint16_t>();
+  const void* res = a.ptr<const void>();
+  const int res_dtype = a.i32();
+  const void* weight = a.ptr<const void>();
+  const int weight_dtype = a.i32();
+  const float eps = a.f32();
+  const int64_t T = a.i64();
+  const int H = a.i32();
+  void* sum = a.ptr<void>();
+  uint16_t* y = a.ptr<uint16_t>();
+  const int q_dtype = a.i32();
+  void* q = a.ptr<void>();
+  float* scales = a.ptr<float>();
+  float* rstd = a.ptr<float>();
+  const int cols = a.i32();
+  void* stream = a.stream();
+  const int64_t x_pitch = a.i64(), res_pitch = a.i64();
+  return finish(a, [&] {
+    return f_moe_rmsnorm(x, x_pitch, res, res_dtype, res_pitch, weight, weight_dtype, eps, T, H,
+                         sum, y, q_dtype, q, scales, cols, rstd, stream);
+  });
+}
+
+PyObject* rmsnorm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_rmsnorm_backward, "moe_rmsnorm_backward")) return nullptr;
+  Args a(args, n);
+  a.expect(13);
+  const uint16_t* gy = a.ptr<const uint16_t>();
+  const void* h = a.ptr<const void>();
+  const int h_dtype = a.i32();
+  const float* rstd = a.ptr<const float>();
+  const void* weight = a.ptr<const void>();
+  const int weight_dtype = a.i32();
+  const void* gsum = a.ptr<const void>();
+  const int64_t T = a.i64();
+  const int H = a.i32();
+  void* gx = a.ptr<void>();
+  float* gw = a.ptr<float>();
+  size_t bytes;
+  void* ws = a.workspace(bytes, true);
+  void* stream = a.stream();
+  return finish(a, [&] {
+    return f_moe_rmsnorm_backward(gy, h, h_dtype, rstd, weight, weight_dtype, gsum, T, H, gx, gw,
+                                  ws, bytes, stream);
+  });
+}
+
+PyObject* quantize(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_quantize, "moe_quantize")) return nullptr;
+  Args a(args, n);
+  a.expect(10);
+  const uint16_t* x = a.ptr<const uint16_t>();
+  const int64_t rows = a.i64();
+  const int H = a.i32(), q_dtype = a.i32();
+  void* q = a.ptr<void>();
+  float* scales = a.ptr<float>();
+  const int32_t* src = a.ptr<const int32_t>();
+  const int cols = a.i32();
+  void* stream = a.stream();
+  const int64_t pitch = a.i64();
+  return finish(a, [&] {
+    return f_moe_quantize(x, pitch, rows, H, src, q_dtype, q, scales, cols, stream);
+  });
+}
+
+PyObject* expert_matmul(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_expert_matmul, "moe_expert_matmul")) return nullptr;
+  Args a(args, n);
+  a.expect(14);
+  const int8_t* x = a.ptr<const int8_t>();
+  const float* xs = a.ptr<const float>();
+  const int64_t rows = a.i64();
+  const int8_t* w = a.ptr<const int8_t>();
+  const float* ws = a.ptr<const float>();
+  const int E = a.i32(), N = a.i32(), K = a.i32();
+  const int32_t* offset = a.ptr<const int32_t>();
+  const int32_t* count = a.ptr<const int32_t>();
+  const int act = a.i32();
+  uint16_t* y = a.ptr<uint16_t>();
+  void* stream = a.stream();
+  const int pitch = a.i32();
+  return finish(a, [&] {
+    return f_moe_expert_matmul(x, xs, pitch, rows, w, ws, E, N, K, offset, count, act, y, stream);
+  });
+}
+
 // init(lib_path, argument_error, c_int, get_device, get_stream): binds the
 // entry points of the libmoe.so that is already loaded.
 PyObject* init(PyObject*, PyObject* args) {
@@ -364,6 +526,9 @@ PyObject* init(PyObject*, PyObject* args) {
     return nullptr;                                                 \
   }
   MOE_CALLS(X)
+#undef X
+#define X(name) f_##name = reinterpret_cast<decltype(&name)>(dlsym(h, #name));
+  MOE_LAYER_CALLS(X)
 #undef X
   Py_INCREF(err);
   Py_XSETREF(g_argument_error, err);
@@ -388,6 +553,12 @@ PyMethodDef methods[] = {
     FAST("expand", expand),
     FAST("combine_local", combine_local),
     FAST("combine_dedup", combine_dedup),
+    FAST("route", route),
+    FAST("route_backward", route_backward),
+    FAST("rmsnorm", rmsnorm),
+    FAST("rmsnorm_backward", rmsnorm_backward),
+    FAST("quantize", quantize),
+    FAST("expert_matmul", expert_matmul),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_moecall", nullptr, -1, methods,

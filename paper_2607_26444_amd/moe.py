@@ -28,6 +28,8 @@ MOE_ELAUNCH = -4
 
 MOE_DTYPE_BF16 = 0
 MOE_DTYPE_FP8_E4M3 = 1
+MOE_DTYPE_F32 = 2
+MOE_DTYPE_INT8 = 3
 
 MOE_STATUS_BAD_INDEX = 1
 MOE_STATUS_DUP_INDEX = 2
@@ -45,15 +47,27 @@ MOE_POLICY_BY_RANK = 2
 MOE_POLICY_DYNAMIC = 3
 MOE_POLICY_STATIC = 4
 
+MOE_SCORE_SOFTMAX = 0
+MOE_SCORE_SIGMOID = 1
+MOE_ACT_NONE = 0
+MOE_ACT_SWIGLU = 1
+MOE_MAX_GROUPS = 64
+MOE_MAX_ROW = 16384
+MOE_MAX_DEPTH = 131056
+
 # Entry points declared in include/moe.h.
 EXPORTS = ("moe_version", "moe_strerror", "moe_last_hip_error", "moe_wall_clock_khz",
            "moe_layout_workspace_bytes", "moe_layout", "moe_layout_fixed", "moe_dispatch",
            "moe_dispatch_ex", "moe_combine", "moe_combine_ex", "moe_expert_scale",
            "moe_layout_dedup_workspace_bytes", "moe_layout_dedup", "moe_dispatch_dedup",
-           "moe_expand", "moe_combine_local", "moe_combine_dedup", "moe_layout_scratch")
+           "moe_expand", "moe_combine_local", "moe_combine_dedup", "moe_layout_scratch",
+           "moe_route", "moe_route_backward", "moe_rmsnorm",
+           "moe_rmsnorm_backward_workspace_bytes", "moe_rmsnorm_backward", "moe_quantize",
+           "moe_expert_matmul")
 
 _lib = None
 P = ctypes.c_void_p
+F32 = ctypes.c_float
 I32 = ctypes.c_int
 I64 = ctypes.c_int64
 SZ = ctypes.c_size_t
@@ -106,6 +120,19 @@ def lib() -> ctypes.CDLL:
         L.moe_combine_dedup.argtypes = [P, I64, I32, I32, I32, I32, P, P, P, P, P, P, SZ, P, P]
         L.moe_layout_scratch.argtypes = [P, I64, I32, I32, I32, P, P, P, P, P, P, P,
                                          ctypes.POINTER(P), ctypes.POINTER(SZ), P]
+        L.moe_route.argtypes = [P, I32, I64, I64, I32, I32, I32, P, I32, I32, I32, I32, F32, P, P,
+                                P, P]
+        L.moe_route_backward.argtypes = [P, I32, I64, I64, I32, I32, I32, I32, F32, P, P, P, P]
+        L.moe_rmsnorm.argtypes = [P, I64, P, I32, I64, P, I32, F32, I64, I32, P, P, I32, P, P,
+                                  I32, P, P]
+        L.moe_rmsnorm_backward_workspace_bytes.argtypes = [I64, I32, ctypes.POINTER(SZ)]
+        L.moe_rmsnorm_backward.argtypes = [P, P, I32, P, P, I32, P, I64, I32, P, P, P, SZ, P]
+        L.moe_quantize.argtypes = [P, I64, I64, I32, P, I32, P, P, I32, P]
+        L.moe_expert_matmul.argtypes = [P, P, I32, I64, P, P, I32, I32, I32, P, P, I32, P, P]
+        for f in ("moe_route", "moe_route_backward", "moe_rmsnorm",
+                  "moe_rmsnorm_backward_workspace_bytes", "moe_rmsnorm_backward",
+                  "moe_quantize", "moe_expert_matmul"):
+            getattr(L, f).restype = I32
         for f in ("moe_layout_scratch", "moe_layout_workspace_bytes", "moe_layout", "moe_layout_fixed", "moe_dispatch",
                   "moe_dispatch_ex", "moe_combine", "moe_combine_ex", "moe_expert_scale",
                   "moe_layout_dedup_workspace_bytes", "moe_layout_dedup", "moe_dispatch_dedup",
@@ -319,6 +346,71 @@ def moe_combine_dedup(partial, H, E, R, topk_idx, tok_pos, tok_offset, part_cap,
         partial, H, E, R, topk_idx, tok_pos, tok_offset, part_cap, y, workspace, status, stream)
     if rc:
         _check("moe_combine_dedup", rc)
+
+
+# --------------------------------------------- the layer around the exchange
+def moe_route(logits, dtype, E, bias, token_mask, topk_idx, topk_w, score=MOE_SCORE_SOFTMAX,
+              groups=1, top_groups=1, group_top=1, renorm=True, scale=1.0, stream=None,
+              logits_pitch=0):
+    """The k experts of each token (topk_idx [T,k], which sets T and k) and
+    their weights."""
+    rc = (_fast or _calls()).route(
+        logits, dtype, E, bias, token_mask, topk_idx, topk_w, score, groups, top_groups,
+        group_top, renorm, scale, stream, logits_pitch)
+    if rc:
+        _check("moe_route", rc)
+
+
+def moe_route_backward(logits, dtype, E, topk_idx, grad_w, grad_logits,
+                       score=MOE_SCORE_SOFTMAX, renorm=True, scale=1.0, stream=None,
+                       logits_pitch=0):
+    rc = (_fast or _calls()).route_backward(
+        logits, dtype, E, topk_idx, grad_w, grad_logits, score, renorm, scale, stream,
+        logits_pitch)
+    if rc:
+        _check("moe_route_backward", rc)
+
+
+def moe_rmsnorm(x, residual, residual_dtype, weight, weight_dtype, eps, T, H, sum_out, y, q_dtype,
+                q, q_scales, rstd, scale_cols=0, stream=None, x_pitch=0, residual_pitch=0):
+    rc = (_fast or _calls()).rmsnorm(
+        x, residual, residual_dtype, weight, weight_dtype, eps, T, H, sum_out, y, q_dtype, q,
+        q_scales, rstd, scale_cols, stream, x_pitch, residual_pitch)
+    if rc:
+        _check("moe_rmsnorm", rc)
+
+
+def moe_rmsnorm_backward_workspace_bytes(T: int, H: int) -> int:
+    out = SZ(0)
+    _check("moe_rmsnorm_backward_workspace_bytes",
+           lib().moe_rmsnorm_backward_workspace_bytes(T, H, ctypes.byref(out)))
+    return out.value
+
+
+def moe_rmsnorm_backward(grad_y, h, h_dtype, rstd, weight, weight_dtype, grad_sum, T, H, grad_x,
+                         grad_weight, workspace, stream=None):
+    rc = (_fast or _calls()).rmsnorm_backward(
+        grad_y, h, h_dtype, rstd, weight, weight_dtype, grad_sum, T, H, grad_x, grad_weight,
+        workspace, stream)
+    if rc:
+        _check("moe_rmsnorm_backward", rc)
+
+
+def moe_quantize(x, rows, H, q_dtype, q, q_scales, row_src=None, scale_cols=0, stream=None,
+                 x_pitch=0):
+    rc = (_fast or _calls()).quantize(
+        x, rows, H, q_dtype, q, q_scales, row_src, scale_cols, stream, x_pitch)
+    if rc:
+        _check("moe_quantize", rc)
+
+
+def moe_expert_matmul(a, a_scales, rows, w, w_scales, E, N, K, expert_offset, expert_count, act,
+                      y, stream=None, a_scale_pitch=0):
+    rc = (_fast or _calls()).expert_matmul(
+        a, a_scales, rows, w, w_scales, E, N, K, expert_offset, expert_count, act, y, stream,
+        a_scale_pitch)
+    if rc:
+        _check("moe_expert_matmul", rc)
 
 
 # ------------------------------------------------------------ buffer plumbing

@@ -1,0 +1,156 @@
+"""The MoE layer as a whole: against its definition in 64 bits, on a stream of its
+own, and replayed from a graph."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import layer_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _inputs(T, H, E, seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    x, r = (torch.randn(T, H, generator=g).bfloat16() for _ in range(2))
+    return x.cuda(), r.cuda(), torch.randn(T, E, generator=g).cuda()
+
+
+def _int8(v):
+    s = ref.amax_scales(v, False)
+    return torch.round(v / s) * s
+
+
+def _want(layer, x, r, logits):
+    """The layer in 64 bits with the experts that it chose."""
+    c = [t.cpu().double() for t in (x, r, layer.norm_weight, logits)]
+    h, _, y = ref.rmsnorm(c[0], c[1], c[2], layer.eps)
+    idx = layer.topk_idx.cpu()
+    w = ref.weights(c[3], idx, layer.options["score"] == 1, layer.options["renorm"],
+                    layer.options["scale"])
+    a, out = _int8(y), torch.zeros_like(y)
+    size = torch.zeros_like(y)
+    for e in range(layer.E):
+        tok, slot = torch.nonzero(idx == e, as_tuple=True)
+        if not len(tok):
+            continue
+        v = a[tok] @ layer.w13[e].cpu().double().T * layer.w13_scale[e].cpu().double()
+        g, u = v[:, :layer.I], v[:, layer.I:]
+        act = _int8(g * torch.sigmoid(g) * u)
+        row = act @ layer.w2[e].cpu().double().T * layer.w2_scale[e].cpu().double()
+        out.index_add_(0, tok, row * w[tok, slot][:, None])
+        size.index_add_(0, tok, (row * w[tok, slot][:, None]).abs())
+    return h, out, size
+
+
+@pytest.mark.parametrize("T,H,I,E,k", [(1, 256, 64, 4, 2), (33, 384, 208, 8, 3), (300, 512, 256, 16, 4),
+                                       (700, 1024, 144, 4, 2)])
+@pytest.mark.parametrize("score", [0, 1])
+def test_layer(T, H, I, E, k, score):
+    """A bf16 rounding (2^-8) before the second quantisation moves a code by
+    one step (1/254 of the row's largest value) here and there, the experts' rows
+    and the result are rounded to bf16: over a token's row the difference stays
+    under 3% of its norm."""
+    from paper_2607_26444_amd.layer import random_layer
+    layer = random_layer(T, H, I, E, k, seed=T, score=score, scale=1.5)
+    x, r, logits = _inputs(T, H, E, seed=1)
+    y = layer.forward(x, r, logits)
+    torch.cuda.synchronize()
+    h, want, size = _want(layer, x, r, logits)
+    assert torch.all((layer.sum.cpu().double() - h).abs() <= 2.0 ** -8 * 1.001 * h.abs())
+    off = (y.cpu().double() - want).norm(dim=1)
+    assert torch.all(off <= 0.03 * want.norm(dim=1)), float((off / want.norm(dim=1)).max())
+    assert int(layer.layout.status) == 0
+
+
+def test_padding_tokens_and_masked_experts():
+    from paper_2607_26444_amd.layer import random_layer
+    layer = random_layer(64, 256, 64, 8, 4, bias=torch.zeros(8, device="cuda"), score=1)
+    x, r, logits = _inputs(64, 256, 8, seed=2)
+    logits[5] = -math.inf
+    logits[6, 2:] = -math.inf
+    mask = torch.ones(64, dtype=torch.uint8, device="cuda")
+    mask[60:] = 0
+    y = layer.forward(x, r, logits, token_mask=mask)
+    torch.cuda.synchronize()
+    assert torch.all(layer.topk_idx[60:] == -1) and torch.all(layer.topk_idx[5] == -1)
+    assert torch.all(y[60:] == 0) and torch.all(y[5] == 0) and torch.all(layer.topk_idx[6, 2:] == -1)
+    _, want, _ = _want(layer, x, r, logits.masked_fill(mask[:, None] == 0, -math.inf))
+    off = (y.cpu().double() - want).norm(dim=1)
+    assert torch.all(off <= 0.03 * want.norm(dim=1) + 1e-12)
+
+
+def test_gate_as_a_function():
+    from paper_2607_26444_amd.layer import random_layer
+    layer = random_layer(40, 256, 64, 8, 2)
+    x, r, _ = _inputs(40, 256, 8, seed=3)
+    gate = torch.randn(256, 8, device="cuda").bfloat16() / 16
+    seen = []
+
+    def logits(normed):
+        seen.append(normed @ gate)
+        return seen[-1]
+    y = layer.forward(x, r, logits)
+    again = layer.forward(x, r, seen[0]).clone()
+    assert torch.equal(y, again)
+
+
+def test_graph_replays():
+    """Captured once, replayed with new inputs, eager work in between: every
+    replay equals the eager result."""
+    from paper_2607_26444_amd.layer import random_layer
+    T, H, E = 48, 512, 8
+    layer = random_layer(T, H, 128, E, 2)
+    eager = random_layer(T, H, 128, E, 2)
+    x, r, logits = (t.clone() for t in _inputs(T, H, E, seed=0))
+    layer.forward(x, r, logits)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward(x, r, logits)
+    for seed in range(1, 5):
+        for t, new in zip((x, r, logits), _inputs(T, H, E, seed)):
+            t.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = eager.forward(x, r, logits)
+        torch.cuda.synchronize()
+        assert torch.equal(layer.y, want) and torch.equal(layer.sum, eager.sum)
+
+
+def test_stream_of_its_own():
+    from paper_2607_26444_amd.layer import random_layer
+    layer = random_layer(100, 256, 64, 8, 2)
+    x, r, logits = _inputs(100, 256, 8, seed=4)
+    want = layer.forward(x, r, logits).clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    y = layer.forward(x, r, logits, stream=s)
+    s.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_refused_arguments():
+    from paper_2607_26444_amd import layer as mod
+    from paper_2607_26444_amd.layer import random_layer
+    with pytest.raises(ValueError, match="multiple"):
+        random_layer(8, 200, 64, 4, 2)
+    layer = random_layer(8, 256, 64, 4, 2)
+    x, r, logits = _inputs(8, 256, 4, seed=5)
+    for bad in ((x.float(), r, logits), (x[:4], r, logits), (x, r.float(), logits),
+                (x, r, logits[:, :3]), (x, r, logits.half())):
+        with pytest.raises(ValueError):
+            layer.forward(*bad)
+    with pytest.raises(ValueError):
+        layer.forward(x, r, logits, token_mask=torch.ones(8, device="cuda"))
+    with pytest.raises(ValueError):
+        mod.MoeLayer(8, 256, 64, 4, 2, layer.norm_weight, layer.w13, layer.w13_scale,
+                     layer.w2[:2], layer.w2_scale)
