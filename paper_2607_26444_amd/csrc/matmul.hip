@@ -15,51 +15,65 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kOutside = 0x7FFFFFF0u;   // past every buffer's range: reads zeros
 
-// One window of rows: expert and first row of tile `tile` of `size` rows, and
-// the rows left from there; rows 0: no such tile.
+// A tile of an expert's window: rows of the window from `row` on (0: no such
+// tile) and the piece of its channels.
 struct Tile {
   int expert;
   int64_t row;
   int rows;
+  int piece;
 };
 
-__device__ __forceinline__ Tile find_tile(const MatmulArgs& a, int64_t tile, int size) {
-  if (!a.offset) {
-    const int64_t row = tile * size, left = a.rows - row;
-    return {0, row, left < 0 ? 0 : left < size ? (int)left : size};
-  }
-  const int lane = threadIdx.x & (kWave - 1);
-  const int first = (int)ld4(a.offset);
-  int64_t before = 0;
-  for (int e0 = 0; e0 < a.E; e0 += kWave) {
-    const int e = e0 + lane;
-    int64_t start = 0, n = 0;
-    if (e < a.E) {
-      const int o = (int)ld4(a.offset + e);
-      start = (int64_t)o - first;
-      n = a.count ? (int64_t)(int)ld4(a.count + e) : (int64_t)(int)ld4(a.offset + e + 1) - o;
-      if (start < 0 || start > a.rows) n = 0;
-      if (n > a.rows - start) n = a.rows - start;
-      if (n < 0) n = 0;
-    }
-    const int tiles = (int)((n + size - 1) / size);
-    int sum = tiles;                                   // inclusive over the lanes
+// Tile `id` of the order expert, group of `group` row tiles, channel piece, row
+// tile in the group, so that neighbouring tiles share rows or weights.  A row
+// tile has `size` rows, a window `pieces` channel pieces.
+__device__ __forceinline__ Tile find_tile(const MatmulArgs& a, int64_t id, int size, int pieces,
+                                          int group) {
+  int expert = 0;
+  int64_t start = 0, n = a.rows, before = 0;
+  if (a.offset) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int first = uniform((int)ld4(a.offset));
+    n = 0;
+    for (int e0 = 0; e0 < a.E; e0 += kWave) {
+      const int e = e0 + lane;
+      int64_t s = 0, m = 0;
+      if (e < a.E) {
+        const int o = (int)ld4(a.offset + e);
+        s = (int64_t)o - first;
+        m = a.count ? (int64_t)(int)ld4(a.count + e) : (int64_t)(int)ld4(a.offset + e + 1) - o;
+        if (s < 0 || s > a.rows) m = 0;
+        if (m > a.rows - s) m = a.rows - s;
+        if (m < 0) m = 0;
+      }
+      const int tiles = (int)((m + size - 1) / size);
+      int sum = tiles;                                 // inclusive over the lanes
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int o = __shfl_up(sum, d, kWave);
-      if (lane >= d) sum += o;
+      for (int d = 1; d < kWave; d *= 2) {
+        const int o = __shfl_up(sum, d, kWave);
+        if (lane >= d) sum += o;
+      }
+      const uint64_t hit = __ballot((before + sum) * pieces > id);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        expert = e0 + l;
+        before += __builtin_amdgcn_readlane(sum - tiles, l);
+        start = (int64_t)readlane64((uint64_t)s, l);
+        n = (int64_t)readlane64((uint64_t)m, l);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(sum, kWave - 1);
     }
-    const uint64_t hit = __ballot(before + sum > tile);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      const int64_t at = tile - before - (__shfl(sum, l, kWave) - __shfl(tiles, l, kWave));
-      const int64_t s = __shfl(start, l, kWave), m = __shfl(n, l, kWave);
-      const int64_t left = m - at * size;
-      return {e0 + l, s + at * size, left < size ? (int)left : size};
-    }
-    before += __shfl(sum, kWave - 1, kWave);
   }
-  return {0, 0, 0};
+  const int tiles = (int)((n + size - 1) / size);
+  const int64_t at = id - before * pieces;
+  if (at >= (int64_t)tiles * pieces) return {0, 0, 0, 0};
+  const int per = group * pieces;
+  const int g = (int)at / per, in = (int)at % per;      // below 2^31: tiles of one launch
+  const int here = tiles - g * group < group ? tiles - g * group : group;   // tiles of this group
+  const int tile = g * group + in % here;
+  const int left = (int)(n - (int64_t)tile * size);
+  return {expert, start + (int64_t)tile * size, left < size ? left : size, in / here};
 }
 
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
@@ -74,9 +88,9 @@ __global__ __launch_bounds__(kBlock) void matmul_split_kernel(MatmulArgs a, int6
   const int row = lane & 15, piece = lane / 16;
   const int half = a.N / 2;
   for (int64_t id = blockIdx.x; id < tiles * pieces; id += gridDim.x) {
-  const Tile t = find_tile(a, id / pieces, MT * 16);
+  const Tile t = find_tile(a, id, MT * 16, pieces, 1);
   if (t.rows == 0) continue;                           // the whole workgroup
-  const int c0 = (int)(id % pieces) * (a.swiglu ? NT * 8 : NT * 16);   // first (gate) channel
+  const int c0 = t.piece * (a.swiglu ? NT * 8 : NT * 16);   // first (gate) channel
 
   // A matrix instruction takes 64 of the depth, 16 bytes per lane.  Lanes read
   // 32 neighbouring bytes for two of them, so that four lanes cover a line of
@@ -156,12 +170,155 @@ __global__ __launch_bounds__(kBlock) void matmul_split_kernel(MatmulArgs a, int6
   }
 }
 
+// Tiles of 256 rows x 256 channels through LDS: eight wavefronts, each 128 rows
+// x 64 channels; pieces of 128 of the depth go from memory into LDS by the
+// loads themselves, one piece ahead of the matrix instructions.
+//
+// LDS holds a row's 128 bytes as eight chunks of 16, chunk c of row r at place
+// c ^ (r & 7), so that eight lanes that read one chunk of eight rows touch all
+// banks.
+constexpr int kTile = 256, kDepth = 128;
+constexpr int kTileThreads = 512;
+constexpr int kTileBytes = kTile * kDepth;
+constexpr int kStageBytes = 2 * kTileBytes;
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
+__device__ __forceinline__ void load_to_lds(Rsrc r, uint32_t offset, lds_u8* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, (int)offset, 0, 0, 0);
+}
+
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2 * kStageBytes];   // rows, weights
+  constexpr int MT = 8, NT = 4;
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  // the 32 tiles that an XCD's compute units hold together are neighbours
+  const int64_t b = blockIdx.x;
+  const int64_t id = b / 256 * 256 + b % 8 * 32 + b / 8 % 32;
+  const Tile t = find_tile(a, id, kTile, pieces, group);
+  if (t.rows == 0) return;
+  const int half = a.N / 2;
+  const int c0 = t.piece * (a.swiglu ? kTile / 2 : kTile);
+
+  // loads: instruction j of a wavefront fills LDS rows (j * 8 + wave) * 8 + lane / 8
+  const int lr = lane / 8, chunk = (lane & 7) ^ lr;
+  uint32_t ao[4], wo[4];
+  const bool up = a.swiglu && (wave & 2);              // rows 16..31 of 32: up channels
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = (j * 8 + wave) * 8 + lr;
+    ao[j] = (uint32_t)r * (uint32_t)a.K + chunk * 16;
+    const int c = a.swiglu ? r / 32 * 16 + (r & 15) : r;
+    wo[j] = (uint32_t)c * (uint32_t)a.K + chunk * 16;
+  }
+  const int channels = (a.swiglu ? half : a.N) - c0;   // at least 1
+  const int most = a.swiglu ? kTile / 2 : kTile;
+  const uint8_t* abase = a.a + t.row * a.K;
+  const uint8_t* wbase = a.w + ((int64_t)t.expert * a.N + c0 + (up ? half : 0)) * a.K;
+  const int arange = t.rows * a.K, wrange = (channels < most ? channels : most) * a.K;
+  const Rsrc ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(abase), (short)0, arange,
+                                                    kRsrcWord3);
+  const Rsrc rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wbase), (short)0, wrange,
+                                                    kRsrcWord3);
+  // past the depth and past the tile's rows and channels: zeros
+  auto load = [&](int k0, uint32_t buf) {
+    const bool in = k0 + chunk * 16 < a.K;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      load_to_lds(ra, in ? ao[j] + k0 : kOutside,
+                  (lds_u8*)(s_tile + buf + (j * 8 + wave) * 1024));
+      load_to_lds(rw, in ? wo[j] + k0 : kOutside,
+                  (lds_u8*)(s_tile + buf + kTileBytes + (j * 8 + wave) * 1024));
+    }
+  };
+
+  const int wm = wave / 4, wn = wave % 4;              // 2 x 4 wavefronts
+  const int row = lane & 15, quarter = lane / 16;
+  const uint32_t place = row * kDepth + ((quarter ^ (row & 7)) * 16);
+  const uint32_t at_a = wm * (128 * kDepth) + place;
+  const uint32_t at_w = kTileBytes + wn * (64 * kDepth) + place;
+  i32x4 acc[MT][NT] = {};
+
+  load(0, 0);
+  __syncthreads();
+  uint32_t buf = 0;
+  for (int k0 = 0; k0 < a.K; k0 += kDepth) {
+    load(k0 + kDepth, buf ^ kStageBytes);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      i32x4 av[MT], wv[NT];
+      const uint8_t* pw = s_tile + (at_w ^ (h * 64)) + buf;
+      const uint8_t* pa = s_tile + (at_a ^ (h * 64)) + buf;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) wv[j] = *(const i32x4*)(pw + j * 16 * kDepth);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) av[i] = *(const i32x4*)(pa + i * 16 * kDepth);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[j], av[i], acc[i][j], 0, 0, 0);
+    }
+    __syncthreads();
+    buf ^= kStageBytes;
+  }
+
+  // a lane's four sums of a tile: channels quarter * 4 .. + 3 of row `row`
+  const int out = a.swiglu ? half : a.N;
+  const float* sw0 = a.w_scales + (int64_t)t.expert * a.N;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int r = wm * 128 + i * 16 + row;
+    if (r >= t.rows) continue;
+    const float sa = a.a_scales[(t.row + r) * a.a_scale_pitch];
+    uint16_t* y = a.y + (t.row + r) * out;
+    if (a.swiglu) {
+#pragma unroll
+      for (int j = 0; j < NT; j += 2) {
+        const int c = c0 + wn * 32 + j * 8 + quarter * 4;
+        if (c >= out) continue;
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float g = (float)acc[i][j][q] * (sa * sw0[c + q]);
+          v[q] = silu(g) * ((float)acc[i][j + 1][q] * (sa * sw0[half + c + q]));
+        }
+        st4(y + c, pack_bf16x2(v[0], v[1]));
+        st4(y + c + 2, pack_bf16x2(v[2], v[3]));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int c = c0 + wn * 64 + j * 16 + quarter * 4;
+        if (c >= out) continue;
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (float)acc[i][j][q] * (sa * sw0[c + q]);
+        st4(y + c, pack_bf16x2(v[0], v[1]));
+        st4(y + c + 2, pack_bf16x2(v[2], v[3]));
+      }
+    }
+  }
+}
+
 }  // namespace
 
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
+  const int out = a.swiglu ? a.N / 2 : a.N;
+  // rows of an expert on average: few are bound by reading the weights once
+  const bool many = a.rows / a.E >= 128;
+  if (many) {
+    const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
+    const int64_t tiles = (a.rows + kTile - 1) / kTile + (a.offset ? a.E : 0);
+    const int64_t blocks = (tiles * pieces + 255) / 256 * 256;
+    hipLaunchKernelGGL(matmul_tile_kernel, dim3((unsigned)blocks), dim3(kTileThreads), 0, stream,
+                       a, pieces, 4);
+    return hipGetLastError();
+  }
   constexpr int MT = 2, NT = 4;
   const int64_t tiles = (a.rows + MT * 16 - 1) / (MT * 16) + (a.offset ? a.E : 0);
-  const int per = a.swiglu ? NT * 8 : NT * 16, out = a.swiglu ? a.N / 2 : a.N;
+  const int per = a.swiglu ? NT * 8 : NT * 16;
   const int pieces = (out + per - 1) / per;
   const int64_t blocks = tiles * pieces < kMaxGrid ? tiles * pieces : kMaxGrid;
   hipLaunchKernelGGL((matmul_split_kernel<MT, NT>), dim3((unsigned)blocks), dim3(kBlock), 0,
