@@ -188,6 +188,32 @@ __device__ __forceinline__ void load_to_lds(Rsrc r, uint32_t offset, lds_u8* to)
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, (int)offset, 0, 0, 0);
 }
 
+// Waits until this wavefront's LDS reads are done and all but its last PENDING
+// memory loads have arrived, then for the workgroup's other wavefronts.
+template <int PENDING>
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | PENDING);        // lgkmcnt(0), vmcnt(PENDING)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Instruction classes of the scheduler's groups.
+constexpr int kIssueMatrix = 0x008, kIssueLdsRead = 0x100;
+
+// Asks for COUNT instructions of a class, each followed by MATRIX matrix
+// instructions.
+template <int CLASS, int COUNT, int MATRIX>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) {
+    __builtin_amdgcn_sched_group_barrier(CLASS, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(kIssueMatrix, MATRIX, 0);
+  }
+}
+
 __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
   __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2 * kStageBytes];   // rows, weights
@@ -240,29 +266,49 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
   const uint32_t at_w = kTileBytes + wn * (64 * kDepth) + place;
   i32x4 acc[MT][NT] = {};
 
+  i32x4 av[2][MT], wv[2][NT];
+  auto read = [&](int h, uint32_t buf) {               // half a stage into registers
+    const uint8_t* pw = s_tile + (at_w ^ (h * 64)) + buf;
+    const uint8_t* pa = s_tile + (at_a ^ (h * 64)) + buf;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) wv[h][j] = *(const i32x4*)(pw + j * 16 * kDepth);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) av[h][i] = *(const i32x4*)(pa + i * 16 * kDepth);
+  };
+  auto multiply = [&](int h, int i0, int i1) {
+#pragma unroll
+    for (int i = i0; i < i1; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[h][j], av[h][i], acc[i][j], 0, 0, 0);
+  };
+
+  // Stage s is in LDS half s % 2.  Within a turn the wavefronts meet once: by
+  // then each has read the last of stage s into registers, and its loads of
+  // stage s + 1, asked for a turn ago, have arrived.  Half of the matrix
+  // instructions of a register set stand on either side of the barrier.
   load(0, 0);
-  __syncthreads();
+  load(kDepth, kStageBytes);
+  meet<8>();                                           // the first stage is there
   uint32_t buf = 0;
+  read(0, 0);
   for (int k0 = 0; k0 < a.K; k0 += kDepth) {
-    load(k0 + kDepth, buf ^ kStageBytes);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      i32x4 av[MT], wv[NT];
-      const uint8_t* pw = s_tile + (at_w ^ (h * 64)) + buf;
-      const uint8_t* pa = s_tile + (at_a ^ (h * 64)) + buf;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) wv[j] = *(const i32x4*)(pw + j * 16 * kDepth);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) av[i] = *(const i32x4*)(pa + i * 16 * kDepth);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[j], av[i], acc[i][j], 0, 0, 0);
-    }
-    __syncthreads();
+    read(1, buf);
+    multiply(0, 0, MT / 2);
+    interleave<kIssueLdsRead, 12, 1>();
+    meet<0>();
+    load(k0 + 2 * kDepth, buf);
+    multiply(0, MT / 2, MT);
     buf ^= kStageBytes;
+    __builtin_amdgcn_sched_barrier(0);
+    read(0, buf);
+    multiply(1, 0, MT);
+    interleave<kIssueLdsRead, 12, 2>();
+    // the reads stay in this turn
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
   }
+  meet<0>();                                           // loads past the end have landed
 
   // a lane's four sums of a tile: channels quarter * 4 .. + 3 of row `row`
   const int out = a.swiglu ? half : a.N;
