@@ -76,7 +76,17 @@ __device__ __forceinline__ Tile find_tile(const MatmulArgs& a, int64_t id, int s
   return {expert, start + (int64_t)tile * size, left < size ? left : size, in / here};
 }
 
-__device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
+// g / (1 + exp(-g)) by the hardware's exponential and reciprocal (1 ulp each;
+// the argument's rounding adds |g| 2^-24): far inside the bf16 rounding that
+// follows, and a tenth of the exact division's instructions.
+__device__ __forceinline__ float silu(float g) {
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+}
+
+__device__ __forceinline__ void st4x2(void* p, uint32_t lo, uint32_t hi) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  *(__attribute__((address_space(1))) u32x2*)(uintptr_t)p = u32x2{lo, hi};
+}
 
 // MT x 16 rows, NT x 16 channels.  With swiglu the channel tiles alternate
 // between gate and up, so that a lane holds both halves of its outputs.
@@ -163,8 +173,7 @@ __global__ __launch_bounds__(kBlock) void matmul_split_kernel(MatmulArgs a, int6
       }
     }
     uint16_t* y = a.y + (t.row + r) * out + c;
-    st4(y, pack_bf16x2(v[0], v[1]));
-    st4(y + 2, pack_bf16x2(v[2], v[3]));
+    st4x2(y, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
   }
   __syncthreads();                                     // s_acc is free again
   }
@@ -214,27 +223,27 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
-  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2 * kStageBytes];   // rows, weights
-  constexpr int MT = 8, NT = 4;
+// One tile whose wavefronts take MT x 16 rows each: 8 for a full tile, 4 or 2
+// for the last rows of a window (as long as reading the weights, but half or
+// a quarter of the products).
+template <int MT>
+__device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t,
+                                              uint8_t* s_tile) {
+  constexpr int NT = 4;
+  constexpr int kLoads = MT / 2 + 4;                   // of a wavefront and stage
+  float* s_scale = reinterpret_cast<float*>(s_tile + 2 * kStageBytes);
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
-  // the 32 tiles that an XCD's compute units hold together are neighbours
-  const int64_t b = blockIdx.x;
-  const int64_t id = b / 256 * 256 + b % 8 * 32 + b / 8 % 32;
-  const Tile t = find_tile(a, id, kTile, pieces, group);
-  if (t.rows == 0) return;
   const int half = a.N / 2;
   const int c0 = t.piece * (a.swiglu ? kTile / 2 : kTile);
 
-  // loads: instruction j of a wavefront fills LDS rows (j * 8 + wave) * 8 + lane / 8
+  // instruction j of a wavefront fills LDS rows (j * 8 + wave) * 8 + lane / 8
   const int lr = lane / 8, chunk = (lane & 7) ^ lr;
-  uint32_t ao[4], wo[4];
+  uint32_t ao[MT / 2], wo[4];
   const bool up = a.swiglu && (wave & 2);              // rows 16..31 of 32: up channels
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int r = (j * 8 + wave) * 8 + lr;
-    ao[j] = (uint32_t)r * (uint32_t)a.K + chunk * 16;
+    if (j < MT / 2) ao[j] = (uint32_t)r * (uint32_t)a.K + chunk * 16;
     const int c = a.swiglu ? r / 32 * 16 + (r & 15) : r;
     wo[j] = (uint32_t)c * (uint32_t)a.K + chunk * 16;
   }
@@ -252,17 +261,33 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
     const bool in = k0 + chunk * 16 < a.K;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      load_to_lds(ra, in ? ao[j] + k0 : kOutside,
-                  (lds_u8*)(s_tile + buf + (j * 8 + wave) * 1024));
+      if (j < MT / 2)
+        load_to_lds(ra, in ? ao[j] + k0 : kOutside,
+                    (lds_u8*)(s_tile + buf + (j * 8 + wave) * 1024));
       load_to_lds(rw, in ? wo[j] + k0 : kOutside,
                   (lds_u8*)(s_tile + buf + kTileBytes + (j * 8 + wave) * 1024));
     }
   };
+  // scales of the tile's rows and channels (LDS order), for the end
+  float scale = 0.0f;
+  {
+    const int n = threadIdx.x & 255;
+    if (threadIdx.x < 256) {
+      if (n < t.rows) scale = a.a_scales[(t.row + n) * a.a_scale_pitch];
+    } else {
+      const int c = a.swiglu ? n / 32 * 16 + (n & 15) : n;
+      if (c < channels)
+        scale = a.w_scales[(int64_t)t.expert * a.N + c0 + c + (a.swiglu && (n & 16) ? half : 0)];
+    }
+  }
+  load(0, 0);
+  load(kDepth, kStageBytes);
+  s_scale[threadIdx.x] = scale;
 
   const int wm = wave / 4, wn = wave % 4;              // 2 x 4 wavefronts
   const int row = lane & 15, quarter = lane / 16;
   const uint32_t place = row * kDepth + ((quarter ^ (row & 7)) * 16);
-  const uint32_t at_a = wm * (128 * kDepth) + place;
+  const uint32_t at_a = wm * (MT * 16 * kDepth) + place;
   const uint32_t at_w = kTileBytes + wn * (64 * kDepth) + place;
   i32x4 acc[MT][NT] = {};
 
@@ -287,15 +312,13 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
   // then each has read the last of stage s into registers, and its loads of
   // stage s + 1, asked for a turn ago, have arrived.  Half of the matrix
   // instructions of a register set stand on either side of the barrier.
-  load(0, 0);
-  load(kDepth, kStageBytes);
-  meet<8>();                                           // the first stage is there
+  meet<kLoads>();                                      // the first stage is there
   uint32_t buf = 0;
   read(0, 0);
   for (int k0 = 0; k0 < a.K; k0 += kDepth) {
     read(1, buf);
     multiply(0, 0, MT / 2);
-    interleave<kIssueLdsRead, 12, 1>();
+    interleave<kIssueLdsRead, MT + NT, 1>();
     meet<0>();
     load(k0 + 2 * kDepth, buf);
     multiply(0, MT / 2, MT);
@@ -303,7 +326,7 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
     __builtin_amdgcn_sched_barrier(0);
     read(0, buf);
     multiply(1, 0, MT);
-    interleave<kIssueLdsRead, 12, 2>();
+    interleave<kIssueLdsRead, MT + NT, MT / 4 + 1 < 2 ? 1 : 2>();
     // the reads stay in this turn
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
@@ -311,41 +334,46 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
   meet<0>();                                           // loads past the end have landed
 
   // a lane's four sums of a tile: channels quarter * 4 .. + 3 of row `row`
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
   const int out = a.swiglu ? half : a.N;
-  const float* sw0 = a.w_scales + (int64_t)t.expert * a.N;
+  f32x4 sw[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+    sw[j] = *(const f32x4*)(s_scale + 256 + wn * 64 + j * 16 + quarter * 4);
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int r = wm * 128 + i * 16 + row;
+    const int r = wm * (MT * 16) + i * 16 + row;
     if (r >= t.rows) continue;
-    const float sa = a.a_scales[(t.row + r) * a.a_scale_pitch];
+    const float sa = s_scale[r];
     uint16_t* y = a.y + (t.row + r) * out;
-    if (a.swiglu) {
 #pragma unroll
-      for (int j = 0; j < NT; j += 2) {
-        const int c = c0 + wn * 32 + j * 8 + quarter * 4;
-        if (c >= out) continue;
-        float v[4];
+    for (int j = 0; j < NT; ++j) {
+      if (a.swiglu && (j & 1)) continue;
+      const int c = c0 + (a.swiglu ? wn * 32 + j * 8 : wn * 64 + j * 16) + quarter * 4;
+      if (c >= out) continue;
+      float v[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float g = (float)acc[i][j][q] * (sa * sw0[c + q]);
-          v[q] = silu(g) * ((float)acc[i][j + 1][q] * (sa * sw0[half + c + q]));
-        }
-        st4(y + c, pack_bf16x2(v[0], v[1]));
-        st4(y + c + 2, pack_bf16x2(v[2], v[3]));
+      for (int q = 0; q < 4; ++q) {
+        v[q] = (float)acc[i][j][q] * (sa * sw[j][q]);
+        if (a.swiglu) v[q] = silu(v[q]) * ((float)acc[i][j | 1][q] * (sa * sw[j | 1][q]));
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int c = c0 + wn * 64 + j * 16 + quarter * 4;
-        if (c >= out) continue;
-        float v[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = (float)acc[i][j][q] * (sa * sw0[c + q]);
-        st4(y + c, pack_bf16x2(v[0], v[1]));
-        st4(y + c + 2, pack_bf16x2(v[2], v[3]));
-      }
+      st4x2(y + c, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
   }
+}
+
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
+  // two stages of rows and weights, then the scales of rows and channels
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2 * kStageBytes + 2 * kTile * 4];
+  // the 32 tiles that an XCD's compute units hold together are neighbours
+  const int64_t b = blockIdx.x;
+  const int64_t id = b / 256 * 256 + b % 8 * 32 + b / 8 % 32;
+  const Tile t = find_tile(a, id, kTile, pieces, group);
+  if (t.rows == 0) return;
+  if (t.rows > 128) multiply_tile<8>(a, t, s_tile);
+  else if (t.rows > 64) multiply_tile<4>(a, t, s_tile);
+  else multiply_tile<2>(a, t, s_tile);
 }
 
 }  // namespace
