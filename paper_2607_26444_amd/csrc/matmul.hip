@@ -1,10 +1,5 @@
-// The experts' products on 8-bit integers.
-//
-// A workgroup takes ROWS rows of one expert's window and CHANNELS of its channels; its
-// four wavefronts take every fourth piece of the depth and add their int32
-// sums in LDS (integer sums: exact in any order).  The operands go from
-// memory into the matrix instructions' registers: weights are read once by one
-// workgroup, rows again by each workgroup along the channels, from the caches.
+// The experts' products on 8-bit integers: int32 sums by matrix instructions,
+// exact in any order, scaled and rounded to bf16 once.
 
 #include "layer.h"
 
@@ -88,111 +83,23 @@ __device__ __forceinline__ void st4x2(void* p, uint32_t lo, uint32_t hi) {
   *(__attribute__((address_space(1))) u32x2*)(uintptr_t)p = u32x2{lo, hi};
 }
 
-// MT x 16 rows, NT x 16 channels.  With swiglu the channel tiles alternate
-// between gate and up, so that a lane holds both halves of its outputs.
-template <int MT, int NT>
-__global__ __launch_bounds__(kBlock) void matmul_split_kernel(MatmulArgs a, int64_t tiles,
-                                                                int pieces) {
-  __shared__ i32x4 s_acc[kWavesPerBlock][MT * NT][kWave];
-  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
-  const int row = lane & 15, piece = lane / 16;
-  const int half = a.N / 2;
-  for (int64_t id = blockIdx.x; id < tiles * pieces; id += gridDim.x) {
-  const Tile t = find_tile(a, id, MT * 16, pieces, 1);
-  if (t.rows == 0) continue;                           // the whole workgroup
-  const int c0 = t.piece * (a.swiglu ? NT * 8 : NT * 16);   // first (gate) channel
-
-  // A matrix instruction takes 64 of the depth, 16 bytes per lane.  Lanes read
-  // 32 neighbouring bytes for two of them, so that four lanes cover a line of
-  // a row; both operands are permuted alike.
-  const Rsrc ra = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t*>(a.a + t.row * a.K), (short)0, t.rows * a.K, kRsrcWord3);
-  uint32_t ao[MT], wo[NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) ao[i] = (uint32_t)(i * 16 + row) * (uint32_t)a.K + piece * 32;
-  const uint8_t* wbase = a.w + (int64_t)t.expert * a.N * a.K;
-  Rsrc rw[NT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    int c = a.swiglu ? c0 + (j / 2) * 16 + (j & 1) * half : c0 + j * 16;
-    int n = (a.swiglu ? (j & 1 ? a.N : half) : a.N) - c;       // channels that are there
-    if (n < 0) c = 0, n = 0;
-    rw[j] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wbase + (int64_t)c * a.K),
-                                              (short)0, (n < 16 ? n : 16) * a.K, kRsrcWord3);
-    wo[j] = (uint32_t)row * (uint32_t)a.K + piece * 32;
-  }
-
-  i32x4 acc[MT][NT] = {};
-  for (int k0 = wave * 128; k0 < a.K; k0 += kWavesPerBlock * 128) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int k = k0 + h * 16;
-      const bool in = k + piece * 32 < a.K;            // past the depth: zeros
-      i32x4 av[MT], wv[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        wv[j] = (i32x4)__builtin_amdgcn_raw_buffer_load_b128(rw[j], in ? wo[j] + k : kOutside, 0, 0);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-        av[i] = (i32x4)__builtin_amdgcn_raw_buffer_load_b128(ra, in ? ao[i] + k : kOutside, 0, 0);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[j], av[i], acc[i][j], 0, 0, 0);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) s_acc[wave][i * NT + j][lane] = acc[i][j];
-  __syncthreads();
-
-  // A lane's four sums of a tile: channels piece * 4 .. + 3 of row `row`.
-  const int step = a.swiglu ? 2 : 1;
-  const int out = a.swiglu ? half : a.N;
-  for (int i = wave * step; i < MT * NT; i += kWavesPerBlock * step) {
-    const int m = i / NT, j = i % NT;
-    const int r = m * 16 + row;
-    const int c = c0 + (a.swiglu ? j / 2 : j) * 16 + piece * 4;
-    if (r >= t.rows || c >= out) continue;
-    const float sa = a.a_scales[(t.row + r) * a.a_scale_pitch];
-    const float* sw = a.w_scales + (int64_t)t.expert * a.N + c;
-    float v[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      int sum = 0;
-#pragma unroll
-      for (int p = 0; p < kWavesPerBlock; ++p) sum += s_acc[p][i][lane][q];
-      v[q] = (float)sum * (sa * sw[q]);
-      if (a.swiglu) {
-        int up = 0;
-#pragma unroll
-        for (int p = 0; p < kWavesPerBlock; ++p) up += s_acc[p][i + 1][lane][q];
-        v[q] = silu(v[q]) * ((float)up * (sa * sw[half + q]));
-      }
-    }
-    uint16_t* y = a.y + (t.row + r) * out + c;
-    st4x2(y, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-  }
-  __syncthreads();                                     // s_acc is free again
-  }
+// Buffer resource of `bytes` bytes from `base`, both the same in every lane.
+__device__ __forceinline__ Rsrc buffer_of(const uint8_t* base, int bytes) {
+  const uint64_t p = (uint64_t)base;
+  const uint32_t lo = (uint32_t)uniform((int)(uint32_t)p), hi = (uint32_t)uniform((int)(p >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(((uint64_t)hi << 32) | lo),
+                                           (short)0, uniform(bytes), kRsrcWord3);
 }
-
-// Tiles of 256 rows x 256 channels through LDS: eight wavefronts, each 128 rows
-// x 64 channels; pieces of 128 of the depth go from memory into LDS by the
-// loads themselves, one piece ahead of the matrix instructions.
-//
-// LDS holds a row's 128 bytes as eight chunks of 16, chunk c of row r at place
-// c ^ (r & 7), so that eight lanes that read one chunk of eight rows touch all
-// banks.
-constexpr int kTile = 256, kDepth = 128;
-constexpr int kTileThreads = 512;
-constexpr int kTileBytes = kTile * kDepth;
-constexpr int kStageBytes = 2 * kTileBytes;
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 
+// LDS rows are 128 bytes of the depth, as eight chunks of 16: chunk c of row r at
+// place c ^ (r & 7), so that eight lanes that read one chunk of eight rows
+// touch all banks.
+constexpr int kDepth = 128;
+
+// One load instruction of a wavefront: eight rows of 128 bytes from memory into
+// the 1 KiB of LDS at `to`.
 __device__ __forceinline__ void load_to_lds(Rsrc r, uint32_t offset, lds_u8* to) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, (int)offset, 0, 0, 0);
 }
@@ -203,11 +110,20 @@ template <int PENDING>
 __device__ __forceinline__ void meet() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070 | PENDING);        // lgkmcnt(0), vmcnt(PENDING)
+  // lgkmcnt(0), vmcnt(PENDING), in the instruction's bit fields
+  __builtin_amdgcn_s_waitcnt(0x0070 | (PENDING & 15) | (PENDING >> 4) << 14);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
+
+// Tiles of 256 rows x 256 channels through LDS: eight wavefronts, each 128 rows
+// x 64 channels; pieces of 128 of the depth go from memory into LDS by the
+// loads themselves, one piece ahead of the matrix instructions.
+constexpr int kTile = 256;
+constexpr int kTileThreads = 512;
+constexpr int kTileBytes = kTile * kDepth;
+constexpr int kStageBytes = 2 * kTileBytes;
 
 // Instruction classes of the scheduler's groups.
 constexpr int kIssueMatrix = 0x008, kIssueLdsRead = 0x100;
@@ -252,10 +168,7 @@ __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t
   const uint8_t* abase = a.a + t.row * a.K;
   const uint8_t* wbase = a.w + ((int64_t)t.expert * a.N + c0 + (up ? half : 0)) * a.K;
   const int arange = t.rows * a.K, wrange = (channels < most ? channels : most) * a.K;
-  const Rsrc ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(abase), (short)0, arange,
-                                                    kRsrcWord3);
-  const Rsrc rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wbase), (short)0, wrange,
-                                                    kRsrcWord3);
+  const Rsrc ra = buffer_of(abase, arange), rw = buffer_of(wbase, wrange);
   // past the depth and past the tile's rows and channels: zeros
   auto load = [&](int k0, uint32_t buf) {
     const bool in = k0 + chunk * 16 < a.K;
@@ -376,6 +289,129 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
   else multiply_tile<2>(a, t, s_tile);
 }
 
+// Few rows: up to 64 rows of a window x 16 WC channels, bound by reading the
+// weights.  Eight wavefronts, WC along the channels and WK along the depth; a
+// stage is 128 WK of the depth, STAGES - 1 stages are on their way while one is
+// multiplied.  A wavefront loads its own weights (8 + 8 channels: with swiglu
+// gate and up channels, so that a lane and its partner 32 further on hold both
+// halves) and an eighth of the rows.  The sums of the WK wavefronts meet in
+// LDS.
+template <int WC, int WK, int STAGES>
+__global__ __launch_bounds__(kTileThreads, 4)
+void matmul_stream_kernel(MatmulArgs a, int64_t first, int pieces) {
+  static_assert(WC * WK == 8, "eight wavefronts");
+  constexpr int kRows = 64, MT = kRows / 16;
+  constexpr int kRowBytes = kRows * kDepth * WK, kStage = kRowBytes + 16 * 1024;
+  constexpr int kLoads = 2 + WK;                       // of a wavefront and stage
+  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[STAGES * kStage];
+  static_assert(STAGES * kStage >= 8 * MT * kWave * 16, "sums meet there");
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  // 32 neighbouring tiles (mostly one window's, which share rows) to an XCD
+  const int64_t b = first + blockIdx.x;
+  const Tile t = find_tile(a, b / 256 * 256 + b % 8 * 32 + b / 8 % 32, kRows, pieces, 1);
+  if (t.rows == 0) return;                             // the whole workgroup
+  const int half = a.N / 2, out = a.swiglu ? half : a.N;
+  const int wc = wave % WC, wk = wave / WC;
+  const int step = a.swiglu ? 8 : 16;                  // output channels of a wavefront
+  const int c0 = t.piece * WC * step + wc * step;
+
+  const int lr = lane / 8, chunk = (lane & 7) ^ lr;
+  const Rsrc ra = buffer_of(a.a + t.row * a.K, t.rows * a.K);
+  const uint8_t* wbase = a.w + ((int64_t)t.expert * a.N + c0) * a.K;
+  const int c1 = a.swiglu ? c0 : c0 + 8;               // channels come in whole eights
+  const Rsrc rw0 = buffer_of(wbase, c0 < out ? 8 * a.K : 0);
+  const Rsrc rw1 = buffer_of(wbase + (int64_t)(a.swiglu ? half : 8) * a.K, c1 < out ? 8 * a.K : 0);
+  const uint32_t ao = (uint32_t)(wave * 8 + lr) * (uint32_t)a.K + chunk * 16;
+  const uint32_t wo = (uint32_t)lr * (uint32_t)a.K + wk * kDepth + chunk * 16;
+  auto load = [&](int k0, uint32_t at) {               // past the depth: zeros
+    const uint32_t w = (uint32_t)k0 + wk * kDepth + chunk * 16 < (uint32_t)a.K ? wo + k0 : kOutside;
+    uint8_t* to = s_mem + at + kRowBytes + wave * 2048;
+    load_to_lds(rw0, w, (lds_u8*)to);
+    load_to_lds(rw1, w, (lds_u8*)(to + 1024));
+#pragma unroll
+    for (int g = 0; g < WK; ++g) {
+      const uint32_t k = (uint32_t)k0 + g * kDepth;
+      load_to_lds(ra, k + chunk * 16 < (uint32_t)a.K ? ao + k : kOutside,
+                  (lds_u8*)(s_mem + at + g * (kRows * kDepth) + wave * 1024));
+    }
+  };
+#pragma unroll
+  for (int s = 0; s + 1 < STAGES; ++s) load(s * kDepth * WK, s * kStage);
+
+  const int row = lane & 15, quarter = lane / 16;
+  const uint32_t place = row * kDepth + ((quarter ^ (row & 7)) * 16);
+  i32x4 acc[MT] = {};
+  auto multiply = [&](auto row_tiles) {
+    constexpr int M = row_tiles.value;
+    uint32_t at = 0, fill = (STAGES - 1) * kStage;     // stage to read, stage to fill
+    for (int k0 = 0; k0 < a.K; k0 += kDepth * WK) {
+      meet<(STAGES - 2) * kLoads>();                   // this stage is there, the last is read
+      load(k0 + (STAGES - 1) * kDepth * WK, fill);
+      i32x4 wv[2], av[2][M];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t p = at + (place ^ (h * 64));
+        wv[h] = *(const i32x4*)(s_mem + kRowBytes + wave * 2048 + p);
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+          av[h][i] = *(const i32x4*)(s_mem + wk * (kRows * kDepth) + i * 16 * kDepth + p);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+          acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[h], av[h][i], acc[i], 0, 0, 0);
+      at = at + kStage == STAGES * kStage ? 0 : at + kStage;
+      fill = fill + kStage == STAGES * kStage ? 0 : fill + kStage;
+    }
+  };
+  const int mt = (t.rows + 15) / 16;
+  if (mt == 1) multiply(std::integral_constant<int, 1>());
+  else if (mt == 2) multiply(std::integral_constant<int, 2>());
+  else multiply(std::integral_constant<int, 4>());
+  meet<0>();                                           // loads past the end have landed
+
+  i32x4* s_acc = reinterpret_cast<i32x4*>(s_mem);      // [wavefront][row tile][lane]
+#pragma unroll
+  for (int i = 0; i < MT; ++i) s_acc[(wave * MT + i) * kWave + lane] = acc[i];
+  __syncthreads();
+  // tile (w, i): channels of wavefront column w, rows 16 i..; a lane's four
+  // sums are channels quarter * 4 .. + 3 of row `row`
+  for (int n = wave; n < WC * mt; n += 8) {
+    const int w = n % WC, i = n / WC;
+    const int r = i * 16 + row;
+    i32x4 sum = s_acc[(w * MT + i) * kWave + lane];
+#pragma unroll
+    for (int g = 1; g < WK; ++g) sum += s_acc[((g * WC + w) * MT + i) * kWave + lane];
+    const int c = (t.piece * WC + w) * step + (quarter * 4) % step;
+    const bool in = r < t.rows && c < out;
+    const float sa = in ? a.a_scales[(t.row + r) * a.a_scale_pitch] : 0.0f;
+    const float* sw = a.w_scales + (int64_t)t.expert * a.N + c + (a.swiglu && quarter > 1 ? half : 0);
+    float v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v[q] = (float)sum[q] * (in ? sa * sw[q] : 0.0f);
+      if (a.swiglu) v[q] = silu(v[q]) * __shfl_xor(v[q], 32, kWave);   // gate lanes, up lanes
+    }
+    if (in && !(a.swiglu && quarter > 1))
+      st4x2(a.y + (t.row + r) * out + c, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
+}
+
+template <int WC, int WK, int STAGES>
+hipError_t launch_stream(const MatmulArgs& a, int out, hipStream_t stream) {
+  const int per = WC * (a.swiglu ? 8 : 16), pieces = (out + per - 1) / per;
+  const int64_t tiles = ((a.rows + 63) / 64 + (a.offset ? a.E : 0)) * pieces;
+  const int64_t blocks = (tiles + 255) / 256 * 256;
+  for (int64_t first = 0; first < blocks; first += kMaxGrid) {   // one launch, in practice
+    const int64_t left = blocks - first;
+    hipLaunchKernelGGL((matmul_stream_kernel<WC, WK, STAGES>),
+                       dim3((unsigned)(left < kMaxGrid ? left : kMaxGrid)), dim3(kTileThreads), 0,
+                       stream, a, first, pieces);
+  }
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
@@ -390,14 +426,7 @@ hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
                        a, pieces, 4);
     return hipGetLastError();
   }
-  constexpr int MT = 2, NT = 4;
-  const int64_t tiles = (a.rows + MT * 16 - 1) / (MT * 16) + (a.offset ? a.E : 0);
-  const int per = a.swiglu ? NT * 8 : NT * 16;
-  const int pieces = (out + per - 1) / per;
-  const int64_t blocks = tiles * pieces < kMaxGrid ? tiles * pieces : kMaxGrid;
-  hipLaunchKernelGGL((matmul_split_kernel<MT, NT>), dim3((unsigned)blocks), dim3(kBlock), 0,
-                     stream, a, tiles, pieces);
-  return hipGetLastError();
+  return launch_stream<8, 1, 3>(a, out, stream);
 }
 
 }  // namespace moe
