@@ -1,6 +1,8 @@
 // The experts' products on 8-bit integers: int32 sums by matrix instructions,
 // exact in any order, scaled and rounded to bf16 once.
 
+#include <type_traits>
+
 #include "layer.h"
 
 namespace moe {
@@ -19,56 +21,59 @@ struct Tile {
   int piece;
 };
 
+// Inclusive sum over the wavefront's lanes.
+__device__ __forceinline__ int scan_add(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return x;
+}
+
 // Tile `id` of the order expert, group of `group` row tiles, channel piece, row
 // tile in the group, so that neighbouring tiles share rows or weights.  A row
 // tile has `size` rows, a window `pieces` channel pieces.
-__device__ __forceinline__ Tile find_tile(const MatmulArgs& a, int64_t id, int size, int pieces,
+__device__ __forceinline__ Tile find_tile(const MatmulArgs& a, int id, int size, int pieces,
                                           int group) {
-  int expert = 0;
-  int64_t start = 0, n = a.rows, before = 0;
+  int expert = 0, start = 0, n = (int)a.rows, before = 0;
   if (a.offset) {
-    const int lane = threadIdx.x & (kWave - 1);
+    const int lane = threadIdx.x & (kWave - 1), rows = (int)a.rows;
     const int first = uniform((int)ld4(a.offset));
     n = 0;
     for (int e0 = 0; e0 < a.E; e0 += kWave) {
-      const int e = e0 + lane;
-      int64_t s = 0, m = 0;
-      if (e < a.E) {
-        const int o = (int)ld4(a.offset + e);
-        s = (int64_t)o - first;
-        m = a.count ? (int64_t)(int)ld4(a.count + e) : (int64_t)(int)ld4(a.offset + e + 1) - o;
-        if (s < 0 || s > a.rows) m = 0;
-        if (m > a.rows - s) m = a.rows - s;
-        if (m < 0) m = 0;
-      }
-      const int tiles = (int)((m + size - 1) / size);
-      int sum = tiles;                                 // inclusive over the lanes
-#pragma unroll
-      for (int d = 1; d < kWave; d *= 2) {
-        const int o = __shfl_up(sum, d, kWave);
-        if (lane >= d) sum += o;
-      }
-      const uint64_t hit = __ballot((before + sum) * pieces > id);
+      const int e = e0 + lane < a.E ? e0 + lane : a.E - 1;
+      const int o = (int)ld4(a.offset + e);
+      const int64_t s64 = (int64_t)o - first;
+      int64_t m64 = a.count ? (int64_t)(int)ld4(a.count + e)
+                            : (int64_t)(int)ld4(a.offset + e + 1) - o;
+      const bool in = e0 + lane < a.E && s64 >= 0 && s64 <= rows && m64 > 0;
+      const int s = in ? (int)s64 : 0;
+      const int m = in ? (int)(m64 < rows - s64 ? m64 : rows - s64) : 0;
+      const int tiles = (m + size - 1) / size;
+      const int sum = before + scan_add(tiles);        // inclusive over the lanes
+      const uint64_t hit = __ballot((int64_t)sum * pieces > id);
       if (hit) {
         const int l = __builtin_ctzll(hit);
         expert = e0 + l;
-        before += __builtin_amdgcn_readlane(sum - tiles, l);
-        start = (int64_t)readlane64((uint64_t)s, l);
-        n = (int64_t)readlane64((uint64_t)m, l);
+        before = __builtin_amdgcn_readlane(sum - tiles, l);
+        start = __builtin_amdgcn_readlane(s, l);
+        n = __builtin_amdgcn_readlane(m, l);
         break;
       }
-      before += __builtin_amdgcn_readlane(sum, kWave - 1);
+      before = __builtin_amdgcn_readlane(sum, kWave - 1);
     }
   }
-  const int tiles = (int)((n + size - 1) / size);
-  const int64_t at = id - before * pieces;
-  if (at >= (int64_t)tiles * pieces) return {0, 0, 0, 0};
+  const int tiles = (n + size - 1) / size;
+  const int at = id - before * pieces;
+  if (at >= tiles * pieces) return {0, 0, 0, 0};
   const int per = group * pieces;
-  const int g = (int)at / per, in = (int)at % per;      // below 2^31: tiles of one launch
+  const int g = at / per, in = at % per;
   const int here = tiles - g * group < group ? tiles - g * group : group;   // tiles of this group
   const int tile = g * group + in % here;
-  const int left = (int)(n - (int64_t)tile * size);
-  return {expert, start + (int64_t)tile * size, left < size ? left : size, in / here};
+  const int left = n - tile * size;
+  return {expert, (int64_t)start + (int64_t)tile * size, left < size ? left : size, in / here};
 }
 
 // g / (1 + exp(-g)) by the hardware's exponential and reciprocal (1 ulp each;
@@ -280,8 +285,8 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
   // two stages of rows and weights, then the scales of rows and channels
   __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2 * kStageBytes + 2 * kTile * 4];
   // the 32 tiles that an XCD's compute units hold together are neighbours
-  const int64_t b = blockIdx.x;
-  const int64_t id = b / 256 * 256 + b % 8 * 32 + b / 8 % 32;
+  const int b = blockIdx.x;
+  const int id = b / 256 * 256 + b % 8 * 32 + b / 8 % 32;
   const Tile t = find_tile(a, id, kTile, pieces, group);
   if (t.rows == 0) return;
   if (t.rows > 128) multiply_tile<8>(a, t, s_tile);
@@ -289,26 +294,30 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
   else multiply_tile<2>(a, t, s_tile);
 }
 
-// Few rows: up to 64 rows of a window x 16 WC channels, bound by reading the
+// Few rows: ROWS rows of a window x 16 WC channels, bound by reading the
 // weights.  Eight wavefronts, WC along the channels and WK along the depth; a
 // stage is 128 WK of the depth, STAGES - 1 stages are on their way while one is
 // multiplied.  A wavefront loads its own weights (8 + 8 channels: with swiglu
 // gate and up channels, so that a lane and its partner 32 further on hold both
 // halves) and an eighth of the rows.  The sums of the WK wavefronts meet in
 // LDS.
-template <int WC, int WK, int STAGES>
-__global__ __launch_bounds__(kTileThreads, 4)
-void matmul_stream_kernel(MatmulArgs a, int64_t first, int pieces) {
+template <int ROWS, int WC, int WK, int STAGES>
+__global__ __launch_bounds__(kTileThreads)
+void matmul_stream_kernel(MatmulArgs a, int pieces) {
   static_assert(WC * WK == 8, "eight wavefronts");
-  constexpr int kRows = 64, MT = kRows / 16;
-  constexpr int kRowBytes = kRows * kDepth * WK, kStage = kRowBytes + 16 * 1024;
-  constexpr int kLoads = 2 + WK;                       // of a wavefront and stage
-  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[STAGES * kStage];
+  constexpr int MT = ROWS / 16;
+  constexpr int kRowBytes = ROWS * kDepth * WK, kStage = kRowBytes + 16 * 1024;
+  constexpr int kRowLoads = WK * ROWS / 64;            // of a wavefront and stage
+  constexpr int kLoads = 2 + kRowLoads;
+  static_assert(kRowLoads * 64 == WK * ROWS, "whole load instructions");
+  // the stages, then the scales of the rows and of the channels (gate | up)
+  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[STAGES * kStage + (ROWS + 16 * WC) * 4];
   static_assert(STAGES * kStage >= 8 * MT * kWave * 16, "sums meet there");
+  float* s_scale = reinterpret_cast<float*>(s_mem + STAGES * kStage);
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   // 32 neighbouring tiles (mostly one window's, which share rows) to an XCD
-  const int64_t b = first + blockIdx.x;
-  const Tile t = find_tile(a, b / 256 * 256 + b % 8 * 32 + b / 8 % 32, kRows, pieces, 1);
+  const int b = blockIdx.x;
+  const Tile t = find_tile(a, b / 256 * 256 + b % 8 * 32 + b / 8 % 32, ROWS, pieces, 1);
   if (t.rows == 0) return;                             // the whole workgroup
   const int half = a.N / 2, out = a.swiglu ? half : a.N;
   const int wc = wave % WC, wk = wave / WC;
@@ -321,7 +330,6 @@ void matmul_stream_kernel(MatmulArgs a, int64_t first, int pieces) {
   const int c1 = a.swiglu ? c0 : c0 + 8;               // channels come in whole eights
   const Rsrc rw0 = buffer_of(wbase, c0 < out ? 8 * a.K : 0);
   const Rsrc rw1 = buffer_of(wbase + (int64_t)(a.swiglu ? half : 8) * a.K, c1 < out ? 8 * a.K : 0);
-  const uint32_t ao = (uint32_t)(wave * 8 + lr) * (uint32_t)a.K + chunk * 16;
   const uint32_t wo = (uint32_t)lr * (uint32_t)a.K + wk * kDepth + chunk * 16;
   auto load = [&](int k0, uint32_t at) {               // past the depth: zeros
     const uint32_t w = (uint32_t)k0 + wk * kDepth + chunk * 16 < (uint32_t)a.K ? wo + k0 : kOutside;
@@ -329,14 +337,23 @@ void matmul_stream_kernel(MatmulArgs a, int64_t first, int pieces) {
     load_to_lds(rw0, w, (lds_u8*)to);
     load_to_lds(rw1, w, (lds_u8*)(to + 1024));
 #pragma unroll
-    for (int g = 0; g < WK; ++g) {
-      const uint32_t k = (uint32_t)k0 + g * kDepth;
-      load_to_lds(ra, k + chunk * 16 < (uint32_t)a.K ? ao + k : kOutside,
-                  (lds_u8*)(s_mem + at + g * (kRows * kDepth) + wave * 1024));
+    for (int g = 0; g < kRowLoads; ++g) {              // eight rows of a 128 of the depth
+      const int n = g * 8 + wave, r = n % (ROWS / 8) * 8 + lr;
+      const uint32_t k = (uint32_t)k0 + n / (ROWS / 8) * kDepth + chunk * 16;
+      load_to_lds(ra, k < (uint32_t)a.K ? (uint32_t)r * (uint32_t)a.K + k : kOutside,
+                  (lds_u8*)(s_mem + at + n * 1024));
     }
   };
+  float scale = 0.0f;
+  if ((int)threadIdx.x < ROWS) {
+    if ((int)threadIdx.x < t.rows) scale = a.a_scales[(t.row + threadIdx.x) * a.a_scale_pitch];
+  } else if (threadIdx.x < ROWS + 16 * WC) {
+    const int n = threadIdx.x - ROWS, c = t.piece * WC * step + n % (WC * step);
+    if (c < out) scale = a.w_scales[(int64_t)t.expert * a.N + c + (n < WC * step ? 0 : half)];
+  }
 #pragma unroll
   for (int s = 0; s + 1 < STAGES; ++s) load(s * kDepth * WK, s * kStage);
+  if (threadIdx.x < ROWS + 16 * WC) s_scale[threadIdx.x] = scale;
 
   const int row = lane & 15, quarter = lane / 16;
   const uint32_t place = row * kDepth + ((quarter ^ (row & 7)) * 16);
@@ -354,7 +371,7 @@ void matmul_stream_kernel(MatmulArgs a, int64_t first, int pieces) {
         wv[h] = *(const i32x4*)(s_mem + kRowBytes + wave * 2048 + p);
 #pragma unroll
         for (int i = 0; i < M; ++i)
-          av[h][i] = *(const i32x4*)(s_mem + wk * (kRows * kDepth) + i * 16 * kDepth + p);
+          av[h][i] = *(const i32x4*)(s_mem + wk * (ROWS * kDepth) + i * 16 * kDepth + p);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -366,9 +383,9 @@ void matmul_stream_kernel(MatmulArgs a, int64_t first, int pieces) {
     }
   };
   const int mt = (t.rows + 15) / 16;
-  if (mt == 1) multiply(std::integral_constant<int, 1>());
-  else if (mt == 2) multiply(std::integral_constant<int, 2>());
-  else multiply(std::integral_constant<int, 4>());
+  if (ROWS == 16 || mt == 1) multiply(std::integral_constant<int, 1>());
+  else if (mt == 2) multiply(std::integral_constant<int, ROWS == 16 ? 1 : 2>());
+  else multiply(std::integral_constant<int, MT>());
   meet<0>();                                           // loads past the end have landed
 
   i32x4* s_acc = reinterpret_cast<i32x4*>(s_mem);      // [wavefront][row tile][lane]
@@ -383,14 +400,14 @@ void matmul_stream_kernel(MatmulArgs a, int64_t first, int pieces) {
     i32x4 sum = s_acc[(w * MT + i) * kWave + lane];
 #pragma unroll
     for (int g = 1; g < WK; ++g) sum += s_acc[((g * WC + w) * MT + i) * kWave + lane];
-    const int c = (t.piece * WC + w) * step + (quarter * 4) % step;
+    const int lc = w * step + (quarter * 4) % step, c = t.piece * WC * step + lc;
     const bool in = r < t.rows && c < out;
-    const float sa = in ? a.a_scales[(t.row + r) * a.a_scale_pitch] : 0.0f;
-    const float* sw = a.w_scales + (int64_t)t.expert * a.N + c + (a.swiglu && quarter > 1 ? half : 0);
+    const float sa = s_scale[r];
+    const float* sw = s_scale + ROWS + lc + (a.swiglu && quarter > 1 ? WC * step : 0);
     float v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      v[q] = (float)sum[q] * (in ? sa * sw[q] : 0.0f);
+      v[q] = (float)sum[q] * (sa * sw[q]);
       if (a.swiglu) v[q] = silu(v[q]) * __shfl_xor(v[q], 32, kWave);   // gate lanes, up lanes
     }
     if (in && !(a.swiglu && quarter > 1))
@@ -398,17 +415,18 @@ void matmul_stream_kernel(MatmulArgs a, int64_t first, int pieces) {
   }
 }
 
-template <int WC, int WK, int STAGES>
+// Tiles of one launch: HIP's limit of 2^32 threads.  The outputs and weights of more would not
+// fit a GPU's memory.
+constexpr int64_t kMaxTiles = (1ll << 32) / kTileThreads - 256;
+
+template <int ROWS, int WC, int WK, int STAGES>
 hipError_t launch_stream(const MatmulArgs& a, int out, hipStream_t stream) {
   const int per = WC * (a.swiglu ? 8 : 16), pieces = (out + per - 1) / per;
-  const int64_t tiles = ((a.rows + 63) / 64 + (a.offset ? a.E : 0)) * pieces;
-  const int64_t blocks = (tiles + 255) / 256 * 256;
-  for (int64_t first = 0; first < blocks; first += kMaxGrid) {   // one launch, in practice
-    const int64_t left = blocks - first;
-    hipLaunchKernelGGL((matmul_stream_kernel<WC, WK, STAGES>),
-                       dim3((unsigned)(left < kMaxGrid ? left : kMaxGrid)), dim3(kTileThreads), 0,
-                       stream, a, first, pieces);
-  }
+  const int64_t tiles = ((a.rows + ROWS - 1) / ROWS + (a.offset ? a.E : 0)) * pieces;
+  if (tiles > kMaxTiles) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((matmul_stream_kernel<ROWS, WC, WK, STAGES>),
+                     dim3((unsigned)((tiles + 255) / 256 * 256)), dim3(kTileThreads), 0, stream, a,
+                     pieces);
   return hipGetLastError();
 }
 
@@ -416,17 +434,33 @@ hipError_t launch_stream(const MatmulArgs& a, int out, hipStream_t stream) {
 
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
   const int out = a.swiglu ? a.N / 2 : a.N;
-  // rows of an expert on average: few are bound by reading the weights once
-  const bool many = a.rows / a.E >= 128;
-  if (many) {
-    const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
-    const int64_t tiles = (a.rows + kTile - 1) / kTile + (a.offset ? a.E : 0);
-    const int64_t blocks = (tiles * pieces + 255) / 256 * 256;
-    hipLaunchKernelGGL(matmul_tile_kernel, dim3((unsigned)blocks), dim3(kTileThreads), 0, stream,
-                       a, pieces, 4);
+  // Many rows: the tile kernel, from 64 rows to an expert and 128 full tiles.
+  // Below either, its tiles leave compute units idle or read the weights no
+  // faster (us, tile / stream): 2048 rows, 32 experts, 7168 x 4096 187 / 201, 1536
+  // rows 182 / 163; one expert, 4096 x 4096, 2048 rows 61 / 73, 1024 rows 58 / 36.
+  const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
+  if (a.rows / a.E >= 64 && a.rows / kTile * pieces >= 128) {
+    const int64_t tiles = ((a.rows + kTile - 1) / kTile + (a.offset ? a.E : 0)) * pieces;
+    if (tiles > kMaxTiles) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(matmul_tile_kernel, dim3((unsigned)((tiles + 255) / 256 * 256)),
+                       dim3(kTileThreads), 0, stream, a, pieces, 4);
     return hipGetLastError();
   }
-  return launch_stream<8, 1, 3>(a, out, stream);
+  // Few rows: 128 channels to a workgroup where that gives every compute unit
+  // one (windows that can have rows are counted), else fewer channels and
+  // more of the depth at once.  With at most 16 rows in all a stage needs room
+  // for no more.  4096 x 7168, one expert, us at 128 / 64 / 32 / 16 channels: 1 row 26 /
+  // 16 / 12 / 9, 64 rows 29 / 19 / 14 / -; 32 experts, 512 rows 159 / 158 / 208 / 258.
+  const int64_t windows = (a.rows < a.E ? a.rows : a.E) + a.rows / 64;
+  const auto groups = [&](int tiles) {
+    const int c = tiles * (a.swiglu ? 8 : 16);
+    return windows * ((out + c - 1) / c);
+  };
+  if (groups(8) >= 256) return launch_stream<64, 8, 1, 3>(a, out, stream);
+  if (groups(4) >= 256) return launch_stream<32, 4, 2, 3>(a, out, stream);
+  if (a.rows > 16) return launch_stream<64, 2, 4, 3>(a, out, stream);
+  if (groups(2) >= 256) return launch_stream<16, 2, 4, 3>(a, out, stream);
+  return launch_stream<16, 1, 8, 2>(a, out, stream);
 }
 
 }  // namespace moe

@@ -7,6 +7,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 #include "layer.h"
 
 namespace moe {
