@@ -142,6 +142,7 @@ int moe_rmsnorm(const uint16_t* x, int64_t x_pitch, const void* residual, int re
   a.H = H;
   a.sum_out = static_cast<uint8_t*>(sum_out);
   a.y = reinterpret_cast<uint8_t*>(y);
+  a.stream_y = T * H >= (int64_t)32 << 20;
   a.q = static_cast<uint8_t*>(q);
   a.q_scales = q_scales;
   a.scale_cols = scale_cols;

@@ -65,6 +65,7 @@ struct NormArgs {
   const int32_t* row_src;    // rows with a negative entry are skipped; or null
   uint8_t* sum_out;
   uint8_t* y;
+  int32_t stream_y;          // y is larger than the caches keep
   QuantKind quant;
   uint8_t* q;
   float* q_scales;

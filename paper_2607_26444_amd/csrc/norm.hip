@@ -32,20 +32,22 @@ __device__ __forceinline__ Vec8 from_f32(const u32x4& a, const u32x4& b) {
                __uint_as_float(b.z), __uint_as_float(b.w)}};
 }
 
-// Vector v (8 values) of a row of bf16 or float32.
-__device__ __forceinline__ Vec8 load8(const uint8_t* row, int64_t v, bool f32) {
-  if (f32) return from_f32(ld16(row + v * 32), ld16(row + v * 32 + 16));
-  return unpack8(ld16(row + v * 16));
+template <bool STREAM>
+__device__ __forceinline__ void put16(uint8_t* p, u32x4 v) {
+  if (STREAM) st16_stream(p, v);
+  else st16(p, v);
 }
 
+// Vector v (8 values) of a row of bf16 or float32.
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(uint8_t* row, int64_t v, bool f32, const Vec8& x) {
   if (f32) {
-    st16(row + v * 32, u32x4{__float_as_uint(x.f[0]), __float_as_uint(x.f[1]),
-                             __float_as_uint(x.f[2]), __float_as_uint(x.f[3])});
-    st16(row + v * 32 + 16, u32x4{__float_as_uint(x.f[4]), __float_as_uint(x.f[5]),
-                                  __float_as_uint(x.f[6]), __float_as_uint(x.f[7])});
+    put16<STREAM>(row + v * 32, u32x4{__float_as_uint(x.f[0]), __float_as_uint(x.f[1]),
+                                      __float_as_uint(x.f[2]), __float_as_uint(x.f[3])});
+    put16<STREAM>(row + v * 32 + 16, u32x4{__float_as_uint(x.f[4]), __float_as_uint(x.f[5]),
+                                           __float_as_uint(x.f[6]), __float_as_uint(x.f[7])});
   } else {
-    st16(row + v * 16, pack8(x.f));
+    put16<STREAM>(row + v * 16, pack8(x.f));
   }
 }
 
@@ -113,45 +115,48 @@ __device__ __forceinline__ void row_reduce(float& sum, uint32_t& top, int waves,
   }
 }
 
-// Row r: thread `at` of the row's `threads`.
-template <int NV>
-__device__ __forceinline__ void norm_row(const NormArgs& a, int64_t r, int at, int waves, int wave,
-                                         int lane, float* s_sum, uint32_t* s_top) {
-  const int threads = waves * kWave;
-  const int nv = a.H / 8;
-  const bool has_res = a.residual != nullptr;
-  Vec8 h[NV], w[NV];
-  const uint8_t* x = a.x + r * a.x_pitch;
+// How a row's second input (the residual, the weight) is there.
+enum Form : int { kNone = 0, kBf16 = 1, kF32 = 2 };
+
+// Vectors of a row as they come from memory.
+template <int NV, Form F>
+struct Raw {
+  u32x4 v[NV * (F == kF32 ? 2 : F == kBf16 ? 1 : 0) + (F == kNone)];
+
+  // Vectors at, at + threads, ... of the nv of a row; zeros past the end.
+  __device__ __forceinline__ void load(const uint8_t* row, int at, int threads, int nv, bool stream) {
+    if constexpr (F != kNone) {
+      constexpr int kParts = F == kF32 ? 2 : 1;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int v = at + i * threads;
-    h[i] = v < nv ? load8(x, v, false) : Vec8{};
-  }
-  if (has_res) {
-    const uint8_t* res = a.residual + r * a.residual_pitch;
+      for (int i = 0; i < NV; ++i) {
+        const int64_t n = at + i * threads;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int v = at + i * threads;
-      if (v < nv) {
-        const Vec8 b = load8(res, v, a.residual_f32);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[i].f[j] += b.f[j];
+        for (int p = 0; p < kParts; ++p) {
+          const uint8_t* from = row + (n * kParts + p) * 16;
+          v[i * kParts + p] = n >= nv ? u32x4{0, 0, 0, 0} : stream ? ld16_stream(from) : ld16(from);
+        }
       }
     }
   }
-  if (a.weight) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int v = at + i * threads;
-      w[i] = v < nv ? load8(a.weight, v, a.weight_f32) : Vec8{};
-    }
+  __device__ __forceinline__ Vec8 get(int i) const {
+    if constexpr (F == kF32) return from_f32(v[2 * i], v[2 * i + 1]);
+    else return unpack8(v[i]);
   }
-  if (a.sum_out) {
-    const int64_t row = r * (int64_t)a.H * (a.residual_f32 ? 4 : 2);
+};
+
+// A row's work after its vectors h (x + residual) are in registers.
+template <int NV, Form RES, Form WEIGHT>
+__device__ __forceinline__ void finish_row(const NormArgs& a, int64_t r, int at, int waves, int wave,
+                                           int lane, Vec8 (&h)[NV], const Raw<NV, WEIGHT>& weight,
+                                           float* s_sum, uint32_t* s_top) {
+  const int threads = waves * kWave;
+  const int nv = a.H / 8;
+  if (RES != kNone && a.sum_out) {
+    uint8_t* out = a.sum_out + r * (int64_t)a.H * (RES == kF32 ? 4 : 2);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int v = at + i * threads;
-      if (v < nv) store8(a.sum_out + row, v, a.residual_f32, h[i]);
+      if (v < nv) store8<true>(out, v, RES == kF32, h[i]);
     }
   }
 
@@ -159,16 +164,18 @@ __device__ __forceinline__ void norm_row(const NormArgs& a, int64_t r, int at, i
   uint32_t top = 0u;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
+    Vec8 w;
+    if constexpr (WEIGHT != kNone) w = weight.get(i);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       sum = __builtin_fmaf(h[i].f[j], h[i].f[j], sum);
-      if (a.weight) h[i].f[j] *= w[i].f[j];
+      if (WEIGHT != kNone) h[i].f[j] *= w.f[j];
       top = umax(top, abs_key(h[i].f[j]));
     }
   }
-  if (a.weight || a.quant == kQuantInt8)
+  if (WEIGHT != kNone || a.quant == kQuantInt8)
     row_reduce(sum, top, waves, wave, lane, s_sum, s_top);
-  if (a.weight) {
+  if constexpr (WEIGHT != kNone) {
     rstd = 1.0f / sqrtf(sum / (float)a.H + a.eps);
     if (a.rstd && at == 0) a.rstd[r] = rstd;
 #pragma unroll
@@ -177,12 +184,14 @@ __device__ __forceinline__ void norm_row(const NormArgs& a, int64_t r, int at, i
       for (int j = 0; j < 8; ++j) h[i].f[j] *= rstd;
   }
 
-  if (a.y) {
+  if (WEIGHT != kNone && a.y) {
     uint8_t* y = a.y + r * (int64_t)a.H * 2;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int v = at + i * threads;
-      if (v < nv) store8(y, v, false, h[i]);
+      if (v >= nv) continue;
+      if (a.stream_y) store8<true>(y, v, false, h[i]);
+      else store8(y, v, false, h[i]);
     }
   }
   if (a.quant == kQuantInt8) {
@@ -213,57 +222,127 @@ __device__ __forceinline__ void norm_row(const NormArgs& a, int64_t r, int at, i
   }
 }
 
+template <int NV, Form RES>
+__device__ __forceinline__ void join(const Raw<NV, kBf16>& x, const Raw<NV, RES>& res,
+                                     Vec8 (&h)[NV]) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    h[i] = x.get(i);
+    if constexpr (RES != kNone) {
+      const Vec8 b = res.get(i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[i].f[j] += b.f[j];
+    }
+  }
+}
+
 // waves: wavefronts of a row; 1: each wavefront of the workgroup has its own row.
-template <int NV>
+// The weights stay in registers over a workgroup's rows, and the next row's
+// vectors are asked for before the present one is worked on.
+template <int NV, Form RES, Form WEIGHT>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a, int waves) {
+  __shared__ float s_sum[2][16];
+  __shared__ uint32_t s_top[2][16];
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  const int at = waves == 1 ? lane : (int)threadIdx.x;
+  const int per = waves == 1 ? blockDim.x / kWave : 1;         // rows of a workgroup
+  const int64_t step = (int64_t)gridDim.x * per;
+  const int threads = waves * kWave, nv = a.H / 8;
+  int64_t r = (int64_t)blockIdx.x * per + (waves == 1 ? wave : 0);
+  if (r >= a.rows) return;                                     // whole wavefronts or workgroups
+  Raw<NV, kBf16> x;
+  Raw<NV, RES> res;
+  Raw<NV, WEIGHT> weight;
+  x.load(a.x + r * a.x_pitch, at, threads, nv, true);
+  res.load(a.residual + r * a.residual_pitch, at, threads, nv, true);
+  weight.load(a.weight, at, threads, nv, false);
+  int phase = 0;
+  for (;;) {
+    Vec8 h[NV];
+    join(x, res, h);
+    const int64_t next = r + step;
+    const bool more = next < a.rows;
+    if (more) {
+      x.load(a.x + next * a.x_pitch, at, threads, nv, true);
+      res.load(a.residual + next * a.residual_pitch, at, threads, nv, true);
+    }
+    finish_row<NV, RES, WEIGHT>(a, r, at, waves, wave, lane, h, weight, s_sum[phase], s_top[phase]);
+    if (!more) break;
+    r = next;
+    phase ^= 1;                                  // the other half is free: all have met since
+  }
+}
+
+// Quantisation alone: rows to skip are found before they are read.
+template <int NV>
+__global__ __launch_bounds__(1024) void quantize_kernel(NormArgs a, int waves) {
   __shared__ float s_sum[16];
   __shared__ uint32_t s_top[16];
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int at = waves == 1 ? lane : (int)threadIdx.x;
   const int per = waves == 1 ? blockDim.x / kWave : 1;         // rows of a workgroup
+  const int threads = waves * kWave, nv = a.H / 8;
   for (int64_t r = (int64_t)blockIdx.x * per + (waves == 1 ? wave : 0); r < a.rows;
        r += (int64_t)gridDim.x * per) {
     if (a.row_src && (int32_t)ld4(a.row_src + r) < 0) continue;   // whole wavefronts or workgroups
-    norm_row<NV>(a, r, at, waves, wave, lane, s_sum, s_top);
+    Raw<NV, kBf16> x;
+    Raw<NV, kNone> none;
+    x.load(a.x + r * a.x_pitch, at, threads, nv, true);
+    Vec8 h[NV];
+    join(x, none, h);
+    finish_row<NV, kNone, kNone>(a, r, at, waves, wave, lane, h, none, s_sum, s_top);
     if (waves > 1 && r + (int64_t)gridDim.x < a.rows) __syncthreads();   // s_sum, s_top are free
   }
 }
 
-// Gradients.  A workgroup takes the rows blockIdx.x, + gridDim.x, ...; each
-// thread keeps the weight gradient of its columns in registers and leaves it
-// in the workgroup's row of `partial` at the end.
-template <int NV>
-__global__ __launch_bounds__(1024) void norm_backward_kernel(NormGradArgs a) {
+// Gradients.  A workgroup takes the rows r, r + step, ... (waves = 1: each of
+// its wavefronts) and asks for the next row before it works on the present
+// one; each thread keeps the weight gradient of its columns in registers and
+// the workgroup leaves it in its row of `partial` at the end.
+template <int NV, Form FORM, Form WEIGHT, bool SUM>
+__global__ __launch_bounds__(1024) void norm_backward_kernel(NormGradArgs a, int waves) {
+  constexpr bool F = FORM == kF32, kLate = F && NV == 2;
   __shared__ float s_sum[2][16];
+  __shared__ float s_dw[NV == 2 ? 1024 : 512][kWavesPerBlock];
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
-  const int threads = blockDim.x, waves = threads / kWave;
-  const int nv = a.H / 8;
-  const int hb = a.h_f32 ? 4 : 2;
-  Vec8 w[NV], dw[NV] = {};
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int v = threadIdx.x + i * threads;
-    w[i] = v < nv ? load8(a.weight, v, a.weight_f32) : Vec8{};
-  }
-  int phase = 0;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const uint8_t* dy = a.grad_y + r * (int64_t)a.H * 2;
-    const uint8_t* hr = a.h + r * (int64_t)a.H * hb;
-    const float rstd = __uint_as_float(ld4(a.rstd + r));
+  const int at = waves == 1 ? lane : (int)threadIdx.x;
+  const int per = waves == 1 ? kWavesPerBlock : 1;             // rows of a workgroup
+  const int64_t step = (int64_t)gridDim.x * per;
+  const int threads = waves * kWave, nv = a.H / 8;
+  const int64_t wide = (int64_t)a.H * (F ? 4 : 2);
+  Raw<NV, WEIGHT> weight;
+  Raw<NV, kBf16> dy;
+  Raw<NV, FORM> hv;
+  Raw<NV, SUM ? FORM : kNone> gs;
+  Vec8 dw[NV] = {};
+  weight.load(a.weight, at, threads, nv, false);
+  int64_t r = (int64_t)blockIdx.x * per + (waves == 1 ? wave : 0);
+  float rstd = 0.0f;
+  auto fetch = [&](int64_t n) {
+    dy.load(a.grad_y + n * a.H * 2, at, threads, nv, true);
+    hv.load(a.h + n * wide, at, threads, nv, true);
+    rstd = __uint_as_float(ld4(a.rstd + n));
+  };
+  if (r < a.rows) fetch(r);
+  for (int phase = 0; r < a.rows; r += step, phase ^= 1) {
     Vec8 u[NV], h[NV];
+    const float rs = rstd;
     float dot = 0.0f;
+    // needed last; float32 rows lack the registers to have it early
+    if (!kLate) gs.load(a.grad_sum + r * wide, at, threads, nv, true);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int v = threadIdx.x + i * threads;
-      u[i] = v < nv ? load8(dy, v, false) : Vec8{};
-      h[i] = v < nv ? load8(hr, v, a.h_f32) : Vec8{};
+      u[i] = dy.get(i);
+      h[i] = hv.get(i);
     }
+    if (!kLate && r + step < a.rows) fetch(r + step);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      const Vec8 w = weight.get(i);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        dw[i].f[j] = __builtin_fmaf(u[i].f[j] * h[i].f[j], rstd, dw[i].f[j]);
-        u[i].f[j] *= w[i].f[j];
+        dw[i].f[j] = __builtin_fmaf(u[i].f[j] * h[i].f[j], rs, dw[i].f[j]);
+        u[i].f[j] *= w.f[j];
         dot = __builtin_fmaf(u[i].f[j], h[i].f[j], dot);
       }
     }
@@ -273,44 +352,86 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormGradArgs a) {
       __syncthreads();                           // the other half is free again by now
       dot = 0.0f;
       for (int k = 0; k < waves; ++k) dot += s_sum[phase][k];
-      phase ^= 1;
     }
-    const float c = dot / (float)a.H * rstd * rstd;
-    uint8_t* dx = a.grad_x + r * (int64_t)a.H * hb;
+    if (kLate) gs.load(a.grad_sum + r * wide, at, threads, nv, true);
+    const float c = dot / (float)a.H * rs * rs;
+    uint8_t* dx = a.grad_x + r * wide;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int v = threadIdx.x + i * threads;
+      const int v = at + i * threads;
       if (v >= nv) continue;
-      Vec8 g = a.grad_sum ? load8(a.grad_sum + r * (int64_t)a.H * hb, v, a.h_f32) : Vec8{};
+      Vec8 g = {};
+      if constexpr (SUM) g = gs.get(i);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        g.f[j] = __builtin_fmaf(rstd, u[i].f[j] - h[i].f[j] * c, g.f[j]);
-      store8(dx, v, a.h_f32, g);
+        g.f[j] = __builtin_fmaf(rs, u[i].f[j] - h[i].f[j] * c, g.f[j]);
+      store8<true>(dx, v, F, g);
     }
+    if (kLate && r + step < a.rows) fetch(r + step);
   }
   if (!a.grad_weight) return;
   uint8_t* part = reinterpret_cast<uint8_t*>(a.partial + (int64_t)blockIdx.x * a.H);
+  if (waves > 1) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int v = threadIdx.x + i * threads;
-    if (v < nv) store8(part, v, true, dw[i]);
+    for (int i = 0; i < NV; ++i) {
+      const int v = at + i * threads;
+      if (v < nv) store8(part, v, true, dw[i]);
+    }
+    return;
   }
+  // the four wavefronts' columns meet in LDS
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int c = (at + i * kWave) * 8 + j;
+      if (c < a.H) s_dw[c][wave] = dw[i].f[j];
+    }
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.H; c += kBlock)
+    reinterpret_cast<float*>(part)[c] = ((s_dw[c][0] + s_dw[c][1]) + s_dw[c][2]) + s_dw[c][3];
 }
 
-// Column sums of partial [parts][H]: 16 columns to a workgroup, 16 threads of
-// a column add every 16th row, their sums meet in LDS.
-__global__ __launch_bounds__(kBlock) void norm_weight_kernel(const float* partial, int parts, int H,
-                                                             float* out) {
-  __shared__ float s[16][17];
-  const int col = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x / 16;
-  float sum = 0.0f;
-  if (col < H)
-    for (int p = row; p < parts; p += 16) sum += partial[(int64_t)p * H + col];
-  s[row][threadIdx.x & 15] = sum;
+// Column sums of partial [parts][H]: 32 columns (a line) to a workgroup, 128
+// rows at a time, the 128 sums of a column added in LDS.  A fixed order.
+__global__ __launch_bounds__(1024) void norm_weight_kernel(const float* partial, int parts, int H,
+                                                           float* out) {
+  __shared__ float s[128][33];
+  const int quad = threadIdx.x & 7, row = threadIdx.x / 8;
+  const int col = blockIdx.x * 32 + quad * 4;            // H % 8 == 0: whole fours
+  float sum[4] = {};
+  if (col < H) {
+    for (int n0 = row; n0 < parts; n0 += 1024) {         // eight rows asked for together
+      u32x4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int n = n0 + i * 128;
+        v[i] = n < parts ? ld16(partial + (int64_t)n * H + col) : u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sum[0] += __uint_as_float(v[i].x);
+        sum[1] += __uint_as_float(v[i].y);
+        sum[2] += __uint_as_float(v[i].z);
+        sum[3] += __uint_as_float(v[i].w);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s[row][quad * 4 + j] = sum[j];
   __syncthreads();
-  if (row == 0 && col < H) {
-    for (int p = 1; p < 16; ++p) sum += s[p][threadIdx.x];
-    out[col] = sum;
+  const int c = threadIdx.x & 31, part = threadIdx.x / 32;   // 32 parts of four rows
+  float t = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t += s[part * 4 + j][c];
+  __syncthreads();
+  s[part][c] = t;
+  __syncthreads();
+  if (part == 0 && blockIdx.x * 32 + c < H) {
+    t = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) t += s[j][c];
+    out[blockIdx.x * 32 + c] = t;
   }
 }
 
@@ -331,40 +452,84 @@ hipError_t by_vectors(int nv, F&& launch) {
                  : launch(std::integral_constant<int, 2>());
 }
 
+template <typename F>
+hipError_t by_type(bool f32, F&& launch) {
+  return f32 ? launch(std::integral_constant<Form, kF32>())
+             : launch(std::integral_constant<Form, kBf16>());
+}
+
+// Workgroups of a persistent row kernel: 16 wavefronts to a compute unit.  More, with the fewer
+// registers that allows, read no faster (16384 rows of 7168 to fp8, us at 16 / 21 / 28
+// wavefronts: 160 / 161 / 198).
+int64_t row_groups(int64_t want, int threads) {
+  const int groups = 16 / (threads / kWave);
+  const int64_t resident = 256 * (int64_t)(groups > 1 ? groups : 1);
+  return want < resident ? want : resident;
+}
+
 }  // namespace
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
   const RowShape s = row_shape(a.H);
-  const int64_t want = s.waves == 1 ? (a.rows + kWavesPerBlock - 1) / kWavesPerBlock : a.rows;
-  const int64_t blocks = want < kMaxGrid ? want : kMaxGrid;
   const int threads = s.waves == 1 ? kBlock : s.waves * kWave;
+  const int64_t want = s.waves == 1 ? (a.rows + kWavesPerBlock - 1) / kWavesPerBlock : a.rows;
+  if (!a.weight) {
+    const int64_t blocks = want < kMaxGrid ? want : kMaxGrid;
+    return by_vectors(s.nv, [&](auto nv) {
+      hipLaunchKernelGGL((quantize_kernel<nv.value>), dim3((unsigned)blocks), dim3(threads), 0,
+                         stream, a, s.waves);
+      return hipGetLastError();
+    });
+  }
+  const int64_t blocks = row_groups(want, threads);
   return by_vectors(s.nv, [&](auto nv) {
-    hipLaunchKernelGGL((norm_kernel<nv.value>), dim3((unsigned)blocks), dim3(threads), 0, stream,
-                       a, s.waves);
-    return hipGetLastError();
+    return by_type(a.weight_f32, [&](auto weight) {
+      const auto run = [&](auto res) {
+        hipLaunchKernelGGL((norm_kernel<nv.value, res.value, weight.value>), dim3((unsigned)blocks),
+                           dim3(threads), 0, stream, a, s.waves);
+        return hipGetLastError();
+      };
+      return a.residual ? by_type(a.residual_f32, run)
+                        : run(std::integral_constant<Form, kNone>());
+    });
   });
 }
 
+// One row of a few thousand columns to a workgroup of the row pass would leave
+// as many partial rows to add: from three rows for each compute unit on, a workgroup takes three (us,
+// one / three rows: 1500 x 4096 17.0 / 14.5, 777 x 2056 float32 12.5 / 10.5, 256 x
+// 4096 8.1 / 9.3).
 int norm_grad_parts(int64_t rows, int H) {
   const RowShape s = row_shape(H);
-  const int64_t most = 256 * 16 / s.waves;      // 16 wavefronts resident on each compute unit
-  return (int)(rows < most ? rows : most);
+  const int threads = s.waves == 1 ? kBlock : s.waves * kWave;
+  const int64_t groups = s.waves == 1 ? (rows + kWavesPerBlock - 1) / kWavesPerBlock : rows;
+  const int64_t want = groups <= 256 ? groups : groups <= 768 ? 256 : groups / 3;
+  return (int)row_groups(want, threads);
 }
 
 hipError_t launch_norm_backward(const NormGradArgs& a, hipStream_t stream) {
   const RowShape s = row_shape(a.H);
+  const int threads = s.waves == 1 ? kBlock : s.waves * kWave;
   const int parts = norm_grad_parts(a.rows, a.H);
   if (parts > 0) {
     const hipError_t err = by_vectors(s.nv, [&](auto nv) {
-      hipLaunchKernelGGL((norm_backward_kernel<nv.value>), dim3((unsigned)parts),
-                         dim3(s.waves * kWave), 0, stream, a);
-      return hipGetLastError();
+      return by_type(a.h_f32, [&](auto form) {
+        return by_type(a.weight_f32, [&](auto weight) {
+          if (a.grad_sum)
+            hipLaunchKernelGGL((norm_backward_kernel<nv.value, form.value, weight.value, true>),
+                               dim3((unsigned)parts), dim3(threads), 0, stream, a, s.waves);
+          else
+            hipLaunchKernelGGL((norm_backward_kernel<nv.value, form.value, weight.value, false>),
+                               dim3((unsigned)parts), dim3(threads), 0, stream, a, s.waves);
+          return hipGetLastError();
+        });
+      });
     });
     if (err != hipSuccess) return err;
   }
   if (a.grad_weight)
-    hipLaunchKernelGGL(norm_weight_kernel, dim3((unsigned)((a.H + 15) / 16)), dim3(kBlock), 0,
-                       stream, a.partial, parts, a.H, a.grad_weight);
+    hipLaunchKernelGGL(norm_weight_kernel, dim3((unsigned)((a.H + 31) / 32)), dim3(1024), 0, stream,
+                       a.partial, parts, a.H, a.grad_weight);
   return hipGetLastError();
 }
 
