@@ -32,41 +32,25 @@ __device__ __forceinline__ int scan_add(int x) {
   return x;
 }
 
-// Tile `id` of the order expert, group of `group` row tiles, channel piece, row
-// tile in the group, so that neighbouring tiles share rows or weights.  A row
-// tile has `size` rows, a window `pieces` channel pieces.
-__device__ __forceinline__ Tile find_tile(const MatmulArgs& a, int id, int size, int pieces,
-                                          int group) {
-  int expert = 0, start = 0, n = (int)a.rows, before = 0;
-  if (a.offset) {
-    const int lane = threadIdx.x & (kWave - 1), rows = (int)a.rows;
-    const int first = uniform((int)ld4(a.offset));
-    n = 0;
-    for (int e0 = 0; e0 < a.E; e0 += kWave) {
-      const int e = e0 + lane < a.E ? e0 + lane : a.E - 1;
-      const int o = (int)ld4(a.offset + e);
-      const int64_t s64 = (int64_t)o - first;
-      int64_t m64 = a.count ? (int64_t)(int)ld4(a.count + e)
-                            : (int64_t)(int)ld4(a.offset + e + 1) - o;
-      const bool in = e0 + lane < a.E && s64 >= 0 && s64 <= rows && m64 > 0;
-      const int s = in ? (int)s64 : 0;
-      const int m = in ? (int)(m64 < rows - s64 ? m64 : rows - s64) : 0;
-      const int tiles = (m + size - 1) / size;
-      const int sum = before + scan_add(tiles);        // inclusive over the lanes
-      const uint64_t hit = __ballot((int64_t)sum * pieces > id);
-      if (hit) {
-        const int l = __builtin_ctzll(hit);
-        expert = e0 + l;
-        before = __builtin_amdgcn_readlane(sum - tiles, l);
-        start = __builtin_amdgcn_readlane(s, l);
-        n = __builtin_amdgcn_readlane(m, l);
-        break;
-      }
-      before = __builtin_amdgcn_readlane(sum, kWave - 1);
-    }
-  }
+// Expert e's window: first row and rows, clipped to the rows there are.
+__device__ __forceinline__ void window_of(const MatmulArgs& a, int e, int first, int& start,
+                                          int& rows) {
+  const int all = (int)a.rows;
+  const int o = (int)ld4(a.offset + e);
+  const int64_t s = (int64_t)o - first;
+  const int64_t m =
+      a.count ? (int64_t)(int)ld4(a.count + e) : (int64_t)(int)ld4(a.offset + e + 1) - o;
+  const bool in = s >= 0 && s <= all && m > 0;
+  start = in ? (int)s : 0;
+  rows = in ? (int)(m < all - s ? m : all - s) : 0;
+}
+
+// Tile `at` of a window of n rows from `start`: `group` row tiles of `size`
+// rows together, all channel pieces of a group before the next, so that
+// neighbouring tiles share rows or weights.
+__device__ __forceinline__ Tile tile_of(int expert, int start, int n, int at, int size, int pieces,
+                                        int group) {
   const int tiles = (n + size - 1) / size;
-  const int at = id - before * pieces;
   if (at >= tiles * pieces) return {0, 0, 0, 0};
   const int per = group * pieces;
   const int g = at / per, in = at % per;
@@ -74,6 +58,29 @@ __device__ __forceinline__ Tile find_tile(const MatmulArgs& a, int id, int size,
   const int tile = g * group + in % here;
   const int left = n - tile * size;
   return {expert, (int64_t)start + (int64_t)tile * size, left < size ? left : size, in / here};
+}
+
+// Tile `id`, windows in the order of the experts.
+__device__ __forceinline__ Tile find_tile(const MatmulArgs& a, int id, int size, int pieces) {
+  if (!a.offset) return tile_of(0, 0, (int)a.rows, id, size, pieces, 1);
+  const int lane = threadIdx.x & (kWave - 1);
+  const int first = uniform((int)ld4(a.offset));
+  int before = 0;
+  for (int e0 = 0; e0 < a.E; e0 += kWave) {
+    int s, m;
+    window_of(a, e0 + lane < a.E ? e0 + lane : a.E - 1, first, s, m);
+    if (e0 + lane >= a.E) m = 0;
+    const int tiles = (m + size - 1) / size;
+    const int sum = before + scan_add(tiles);          // inclusive over the lanes
+    const uint64_t hit = __ballot((int64_t)sum * pieces > id);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      return tile_of(e0 + l, __builtin_amdgcn_readlane(s, l), __builtin_amdgcn_readlane(m, l),
+                     id - __builtin_amdgcn_readlane(sum - tiles, l) * pieces, size, pieces, 1);
+    }
+    before = __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  return {0, 0, 0, 0};
 }
 
 // g / (1 + exp(-g)) by the hardware's exponential and reciprocal (1 ulp each;
@@ -144,63 +151,86 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-// One tile whose wavefronts take MT x 16 rows each: 8 for a full tile, 4 or 2
-// for the last rows of a window (as long as reading the weights, but half or
-// a quarter of the products).
-template <int MT>
-__device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t,
-                                              uint8_t* s_tile) {
-  constexpr int NT = 4;
-  constexpr int kLoads = MT / 2 + 4;                   // of a wavefront and stage
-  float* s_scale = reinterpret_cast<float*>(s_tile + 2 * kStageBytes);
-  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
-  const int half = a.N / 2;
-  const int c0 = t.piece * (a.swiglu ? kTile / 2 : kTile);
+// Channel (of the tile's) that an LDS row of weights holds.  A lane's sums of a
+// wavefront's four 16-channel tiles are 16 neighbouring channels this way (with
+// swiglu tiles 1 and 3 are the up channels of 0 and 2, and a lane has 8), so that
+// its outputs are whole vectors and a row's are whole lines.
+__device__ __forceinline__ int channel_of(int r, bool swiglu) {
+  const int block = r / 64, tile = r / 16 & 3, d = r & 15;
+  return swiglu ? block * 32 + d / 4 * 8 + tile / 2 * 4 + (d & 3)
+                : block * 64 + d / 4 * 16 + tile * 4 + (d & 3);
+}
 
-  // instruction j of a wavefront fills LDS rows (j * 8 + wave) * 8 + lane / 8
-  const int lr = lane / 8, chunk = (lane & 7) ^ lr;
-  uint32_t ao[MT / 2], wo[4];
-  const bool up = a.swiglu && (wave & 2);              // rows 16..31 of 32: up channels
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int r = (j * 8 + wave) * 8 + lr;
-    if (j < MT / 2) ao[j] = (uint32_t)r * (uint32_t)a.K + chunk * 16;
-    const int c = a.swiglu ? r / 32 * 16 + (r & 15) : r;
-    wo[j] = (uint32_t)c * (uint32_t)a.K + chunk * 16;
+// What a wavefront loads of a tile.
+struct TileLoads {
+  Rsrc ra, rw;
+  uint32_t ao, wo;             // of instruction 0
+  int a_step, w_step;          // from one instruction to the next
+  int K, chunk, wave;
+  uint8_t* s_tile;
+
+  __device__ __forceinline__ TileLoads(const MatmulArgs& a, const Tile& t, int tid, uint8_t* lds)
+      : K(a.K), s_tile(lds) {
+    const int lane = tid & (kWave - 1);
+    wave = uniform(tid / kWave);
+    // instruction j of a wavefront fills LDS rows (j * 8 + wave) * 8 + lane / 8
+    const int lr = lane / 8, half = a.N / 2, c0 = t.piece * (a.swiglu ? kTile / 2 : kTile);
+    chunk = (lane & 7) ^ lr;
+    const int r = wave * 8 + lr;
+    ao = (uint32_t)r * (uint32_t)K + chunk * 16;
+    wo = (uint32_t)channel_of(r, a.swiglu) * (uint32_t)K + chunk * 16;
+    a_step = 64 * K;
+    w_step = (a.swiglu ? 32 : 64) * K;
+    const int channels = (a.swiglu ? half : a.N) - c0, most = a.swiglu ? kTile / 2 : kTile;
+    const bool up = a.swiglu && (wave & 2);            // this wavefront's rows are of odd tiles
+    ra = buffer_of(a.a + t.row * K, t.rows * K);
+    rw = buffer_of(a.w + ((int64_t)t.expert * a.N + c0 + (up ? half : 0)) * K,
+                   (channels < most ? channels : most) * K);
   }
-  const int channels = (a.swiglu ? half : a.N) - c0;   // at least 1
-  const int most = a.swiglu ? kTile / 2 : kTile;
-  const uint8_t* abase = a.a + t.row * a.K;
-  const uint8_t* wbase = a.w + ((int64_t)t.expert * a.N + c0 + (up ? half : 0)) * a.K;
-  const int arange = t.rows * a.K, wrange = (channels < most ? channels : most) * a.K;
-  const Rsrc ra = buffer_of(abase, arange), rw = buffer_of(wbase, wrange);
-  // past the depth and past the tile's rows and channels: zeros
-  auto load = [&](int k0, uint32_t buf) {
-    const bool in = k0 + chunk * 16 < a.K;
+
+  // A stage into LDS; past the depth and past the tile's rows and channels:
+  // zeros.  ROW_LOADS: as many 64 rows as the tile multiplies.
+  template <int ROW_LOADS>
+  __device__ __forceinline__ void stage(int k0, uint32_t buf) const {
+    const bool in = k0 + chunk * 16 < K;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (j < MT / 2)
-        load_to_lds(ra, in ? ao[j] + k0 : kOutside,
+      if (j < ROW_LOADS)
+        load_to_lds(ra, in ? ao + (k0 + j * a_step) : kOutside,
                     (lds_u8*)(s_tile + buf + (j * 8 + wave) * 1024));
-      load_to_lds(rw, in ? wo[j] + k0 : kOutside,
+      load_to_lds(rw, in ? wo + (k0 + j * w_step) : kOutside,
                   (lds_u8*)(s_tile + buf + kTileBytes + (j * 8 + wave) * 1024));
     }
-  };
-  // scales of the tile's rows and channels (LDS order), for the end
-  float scale = 0.0f;
-  {
-    const int n = threadIdx.x & 255;
-    if (threadIdx.x < 256) {
-      if (n < t.rows) scale = a.a_scales[(t.row + n) * a.a_scale_pitch];
-    } else {
-      const int c = a.swiglu ? n / 32 * 16 + (n & 15) : n;
-      if (c < channels)
-        scale = a.w_scales[(int64_t)t.expert * a.N + c0 + c + (a.swiglu && (n & 16) ? half : 0)];
-    }
   }
-  load(0, 0);
-  load(kDepth, kStageBytes);
-  s_scale[threadIdx.x] = scale;
+};
+
+// A thread's scale of the tile: a row's, or a channel's in the order of LDS.
+__device__ __forceinline__ float tile_scale(const MatmulArgs& a, const Tile& t, int tid) {
+  const int n = tid & 255;
+  if (tid < 256) return n < t.rows ? a.a_scales[(t.row + n) * a.a_scale_pitch] : 0.0f;
+  const int out = a.swiglu ? a.N / 2 : a.N;
+  const int c = t.piece * (a.swiglu ? kTile / 2 : kTile) + channel_of(n, a.swiglu);
+  const bool up = a.swiglu && (n & 16);
+  return c < out ? a.w_scales[(int64_t)t.expert * a.N + c + (up ? out : 0)] : 0.0f;
+}
+
+// LDS of the tile kernel: two stages of rows and weights, the scales of this tile and
+// the next, and the windows.
+constexpr int kScaleAt = 2 * kStageBytes, kWindowAt = kScaleAt + 2 * 2 * kTile * 4;
+constexpr int kTileLds = kWindowAt + 3 * MOE_MAX_EXPERTS * 4;
+
+// One tile whose wavefronts take MT x 16 rows each: 8 for a full tile, 4 or 2
+// for the last rows of a window (as long as reading the weights, but half or
+// a quarter of the products).  Its first two stages have been asked for; those
+// of `next` are before its own outputs are computed and stored.
+template <int MT>
+__device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t, const Tile& next,
+                                              int tid, uint8_t* s_tile, int slot, float& scale) {
+  constexpr int NT = 4;
+  float* s_scale = reinterpret_cast<float*>(s_tile + kScaleAt) + slot * 2 * kTile;
+  const int lane = tid & (kWave - 1), wave = uniform(tid / kWave);
+  const TileLoads loads(a, t, tid, s_tile);
+  s_scale[tid] = scale;
 
   const int wm = wave / 4, wn = wave % 4;              // 2 x 4 wavefronts
   const int row = lane & 15, quarter = lane / 16;
@@ -230,7 +260,7 @@ __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t
   // then each has read the last of stage s into registers, and its loads of
   // stage s + 1, asked for a turn ago, have arrived.  Half of the matrix
   // instructions of a register set stand on either side of the barrier.
-  meet<kLoads>();                                      // the first stage is there
+  meet<0>();                                           // the first two stages are there
   uint32_t buf = 0;
   read(0, 0);
   for (int k0 = 0; k0 < a.K; k0 += kDepth) {
@@ -238,7 +268,7 @@ __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t
     multiply(0, 0, MT / 2);
     interleave<kIssueLdsRead, MT + NT, 1>();
     meet<0>();
-    load(k0 + 2 * kDepth, buf);
+    loads.stage<MT / 2>(k0 + 2 * kDepth, buf);
     multiply(0, MT / 2, MT);
     buf ^= kStageBytes;
     __builtin_amdgcn_sched_barrier(0);
@@ -251,9 +281,17 @@ __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t
   }
   meet<0>();                                           // loads past the end have landed
 
-  // a lane's four sums of a tile: channels quarter * 4 .. + 3 of row `row`
+  if (next.rows) {
+    scale = tile_scale(a, next, tid);
+    const TileLoads first(a, next, tid, s_tile);
+    first.stage<4>(0, 0);
+    first.stage<4>(kDepth, kStageBytes);
+  }
+
   typedef float f32x4 __attribute__((ext_vector_type(4)));
-  const int out = a.swiglu ? half : a.N;
+  const int out = a.swiglu ? a.N / 2 : a.N;
+  const int c0 = t.piece * (a.swiglu ? kTile / 2 : kTile) +
+                 (a.swiglu ? wn * 32 + quarter * 8 : wn * 64 + quarter * 16);
   f32x4 sw[NT];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -264,34 +302,89 @@ __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t
     if (r >= t.rows) continue;
     const float sa = s_scale[r];
     uint16_t* y = a.y + (t.row + r) * out;
+    float v[8];
+    if (a.swiglu) {
+      if (c0 >= out) continue;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      if (a.swiglu && (j & 1)) continue;
-      const int c = c0 + (a.swiglu ? wn * 32 + j * 8 : wn * 64 + j * 16) + quarter * 4;
-      if (c >= out) continue;
-      float v[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v[q] = (float)acc[i][j][q] * (sa * sw[j][q]);
-        if (a.swiglu) v[q] = silu(v[q]) * ((float)acc[i][j | 1][q] * (sa * sw[j | 1][q]));
+      for (int q = 0; q < 8; ++q) {
+        const int j = q / 4 * 2;
+        v[q] = silu((float)acc[i][j][q & 3] * (sa * sw[j][q & 3])) *
+               ((float)acc[i][j + 1][q & 3] * (sa * sw[j + 1][q & 3]));
       }
-      st4x2(y + c, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      st16(y + c0, pack8(v));
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (c0 + h * 8 >= out) continue;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int j = h * 2 + q / 4;
+          v[q] = (float)acc[i][j][q & 3] * (sa * sw[j][q & 3]);
+        }
+        st16(y + c0 + h * 8, pack8(v));
+      }
     }
   }
 }
 
+// A workgroup to each compute unit takes the tiles blockIdx.x, + 256, ... of
+// an order in which the 32 tiles that an XCD's compute units hold together are
+// neighbours.
 __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
-  // two stages of rows and weights, then the scales of rows and channels
-  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2 * kStageBytes + 2 * kTile * 4];
-  // the 32 tiles that an XCD's compute units hold together are neighbours
-  const int b = blockIdx.x;
-  const int id = b / 256 * 256 + b % 8 * 32 + b / 8 % 32;
-  const Tile t = find_tile(a, id, kTile, pieces, group);
-  if (t.rows == 0) return;
-  if (t.rows > 128) multiply_tile<8>(a, t, s_tile);
-  else if (t.rows > 64) multiply_tile<4>(a, t, s_tile);
-  else multiply_tile<2>(a, t, s_tile);
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[kTileLds];
+  int* s_end = reinterpret_cast<int*>(s_tile + kWindowAt);   // row tiles up to and with a window
+  int* s_start = s_end + MOE_MAX_EXPERTS;
+  int* s_rows = s_start + MOE_MAX_EXPERTS;
+  const int lane = threadIdx.x & (kWave - 1);
+  if (threadIdx.x < kWave) {
+    const int first = a.offset ? uniform((int)ld4(a.offset)) : 0;
+    int before = 0;
+    for (int e0 = 0; e0 < a.E; e0 += kWave) {
+      int s = 0, m = (int)a.rows;
+      if (a.offset) window_of(a, e0 + lane < a.E ? e0 + lane : a.E - 1, first, s, m);
+      if (e0 + lane >= a.E) m = 0;
+      const int end = before + scan_add((m + kTile - 1) / kTile);
+      s_end[e0 + lane] = end;                          // E is at most 16 times 64
+      s_start[e0 + lane] = s;
+      s_rows[e0 + lane] = m;
+      before = __builtin_amdgcn_readlane(end, kWave - 1);
+    }
+  }
+  __syncthreads();
+  auto tile_at = [&](int n) -> Tile {
+    const int id = n * 256 + (blockIdx.x & 7) * 32 + blockIdx.x / 8;
+    for (int e0 = 0; e0 < a.E; e0 += kWave) {
+      const uint64_t hit = __ballot((int64_t)s_end[e0 + lane] * pieces > id);
+      if (!hit) continue;
+      const int e = e0 + __builtin_ctzll(hit);
+      const int before = e ? uniform(s_end[e - 1]) : 0;
+      return tile_of(e, uniform(s_start[e]), uniform(s_rows[e]), id - before * pieces, kTile, pieces,
+                     group);
+    }
+    return {0, 0, 0, 0};
+  };
+
+  Tile t = tile_at(0);
+  if (t.rows == 0) return;                             // the whole workgroup
+  int tid = threadIdx.x;
+  float scale = tile_scale(a, t, tid);
+  {
+    const TileLoads first(a, t, tid, s_tile);
+    first.stage<4>(0, 0);
+    first.stage<4>(kDepth, kStageBytes);
+  }
+  for (int n = 1;; ++n) {
+    const Tile next = tile_at(n);
+    // what follows from the thread's number is worked out anew for each tile:
+    // kept over the loop it would not fit the registers
+    asm volatile("" : "+v"(tid));
+    if (t.rows > 128) multiply_tile<8>(a, t, next, tid, s_tile, n & 1, scale);
+    else if (t.rows > 64) multiply_tile<4>(a, t, next, tid, s_tile, n & 1, scale);
+    else multiply_tile<2>(a, t, next, tid, s_tile, n & 1, scale);
+    if (next.rows == 0) return;
+    t = next;
+  }
 }
 
 // Few rows: ROWS rows of a window x 16 WC channels, bound by reading the
@@ -317,7 +410,7 @@ void matmul_stream_kernel(MatmulArgs a, int pieces) {
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   // 32 neighbouring tiles (mostly one window's, which share rows) to an XCD
   const int b = blockIdx.x;
-  const Tile t = find_tile(a, b / 256 * 256 + b % 8 * 32 + b / 8 % 32, ROWS, pieces, 1);
+  const Tile t = find_tile(a, b / 256 * 256 + b % 8 * 32 + b / 8 % 32, ROWS, pieces);
   if (t.rows == 0) return;                             // the whole workgroup
   const int half = a.N / 2, out = a.swiglu ? half : a.N;
   const int wc = wave % WC, wk = wave / WC;
@@ -441,9 +534,8 @@ hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
   const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
   if (a.rows / a.E >= 64 && a.rows / kTile * pieces >= 128) {
     const int64_t tiles = ((a.rows + kTile - 1) / kTile + (a.offset ? a.E : 0)) * pieces;
-    if (tiles > kMaxTiles) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(matmul_tile_kernel, dim3((unsigned)((tiles + 255) / 256 * 256)),
-                       dim3(kTileThreads), 0, stream, a, pieces, 4);
+    if (tiles > INT32_MAX - 256) return hipErrorInvalidConfiguration;   // tile numbers are int
+    hipLaunchKernelGGL(matmul_tile_kernel, dim3(256), dim3(kTileThreads), 0, stream, a, pieces, 4);
     return hipGetLastError();
   }
   // Few rows: 128 channels to a workgroup where that gives every compute unit
