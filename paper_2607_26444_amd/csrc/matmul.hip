@@ -52,6 +52,10 @@ __device__ __forceinline__ Tile tile_of(int expert, int start, int n, int at, in
                                         int group) {
   const int tiles = (n + size - 1) / size;
   if (at >= tiles * pieces) return {0, 0, 0, 0};
+  if (group > 1) {                                     // groups as even as they can be
+    const int groups = (tiles + group - 1) / group;
+    group = (tiles + groups - 1) / groups;
+  }
   const int per = group * pieces;
   const int g = at / per, in = at % per;
   const int here = tiles - g * group < group ? tiles - g * group : group;   // tiles of this group
@@ -535,7 +539,9 @@ hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
   if (a.rows / a.E >= 64 && a.rows / kTile * pieces >= 128) {
     const int64_t tiles = ((a.rows + kTile - 1) / kTile + (a.offset ? a.E : 0)) * pieces;
     if (tiles > INT32_MAX - 256) return hipErrorInvalidConfiguration;   // tile numbers are int
-    hipLaunchKernelGGL(matmul_tile_kernel, dim3(256), dim3(kTileThreads), 0, stream, a, pieces, 4);
+    // six row tiles together: of 2, 4, 5, 6 and 8 the best or near it (32768 x 2048 x 7168
+    // over 32 experts 528 / 522 / 512 / 510 / 509 us, 16384 x 8192 x 8192 846 / 832 / 815 / 811 / 835)
+    hipLaunchKernelGGL(matmul_tile_kernel, dim3(256), dim3(kTileThreads), 0, stream, a, pieces, 6);
     return hipGetLastError();
   }
   // Few rows: 128 channels to a workgroup where that gives every compute unit
