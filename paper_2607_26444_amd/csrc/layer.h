@@ -113,7 +113,7 @@ struct MatmulArgs {
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------- device
-// Value of the lane n further on in the row of 16 (rotation).
+// Value of the lane N before, around the row of 16.
 template <int N>
 __device__ __forceinline__ uint32_t row_rotate(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xf, 0xf, true);

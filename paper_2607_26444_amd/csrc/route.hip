@@ -89,7 +89,17 @@ __device__ __forceinline__ float exp_term(float x, float m) {
   return x == m ? 1.0f : expf(x - m);
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+
+// 1 / x for x >= 1 as an exact division rounds it: one Newton step on the
+// hardware's reciprocal (1 ulp) is the correctly rounded one for every
+// significand; a quarter of a division's instructions.  Infinity gives 0.
+__device__ __forceinline__ float reciprocal(float x) {
+  const float r = __builtin_amdgcn_rcpf(x);
+  const float y = __builtin_fmaf(__builtin_fmaf(-x, r, 1.0f), r, r);
+  return x < 0x1p126f ? y : 1.0f / x;              // beyond: the result is subnormal
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return reciprocal(1.0f + expf(-x)); }
 
 // Largest of the lanes' values; -inf where there is none.  NaN is passed over.
 template <int LANES, int VPL>
@@ -128,92 +138,102 @@ __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Route token t: lane `sub` of its LANES, `tok` its place in the wavefront, `mine`
-// the token's keys in LDS.  Every lane of the wavefront takes part.
-template <int LANES, int VPL>
-__device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t t, int sub, int tok,
-                                            float* mine) {
-#pragma clang fp contract(off)
-  const bool in = t < a.tokens;
-  const bool live = in && (!a.token_mask || a.token_mask[t]);
-  const int e0 = sub * VPL;
-  float x[VPL];
-  if (live) {
-    load_logits<VPL>(a.logits, a.f32, t * a.pitch, e0, a.E, vec, x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
+// The two highest of a group's keys, over the lanes that share it.
+struct TopTwo {
+  float best, second;
+  __device__ __forceinline__ void add(float b, float s) {
+    second = fmaxf(fminf(best, b), fmaxf(second, s));
+    best = fmaxf(best, b);
   }
+  template <int CTRL>
+  __device__ __forceinline__ void from_lane() {       // DPP exchange between lanes
+    const int b = __float_as_int(best), s = __float_as_int(second);
+    add(__int_as_float(__builtin_amdgcn_update_dpp(b, b, CTRL, 0xf, 0xf, false)),
+        __int_as_float(__builtin_amdgcn_update_dpp(s, s, CTRL, 0xf, 0xf, false)));
+  }
+};
 
-  // scores, where they order the experts or weigh them as they are
-  const bool by_score = a.bias || (a.groups > 1 && a.group_top > 1);
-  float m = 0.0f, total = 1.0f;
-  const bool plain = !a.sigmoid && !a.renorm;
-  float s[VPL];
-  if (by_score || plain) {
-    if (a.sigmoid) {
+__device__ __forceinline__ float group_key(const TopTwo& g, int group_top) {
+  return group_top > 1 && g.second > -INFINITY ? g.best + g.second : g.best;
+}
+
+// Groups of whole lanes, a power of two of them, that fill the token's 16 lanes
+// (256 experts in 8 groups: two lanes each): keys of the groups that do not
+// take part become -inf, by exchanges between lanes.
+template <int VPL>
+__device__ __forceinline__ void keep_lane_groups(const RouteArgs& a, int sub, float (&kf)[VPL]) {
+  const int lanes = 16 / a.groups;
+  TopTwo g = {-INFINITY, -INFINITY};
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) s[i] = sigmoid(x[i]);
-    } else {
-      m = row_max<LANES, VPL>(x);
+  for (int i = 0; i < VPL; ++i) g.add(kf[i], -INFINITY);
+  if (lanes > 1) g.from_lane<0xB1>();               // lane ^ 1
+  if (lanes > 2) g.from_lane<0x4E>();               // lane ^ 2
+  if (lanes > 4) g.from_lane<0x141>();              // the other four of eight
+  if (lanes > 8) g.from_lane<0x140>();              // the other eight
+  const float key = group_key(g, a.group_top);
+  const uint32_t own = order_key(key);
+  // lanes of better groups, and of equal ones before this; each counts as often
+  // as a group has lanes
+  int better = 0;
+  const int shift = __builtin_ctz((unsigned)lanes), group = sub >> shift;
+  auto look = [&](uint32_t other, int n) {
+    const bool before = ((sub - n) & 15) >> shift < group;
+    better += other >= own + (before ? 0u : 1u);
+  };
+#define MOE_LOOK(N) look(row_rotate<N>(own), N);
+  MOE_LOOK(1) MOE_LOOK(2) MOE_LOOK(3) MOE_LOOK(4) MOE_LOOK(5) MOE_LOOK(6) MOE_LOOK(7) MOE_LOOK(8)
+  MOE_LOOK(9) MOE_LOOK(10) MOE_LOOK(11) MOE_LOOK(12) MOE_LOOK(13) MOE_LOOK(14) MOE_LOOK(15)
+#undef MOE_LOOK
+  const bool keep = key > -INFINITY && better < a.top_groups * lanes;
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) s[i] = exp_term(x[i], m);
-      total = fold<LANES, VPL>(s);
-      if (!(total > 0.0f)) total = 1.0f;
+  for (int i = 0; i < VPL; ++i) kf[i] = keep ? kf[i] : -INFINITY;
+}
+
+// The same for any groups; `mine`: the keys in LDS.
+template <int LANES, int VPL>
+__device__ __forceinline__ void keep_groups(const RouteArgs& a, int sub, int tok, float* mine,
+                                            float (&kf)[VPL]) {
+  const int e0 = sub * VPL, size = a.E / a.groups;
+  TopTwo g = {-INFINITY, -INFINITY};
+  if (sub < a.groups) {
+    const float* from = mine + sub * size;
+    int i = 0;
+    for (; i + 3 < size; i += 4) {
+      const float v[4] = {from[i], from[i + 1], from[i + 2], from[i + 3]};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) g.add(v[j], -INFINITY);
     }
+    for (; i < size; ++i) g.add(from[i], -INFINITY);
   }
-  float kf[VPL];
+  const float key = group_key(g, a.group_top);
+  wave_order();
+  if (sub < a.groups) mine[sub] = key;
+  wave_order();
+  int rank = 0;
+  for (int n = 0; n < a.groups; ++n) {
+    const float v = mine[n];
+    rank += v > key || (v == key && n < sub);
+  }
+  const uint64_t kept =
+      __ballot(sub < a.groups && key > -INFINITY && rank < a.top_groups) >> (tok * LANES);
+  int n = e0 / size, r = e0 - n * size;
 #pragma unroll
   for (int i = 0; i < VPL; ++i) {
-    kf[i] = x[i];
-    if (by_score) {
-      float v = a.sigmoid ? s[i] : s[i] / total;
-      if (a.bias && e0 + i < a.E) v += a.bias[e0 + i];
-      kf[i] = x[i] > -INFINITY ? v : -INFINITY;
-    }
-    if (!(kf[i] > -INFINITY)) kf[i] = -INFINITY;   // NaN too
-  }
-
-  if (a.groups > 1) {
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) mine[e0 + i] = kf[i];
-    wave_order();
-    const int size = a.E / a.groups;
-    float best = -INFINITY, second = -INFINITY;
-    if (sub < a.groups) {
-      for (int i = 0; i < size; ++i) {
-        const float v = mine[sub * size + i];
-        second = fmaxf(second, fminf(best, v));
-        best = fmaxf(best, v);
-      }
-      if (a.group_top > 1 && second > -INFINITY) best += second;
-    }
-    wave_order();
-    if (sub < a.groups) mine[sub] = best;
-    wave_order();
-    int rank = 0;
-    for (int g = 0; g < a.groups; ++g) {
-      const float v = mine[g];
-      rank += v > best || (v == best && g < sub);
-    }
-    const uint64_t kept =
-        __ballot(sub < a.groups && best > -INFINITY && rank < a.top_groups) >> (tok * LANES);
-    int g = e0 / size, r = e0 - g * size;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      if (g >= a.groups || !((kept >> g) & 1)) kf[i] = -INFINITY;
-      if (++r == size) {
-        r = 0;
-        ++g;
-      }
+    if (n >= a.groups || !((kept >> n) & 1)) kf[i] = -INFINITY;
+    if (++r == size) {
+      r = 0;
+      ++n;
     }
   }
+  wave_order();
+}
 
-  uint32_t key[VPL];
-#pragma unroll
-  for (int i = 0; i < VPL; ++i) key[i] = kf[i] > -INFINITY ? order_key(kf[i]) : 0u;
-  int won = -1;                                   // slot `sub`'s expert
-  for (int j = 0; j < a.k; ++j) {
+// Slot `sub`'s expert, or -1: the k highest keys one after another.
+template <int LANES, int VPL>
+__device__ __forceinline__ int winners_in_turn(int k, int sub, uint32_t (&key)[VPL]) {
+  const int e0 = sub * VPL;
+  int won = -1;
+  for (int j = 0; j < k; ++j) {
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) top = umax(top, key[i]);
@@ -226,6 +246,190 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t
     for (int i = 0; i < VPL; ++i) key[i] = at == (uint32_t)(e0 + i) ? 0u : key[i];
     if (sub == j && top) won = (int)at;
   }
+  return won;
+}
+
+constexpr int kCandidates = 64;
+
+// Candidates of a token in LDS, in the order of their experts.
+struct Candidates {
+  uint32_t key[kCandidates];
+  uint16_t expert[kCandidates];
+  int16_t slot[MOE_MAX_K];
+};
+
+// The same by a threshold: the k-th highest of the lanes' own maxima.  The k
+// winners are at least as high, few others are; they are collected in LDS and
+// each counts those above it.  Returns false, for the whole wavefront, where a
+// token has more than kCandidates (equal keys, few lanes left).
+template <int LANES, int VPL, int PARTS>
+__device__ __forceinline__ bool winners_by_threshold(int k, int sub, int tok, const uint32_t (&key)[VPL],
+                                                     const uint32_t* mine, Candidates* c, int& won) {
+  const int e0 = sub * VPL;
+  uint32_t least;
+  if constexpr (LANES == 16) {
+    // PARTS maxima of a lane: with groups left out half the lanes have none, and
+    // half a lane's are needed for k high ones
+    constexpr int PER = VPL / PARTS;
+    uint32_t top[PARTS] = {};
+    int above[PARTS] = {};
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) top[p] = umax(top[p], key[p * PER + i]);
+    auto look = [&](uint32_t other) {
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) above[p] += other > top[p];
+    };
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      if (PARTS > 1) look(top[p]);
+#define MOE_LOOK(N) look(row_rotate<N>(top[p]));
+      MOE_LOOK(1) MOE_LOOK(2) MOE_LOOK(3) MOE_LOOK(4) MOE_LOOK(5) MOE_LOOK(6) MOE_LOOK(7)
+      MOE_LOOK(8) MOE_LOOK(9) MOE_LOOK(10) MOE_LOOK(11) MOE_LOOK(12) MOE_LOOK(13) MOE_LOOK(14)
+      MOE_LOOK(15)
+#undef MOE_LOOK
+    }
+    least = ~0u;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) least = above[p] < k ? umin(least, top[p]) : least;
+  } else {
+    uint32_t left = 0;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) left = umax(left, key[i]);
+    least = ~0u;
+    for (int seen = 0; seen < k;) {                   // the same in every lane
+      const uint32_t m = reduce_max<LANES>(left);
+      const bool is = left == m;
+      least = m;
+      if (m == 0) break;
+      left = is ? 0u : left;
+      seen += __builtin_popcountll(__ballot(is));
+    }
+  }
+  least = reduce_min<LANES>(least);
+  least = umax(least, 1u);                            // eligible ones only
+  uint32_t mask = 0;
+#pragma unroll
+  for (int i = 0; i < VPL; ++i) mask |= key[i] >= least ? 1u << i : 0u;
+  const int count = __builtin_popcount(mask);
+  uint32_t end = (uint32_t)count;                     // inclusive over the token's lanes
+  end += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)end, 0x111, 0xf, 0xf, true);
+  end += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)end, 0x112, 0xf, 0xf, true);
+  end += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)end, 0x114, 0xf, 0xf, true);
+  end += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)end, 0x118, 0xf, 0xf, true);
+  if (LANES == 64) {
+    end += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)end, 0x142, 0xa, 0xf, false);
+    end += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)end, 0x143, 0xc, 0xf, false);
+  }
+  const int n = (int)reduce_max<LANES>(end);
+  if (__ballot(n > kCandidates)) return false;
+  for (int p = (int)end - count; mask; ++p, mask &= mask - 1) {
+    const int e = e0 + __builtin_ctz(mask);
+    c->key[p] = mine[e];
+    c->expert[p] = (uint16_t)e;
+  }
+  if (sub < 4 && n + sub < kCandidates) c->key[n + sub] = 0;   // read in fours below
+  if (sub < k) c->slot[sub] = -1;
+  wave_order();
+  for (int p = sub; p < n; p += LANES) {
+    const uint32_t own = c->key[p];
+    int rank = 0;
+    for (int q = 0; q < n; q += 4) {                  // equal keys: the earlier one first
+      const u32x4 o = *reinterpret_cast<const u32x4*>(&c->key[q]);
+      rank += o.x >= own + (q >= p);
+      rank += o.y >= own + (q + 1 >= p);
+      rank += o.z >= own + (q + 2 >= p);
+      rank += o.w >= own + (q + 3 >= p);
+    }
+    if (rank < k) c->slot[rank] = (int16_t)c->expert[p];
+  }
+  wave_order();
+  won = sub < k ? c->slot[sub] : -1;
+  return true;
+}
+
+// What the experts are ordered by: the logits, scores (+ bias), or the logits
+// with the softmax's sum taken for the weights.  Kernels of their own: what
+// each needs beyond the others costs it microseconds.
+enum Groups : int { kOneGroup = 0, kLaneGroups = 1, kAnyGroups = 2 };
+enum Keys : int { kLogits = 0, kSigmoidKeys = 1, kSoftmaxKeys = 2, kSoftmaxSum = 3 };
+
+// From eight experts to a lane on the threshold is the faster way (16384 tokens, 256 experts, 8
+// slots 9.0 -> 6.7 us; 32768 tokens, 128 experts 9.5 -> 8.2; four to a lane: equal).
+constexpr bool by_threshold(int vpl) { return vpl >= 8; }
+
+// Route token t: lane `sub` of its LANES, `tok` its place in the wavefront,
+// `mine` and `c` its LDS.  Every lane of the wavefront takes part.
+template <int LANES, int VPL, Keys KEYS, Groups GROUPS>
+__device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t t, int sub, int tok,
+                                            float* mine, Candidates* c) {
+#pragma clang fp contract(off)
+  const bool in = t < a.tokens;
+  const bool live = in && (!a.token_mask || a.token_mask[t]);
+  const int e0 = sub * VPL;
+  float x[VPL];
+  if (live) {
+    load_logits<VPL>(a.logits, a.f32, t * a.pitch, e0, a.E, vec, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
+  }
+
+  // x becomes the keys
+  float m = 0.0f, total = 1.0f;
+  if constexpr (KEYS == kSigmoidKeys) {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) x[i] = x[i] > -INFINITY ? sigmoid(x[i]) : -INFINITY;
+  }
+  if constexpr (KEYS == kSoftmaxKeys || KEYS == kSoftmaxSum) {
+    m = row_max<LANES, VPL>(x);
+    float s[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) s[i] = exp_term(x[i], m);
+    total = fold<LANES, VPL>(s);
+    if (!(total > 0.0f)) total = 1.0f;
+    if constexpr (KEYS == kSoftmaxKeys) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) x[i] = x[i] > -INFINITY ? s[i] / total : -INFINITY;
+    }
+  }
+  if constexpr (KEYS == kSigmoidKeys || KEYS == kSoftmaxKeys) {
+    if (a.bias) {
+      float b[VPL];
+      load_logits<VPL>(a.bias, true, 0, e0, a.E, vec && (uintptr_t)a.bias % 16 == 0, b);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) x[i] += b[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VPL; ++i) x[i] = x[i] > -INFINITY ? x[i] : -INFINITY;   // NaN too
+
+  constexpr bool kThreshold = by_threshold(VPL);
+  uint32_t key[VPL];
+  if constexpr (GROUPS == kLaneGroups) {
+    keep_lane_groups<VPL>(a, sub, x);
+  } else if constexpr (GROUPS == kAnyGroups) {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) mine[e0 + i] = x[i];
+    wave_order();
+    keep_groups<LANES, VPL>(a, sub, tok, mine, x);
+  }
+#pragma unroll
+  for (int i = 0; i < VPL; ++i) key[i] = x[i] > -INFINITY ? order_key(x[i]) : 0u;
+
+  int won = -1;                                   // slot `sub`'s expert
+  bool found = false;
+  if constexpr (kThreshold) {
+    if (a.k > 2) {
+      uint32_t* keys = reinterpret_cast<uint32_t*>(mine);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) keys[e0 + i] = key[i];
+      wave_order();
+      found = winners_by_threshold<LANES, VPL, GROUPS == kOneGroup ? 1 : 2>(a.k, sub, tok, key, keys, c, won);
+    }
+  }
+  if (!found) won = winners_in_turn<LANES, VPL>(a.k, sub, key);
 
   // weights: lane j of the token has slot j
   float w = 0.0f;
@@ -234,7 +438,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t
   if (won >= 0) xw = logit_at(a.logits, a.f32, t * a.pitch + won);
   if (a.sigmoid) {
     w = won >= 0 ? sigmoid(xw) : 0.0f;
-  } else if (plain) {
+  } else if ((KEYS == kSoftmaxKeys || KEYS == kSoftmaxSum) && !a.renorm) {
     w = exp_term(xw, m) / total;
   } else {
     const float one[1] = {xw};
@@ -250,15 +454,19 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t
   }
 }
 
-template <int LANES, int VPL>
-__global__ __launch_bounds__(kBlock) void route_kernel(RouteArgs a, int vec) {
+template <int LANES, int VPL, Keys KEYS, Groups GROUPS>
+__global__ __launch_bounds__(kBlock, GROUPS == kAnyGroups || VPL == 16 ? 2 : 4) void route_kernel(RouteArgs a, int vec) {
   constexpr int kTokens = kWave / LANES;         // of a wavefront
-  __shared__ float s_key[kWavesPerBlock][kTokens][LANES * VPL];
+  __shared__ __attribute__((aligned(16))) float s_key[kWavesPerBlock][kTokens][LANES * VPL];
+  constexpr bool kThreshold = by_threshold(VPL);
+  __shared__ __attribute__((aligned(16)))
+  Candidates s_candidates[kThreshold ? kWavesPerBlock : 1][kThreshold ? kTokens : 1];
   const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
   const int sub = lane & (LANES - 1), tok = lane / LANES;
   for (int64_t t0 = ((int64_t)blockIdx.x * kWavesPerBlock + wave) * kTokens; t0 < a.tokens;
        t0 += (int64_t)gridDim.x * kWavesPerBlock * kTokens)
-    route_token<LANES, VPL>(a, vec, t0 + tok, sub, tok, s_key[wave][tok]);
+    route_token<LANES, VPL, KEYS, GROUPS>(a, vec, t0 + tok, sub, tok, s_key[wave][tok],
+                                           &s_candidates[kThreshold ? wave : 0][kThreshold ? tok : 0]);
 }
 
 // The dense part of a softmax's gradient reaches every expert, the others only
@@ -407,9 +615,25 @@ unsigned route_blocks(int64_t tokens, int lanes) {
 hipError_t launch_route(const RouteArgs& a, hipStream_t stream) {
   return by_width(a.E, a.k, a.groups, a.tokens, [&](auto lanes, auto vpl) {
     const int vec = vector_rows(a.logits, nullptr, a.pitch, a.E, vpl.value, a.f32);
-    hipLaunchKernelGGL((route_kernel<lanes.value, vpl.value>),
-                       dim3(route_blocks(a.tokens, lanes.value)), dim3(kBlock), 0, stream, a, vec);
-    return hipGetLastError();
+    const dim3 grid(route_blocks(a.tokens, lanes.value));
+    const auto run = [&](auto keys, auto groups) {
+      hipLaunchKernelGGL((route_kernel<lanes.value, vpl.value, keys.value, groups.value>), grid,
+                         dim3(kBlock), 0, stream, a, vec);
+      return hipGetLastError();
+    };
+    const auto by_groups = [&](auto keys) {
+      if (a.groups == 1) return run(keys, std::integral_constant<Groups, kOneGroup>());
+      if constexpr (lanes.value == 16) {
+        if (a.E == 16 * vpl.value && 16 % a.groups == 0)
+          return run(keys, std::integral_constant<Groups, kLaneGroups>());
+      }
+      return run(keys, std::integral_constant<Groups, kAnyGroups>());
+    };
+    if (a.bias || (a.groups > 1 && a.group_top > 1))
+      return a.sigmoid ? by_groups(std::integral_constant<Keys, kSigmoidKeys>())
+                       : by_groups(std::integral_constant<Keys, kSoftmaxKeys>());
+    if (!a.sigmoid && !a.renorm) return by_groups(std::integral_constant<Keys, kSoftmaxSum>());
+    return by_groups(std::integral_constant<Keys, kLogits>());
   });
 }
 
