@@ -472,7 +472,7 @@ __global__ __launch_bounds__(kBlock, GROUPS == kAnyGroups || VPL == 16 ? 2 : 4) 
 // The dense part of a softmax's gradient reaches every expert, the others only
 // the chosen ones; either way a token's row is put together in LDS (one
 // value per slot) and written whole.
-template <int LANES, int VPL>
+template <int LANES, int VPL, bool DENSE>
 __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int vec, int64_t t,
                                                      int sub, float* row) {
   const bool in = t < a.tokens;
@@ -495,9 +495,8 @@ __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int
     }
   }
 
-  const bool dense = !a.sigmoid && !a.renorm;
   float x[VPL], m = 0.0f, inv = 0.0f, q, d;
-  if (dense) {
+  if constexpr (DENSE) {
 #pragma unroll
     for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
     if (in) load_logits<VPL>(a.logits, a.f32, t * a.pitch, e0, a.E, vec, x);
@@ -527,14 +526,14 @@ __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int
     q = sum > 0.0f ? q / sum : 0.0f;
     d = q;
   }
-  const float dot = dense || a.renorm ? reduce_sum<LANES>(g * q) : 0.0f;
+  const float dot = DENSE || a.renorm ? reduce_sum<LANES>(g * q) : 0.0f;
   wave_order();
-  if (e >= 0) row[e] = dense ? d : d * (g - dot);
+  if (e >= 0) row[e] = DENSE ? d : d * (g - dot);
   wave_order();
   if (!in) return;
 #pragma unroll
   for (int i = 0; i < VPL; ++i) {
-    if (dense) x[i] = x[i] * inv * (row[e0 + i] - dot);
+    if (DENSE) x[i] = x[i] * inv * (row[e0 + i] - dot);
     else x[i] = row[e0 + i];
   }
   const int64_t at = t * a.E + e0;
@@ -548,8 +547,15 @@ __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int
                           __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3])});
     } else {
       uint16_t* p = static_cast<uint16_t*>(a.grad_logits) + at;
+      if constexpr (VPL >= 8) {
 #pragma unroll
-      for (int i = 0; i + 1 < VPL; i += 2) st4(p + i, pack_bf16x2(x[i], x[i + 1]));
+        for (int i = 0; i + 7 < VPL; i += 8)
+          st16(p + i, u32x4{pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3]),
+                            pack_bf16x2(x[i + 4], x[i + 5]), pack_bf16x2(x[i + 6], x[i + 7])});
+      } else {
+#pragma unroll
+        for (int i = 0; i + 1 < VPL; i += 2) st4(p + i, pack_bf16x2(x[i], x[i + 1]));
+      }
     }
     return;
   }
@@ -564,7 +570,7 @@ __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int
   }
 }
 
-template <int LANES, int VPL>
+template <int LANES, int VPL, bool DENSE>
 __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteGradArgs a, int vec) {
   constexpr int kTokens = kWave / LANES;         // of a wavefront
   __shared__ float s_row[kWavesPerBlock][kTokens][LANES * VPL];
@@ -572,7 +578,7 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteGradArgs a,
   const int sub = lane & (LANES - 1), tok = lane / LANES;
   for (int64_t t0 = ((int64_t)blockIdx.x * kWavesPerBlock + wave) * kTokens; t0 < a.tokens;
        t0 += (int64_t)gridDim.x * kWavesPerBlock * kTokens) {
-    route_token_backward<LANES, VPL>(a, vec, t0 + tok, sub, s_row[wave][tok]);
+    route_token_backward<LANES, VPL, DENSE>(a, vec, t0 + tok, sub, s_row[wave][tok]);
     wave_order();
   }
 }
@@ -640,8 +646,13 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t stream) {
 hipError_t launch_route_backward(const RouteGradArgs& a, hipStream_t stream) {
   return by_width(a.E, a.k, 1, a.tokens, [&](auto lanes, auto vpl) {
     const int vec = vector_rows(a.logits, a.grad_logits, a.pitch, a.E, vpl.value, a.f32);
-    hipLaunchKernelGGL((route_backward_kernel<lanes.value, vpl.value>),
-                       dim3(route_blocks(a.tokens, lanes.value)), dim3(kBlock), 0, stream, a, vec);
+    const dim3 grid(route_blocks(a.tokens, lanes.value));
+    if (!a.sigmoid && !a.renorm)
+      hipLaunchKernelGGL((route_backward_kernel<lanes.value, vpl.value, true>), grid, dim3(kBlock), 0,
+                         stream, a, vec);
+    else
+      hipLaunchKernelGGL((route_backward_kernel<lanes.value, vpl.value, false>), grid, dim3(kBlock),
+                         0, stream, a, vec);
     return hipGetLastError();
   });
 }

@@ -163,6 +163,24 @@ def test_equal_keys_take_the_lowest_index():
     assert torch.all(w == 0.125)
 
 
+@pytest.mark.parametrize("E,groups,top", [(256, 8, 4), (128, 4, 2), (256, 16, 3), (64, 2, 1), (60, 6, 2),
+                                          (160, 8, 3)])
+@pytest.mark.parametrize("two", [1, 2])
+def test_equal_groups_take_the_lowest_index(E, groups, top, two):
+    x = torch.zeros(6, E)
+    x[1, E // groups:] = 1.0                    # all groups but the first
+    x[2, E - 1] = 1.0                           # the last one stands out
+    x[3, : E // groups] = -math.inf
+    opt = dict(groups=groups, top_groups=top, group_top=two, score=1)
+    idx, w = _route(x, 6, **opt)
+    _check(x, idx, w, 6, **opt)
+    size = E // groups
+    assert idx[0].tolist() == list(range(6))
+    assert idx[1].tolist() == list(range(size, size + 6))
+    assert idx[2, 0] == E - 1 and (top == 1 or idx[2, 1] == 0)
+    assert idx[3].tolist() == list(range(size, size + 6))
+
+
 def test_token_mask_pitch_and_offset_bases():
     wide = _draw(40, 300, True, seed=9).cuda()
     mask = (torch.arange(40) % 3 != 0).to(torch.uint8)
