@@ -113,6 +113,15 @@ struct MatmulArgs {
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------- device
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(1))) u32x2 gu32x2;
+
+// 8-byte accesses to global memory.
+__device__ __forceinline__ u32x2 ld8(const void* p) { return *(const gu32x2*)(uintptr_t)p; }
+__device__ __forceinline__ void st4x2(void* p, uint32_t lo, uint32_t hi) {
+  *(gu32x2*)(uintptr_t)p = u32x2{lo, hi};
+}
+
 // Value of the lane N before, around the row of 16.
 template <int N>
 __device__ __forceinline__ uint32_t row_rotate(uint32_t x) {

@@ -94,11 +94,6 @@ __device__ __forceinline__ float silu(float g) {
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
 }
 
-__device__ __forceinline__ void st4x2(void* p, uint32_t lo, uint32_t hi) {
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  *(__attribute__((address_space(1))) u32x2*)(uintptr_t)p = u32x2{lo, hi};
-}
-
 // Buffer resource of `bytes` bytes from `base`, both the same in every lane.
 __device__ __forceinline__ Rsrc buffer_of(const uint8_t* base, int bytes) {
   const uint64_t p = (uint64_t)base;

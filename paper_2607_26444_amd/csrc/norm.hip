@@ -51,11 +51,6 @@ __device__ __forceinline__ void store8(uint8_t* row, int64_t v, bool f32, const 
   }
 }
 
-__device__ __forceinline__ void st8(uint8_t* p, uint32_t lo, uint32_t hi) {
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  *(__attribute__((address_space(1))) u32x2*)(uintptr_t)p = u32x2{lo, hi};
-}
-
 // |x| as an unsigned that orders alike, with NaN above infinity, so that a
 // maximum keeps it.
 __device__ __forceinline__ uint32_t abs_key(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
@@ -92,7 +87,7 @@ __device__ __forceinline__ void store_codes(uint8_t* q, int64_t v, bool fp8, con
     else
       w[h] = code_int8(a) | code_int8(b) << 8 | code_int8(c) << 16 | code_int8(d) << 24;
   }
-  st8(q + v * 8, w[0], w[1]);
+  st4x2(q + v * 8, w[0], w[1]);
 }
 
 // Sum and maximum over the row's wavefronts: wavefront results meet in LDS.

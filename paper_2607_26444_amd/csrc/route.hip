@@ -67,12 +67,11 @@ __device__ __forceinline__ void load_logits(const void* logits, bool f32, int64_
           }
         }
       } else {
-#pragma unroll
-        for (int i = 0; i + 1 < VPL; i += 2) {
-          const uint32_t w = ld4(p + i);
-          x[i] = bf16_lo(w);
-          x[i + 1] = bf16_hi(w);
-        }
+        const u32x2 w = ld8(p);                       // VPL is 4
+        x[0] = bf16_lo(w.x);
+        x[1] = bf16_hi(w.x);
+        x[2] = bf16_lo(w.y);
+        x[3] = bf16_hi(w.y);
       }
     }
     return;
@@ -472,13 +471,19 @@ __global__ __launch_bounds__(kBlock, GROUPS == kAnyGroups || VPL == 16 ? 2 : 4) 
 // The dense part of a softmax's gradient reaches every expert, the others only
 // the chosen ones; either way a token's row is put together in LDS (one
 // value per slot) and written whole.
+// Expert of a lane's i-th value in the gradient: fours of neighbours, dealt
+// to the lanes in turn, so that 16 lanes read and write 64 neighbours at once.
+template <int LANES, int VPL>
+__device__ __forceinline__ int dealt(int sub, int i) {
+  return VPL >= 4 ? (i / 4 * LANES + sub) * 4 + (i & 3) : sub * VPL + i;
+}
+
 template <int LANES, int VPL, bool DENSE>
 __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int vec, int64_t t,
                                                      int sub, float* row) {
   const bool in = t < a.tokens;
-  const int e0 = sub * VPL;
 #pragma unroll
-  for (int i = 0; i < VPL; ++i) row[e0 + i] = 0.0f;
+  for (int i = 0; i < VPL; ++i) row[dealt<LANES, VPL>(sub, i)] = 0.0f;
 
   int e = -1;
   float g = 0.0f, xe = -INFINITY;
@@ -499,7 +504,16 @@ __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int
   if constexpr (DENSE) {
 #pragma unroll
     for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
-    if (in) load_logits<VPL>(a.logits, a.f32, t * a.pitch, e0, a.E, vec, x);
+    if (in) {
+      constexpr int N = VPL >= 4 ? 4 : VPL;
+#pragma unroll
+      for (int g4 = 0; g4 < VPL / N; ++g4) {
+        float v[N];
+        load_logits<N>(a.logits, a.f32, t * a.pitch, dealt<LANES, VPL>(sub, g4 * N), a.E, vec, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[g4 * N + j] = v[j];
+      }
+    }
     m = row_max<LANES, VPL>(x);
     float local = 0.0f;
 #pragma unroll
@@ -533,39 +547,32 @@ __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int
   if (!in) return;
 #pragma unroll
   for (int i = 0; i < VPL; ++i) {
-    if (DENSE) x[i] = x[i] * inv * (row[e0 + i] - dot);
-    else x[i] = row[e0 + i];
+    const float r = row[dealt<LANES, VPL>(sub, i)];
+    x[i] = DENSE ? x[i] * inv * (r - dot) : r;
   }
-  const int64_t at = t * a.E + e0;
   if constexpr (VPL >= 4) if (vec) {
-    if (e0 >= a.E) return;
-    if (a.f32) {
-      float* p = static_cast<float*>(a.grad_logits) + at;
 #pragma unroll
-      for (int i = 0; i + 3 < VPL; i += 4)
-        st16(p + i, u32x4{__float_as_uint(x[i]), __float_as_uint(x[i + 1]),
-                          __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3])});
-    } else {
-      uint16_t* p = static_cast<uint16_t*>(a.grad_logits) + at;
-      if constexpr (VPL >= 8) {
-#pragma unroll
-        for (int i = 0; i + 7 < VPL; i += 8)
-          st16(p + i, u32x4{pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3]),
-                            pack_bf16x2(x[i + 4], x[i + 5]), pack_bf16x2(x[i + 6], x[i + 7])});
-      } else {
-#pragma unroll
-        for (int i = 0; i + 1 < VPL; i += 2) st4(p + i, pack_bf16x2(x[i], x[i + 1]));
-      }
+    for (int i = 0; i < VPL; i += 4) {
+      const int n = dealt<LANES, VPL>(sub, i);
+      if (n >= a.E) continue;
+      if (a.f32)
+        st16(static_cast<float*>(a.grad_logits) + t * a.E + n,
+             u32x4{__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]),
+                   __float_as_uint(x[i + 3])});
+      else
+        st4x2(static_cast<uint16_t*>(a.grad_logits) + t * a.E + n, pack_bf16x2(x[i], x[i + 1]),
+              pack_bf16x2(x[i + 2], x[i + 3]));
     }
     return;
   }
 #pragma unroll
   for (int i = 0; i < VPL; ++i) {
-    if (e0 + i >= a.E) {
+    const int n = dealt<LANES, VPL>(sub, i);
+    if (n >= a.E) {
     } else if (a.f32) {
-      static_cast<float*>(a.grad_logits)[at + i] = x[i];
+      static_cast<float*>(a.grad_logits)[t * a.E + n] = x[i];
     } else {
-      static_cast<uint16_t*>(a.grad_logits)[at + i] = (uint16_t)pack_bf16x2(x[i], 0.0f);
+      static_cast<uint16_t*>(a.grad_logits)[t * a.E + n] = (uint16_t)pack_bf16x2(x[i], 0.0f);
     }
   }
 }
@@ -645,7 +652,8 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t stream) {
 
 hipError_t launch_route_backward(const RouteGradArgs& a, hipStream_t stream) {
   return by_width(a.E, a.k, 1, a.tokens, [&](auto lanes, auto vpl) {
-    const int vec = vector_rows(a.logits, a.grad_logits, a.pitch, a.E, vpl.value, a.f32);
+    const int vec = vpl.value >= 4 &&
+                    vector_rows(a.logits, a.grad_logits, a.pitch, a.E, 4, a.f32);
     const dim3 grid(route_blocks(a.tokens, lanes.value));
     if (!a.sigmoid && !a.renorm)
       hipLaunchKernelGGL((route_backward_kernel<lanes.value, vpl.value, true>), grid, dim3(kBlock), 0,
