@@ -511,10 +511,39 @@ void matmul_stream_kernel(MatmulArgs a, int pieces) {
 // fit a GPU's memory.
 constexpr int64_t kMaxTiles = (1ll << 32) / kTileThreads - 256;
 
+// Row tiles of `size` that the windows can have: each window with rows adds at
+// most one that is not full.
+int64_t row_tiles(const MatmulArgs& a, int size) {
+  if (!a.offset) return (a.rows + size - 1) / size;
+  return a.rows / size + (a.rows < a.E ? a.rows : a.E);
+}
+
+// Microseconds that the two kernels take if the rows are spread evenly, from
+// their times on MI355X: a tile takes 1.6 a stage and 9 beside, on one of 256 compute
+// units; 64 rows x 128 channels of the stream kernel 1.15 a stage and 3 beside, two at
+// once on a compute unit (alone there 0.72).  Measured, tile / stream, and by
+// these rules: 2048 rows, 32 experts, 7168 x 4096 187 / 201 (198 / 201), 1536 rows 182 / 163
+// (198 / 167); one expert, 4096 x 4096, 2048 rows 61 / 73 (60 / 80), 1024 rows 58 / 36 (60 /
+// 40); 16384 rows, 64 experts, 1024 x 512 25 / 26 (22 / 27), 8192 rows 22 / 18 (22 / 15).
+double window_tiles(const MatmulArgs& a, int size) {
+  const double windows = (double)(a.rows < a.E ? a.rows : a.E), n = (double)a.rows / windows / size;
+  return windows * (a.E == 1 ? __builtin_ceil(n) : n > 0.5 ? n + 0.5 : 1.0);
+}
+double tile_time(const MatmulArgs& a, int pieces) {
+  const double rounds = window_tiles(a, kTile) * pieces / 256.0;
+  return (rounds < 1.0 ? 1.0 : rounds) * (9.0 + 1.6 * ((a.K + kDepth - 1) / kDepth));
+}
+double stream_time(const MatmulArgs& a, int pieces) {
+  const double stages = (a.K + kDepth - 1) / kDepth;
+  const double groups = window_tiles(a, 64) * 2.0 * pieces;
+  return groups <= 256.0 ? 3.0 + 0.72 * stages
+                         : (groups < 512.0 ? 1.0 : groups / 512.0) * (3.0 + 1.15 * stages);
+}
+
 template <int ROWS, int WC, int WK, int STAGES>
 hipError_t launch_stream(const MatmulArgs& a, int out, hipStream_t stream) {
   const int per = WC * (a.swiglu ? 8 : 16), pieces = (out + per - 1) / per;
-  const int64_t tiles = ((a.rows + ROWS - 1) / ROWS + (a.offset ? a.E : 0)) * pieces;
+  const int64_t tiles = row_tiles(a, ROWS) * pieces;
   if (tiles > kMaxTiles) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((matmul_stream_kernel<ROWS, WC, WK, STAGES>),
                      dim3((unsigned)((tiles + 255) / 256 * 256)), dim3(kTileThreads), 0, stream, a,
@@ -526,14 +555,9 @@ hipError_t launch_stream(const MatmulArgs& a, int out, hipStream_t stream) {
 
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
   const int out = a.swiglu ? a.N / 2 : a.N;
-  // Many rows: the tile kernel, from 64 rows to an expert and 128 full tiles.
-  // Below either, its tiles leave compute units idle or read the weights no
-  // faster (us, tile / stream): 2048 rows, 32 experts, 7168 x 4096 187 / 201, 1536
-  // rows 182 / 163; one expert, 4096 x 4096, 2048 rows 61 / 73, 1024 rows 58 / 36.
   const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
-  if (a.rows / a.E >= 64 && a.rows / kTile * pieces >= 128) {
-    const int64_t tiles = ((a.rows + kTile - 1) / kTile + (a.offset ? a.E : 0)) * pieces;
-    if (tiles > INT32_MAX - 256) return hipErrorInvalidConfiguration;   // tile numbers are int
+  const int64_t tiles = row_tiles(a, kTile) * pieces;
+  if (tile_time(a, pieces) < stream_time(a, pieces) && tiles < INT32_MAX - 256) {
     // six row tiles together: of 2, 4, 5, 6 and 8 the best or near it (32768 x 2048 x 7168
     // over 32 experts 528 / 522 / 512 / 510 / 509 us, 16384 x 8192 x 8192 846 / 832 / 815 / 811 / 835)
     hipLaunchKernelGGL(matmul_tile_kernel, dim3(256), dim3(kTileThreads), 0, stream, a, pieces, 6);
