@@ -126,6 +126,45 @@ def test_large_tiles(rows, N, K, E, swiglu):
     t = _inputs(rows, E, N, K, seed=rows)
     _check(_run(*t, offset, counts, swiglu), *t, windows, swiglu)
 
+# Sizes whose products fill the GPU with 256 x 256 tiles: windows that end after
+# 1, 4, 65, 76 .. rows of a tile, outputs that end inside a tile, a depth that ends inside a
+# stage and one that is shorter than a stage.
+@pytest.mark.parametrize("counts,N,K", [([4100], 4112, 1040), ([8193], 2064, 16),
+                                        ([0, 1024, 700, 2300, 65], 4112, 400),
+                                        ([1000, 1], 16400, 272),
+                                        ([65, 190, 3, 250] * 32 + [0, 700], 2064, 144)])
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_many_tiles(counts, N, K, swiglu):
+    E, rows = len(counts), sum(counts)
+    N -= 0 if swiglu else 8                                   # an odd number of eights
+    offset, windows = _packed(counts)
+    t = _inputs(rows, E, N, K, seed=rows)
+    y = _run(*t, offset, counts, swiglu) if E > 1 else _run(*t, None, None, swiglu)
+    _check(y, *t, windows, swiglu)
+    if E > 1:
+        assert torch.equal(_run(*t, offset, None, swiglu), y)
+
+
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_many_tiles_fixed_windows(swiglu):
+    """Equal capacities of which some are empty, full or hold a few rows; then all empty."""
+    E, cap, N, K = 12, 800, 2064, 272
+    counts = [0, 800, 1, 130, 257, 0, 799, 70, 512, 0, 0, 5]
+    base = 4321
+    offset = [base + e * cap for e in range(E + 1)]
+    t = _inputs(E * cap, E, N, K, seed=12)
+    windows = [(e * cap, n) for e, n in enumerate(counts)]
+    _check(_run(*t, offset, counts, swiglu), *t, windows, swiglu)
+    assert torch.all(torch.isnan(_run(*t, offset, [0] * E, swiglu).float()))
+
+
+def test_many_tiles_against_few():
+    """The same rows in one call and in calls of 40 rows, which another kernel takes."""
+    a, sa, w, sw = _inputs(4100, 1, 4112, 1040, seed=5)
+    y = _run(a, sa, w, sw, None, None, True)
+    for r in (0, 1000, 2048, 4060):
+        assert torch.equal(_run(a[r:r + 40], sa[r:r + 40], w, sw, None, None, True), y[r:r + 40])
+
 
 def test_scale_pitch():
     a, sa, w, sw = _inputs(40, 1, 64, 128, seed=2)
