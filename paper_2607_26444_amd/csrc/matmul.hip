@@ -1,5 +1,11 @@
-// The experts' products on 8-bit integers: int32 sums by matrix instructions,
-// exact in any order, scaled and rounded to bf16 once.
+// The experts' products on 8-bit integers:
+//   v[r,n] = (sum_k a[r,k] w[e,n,k]) a_scale[r] w_scale[e,n], y = bf16(v), or with
+//   swiglu y[r,i] = bf16(silu(v[r,i]) v[r,N/2+i]).
+// int32 sums by matrix instructions, exact in any order, scaled and rounded to
+// bf16 once.  Two kernels: tiles of 256 x 256 where arithmetic bounds the call,
+// 64 rows or fewer x 128 channels or fewer where reading the weights does.
+// Windows are on the GPU, so a launch covers every tile that they can have;
+// workgroups find theirs by a scan of the counts.
 
 #include <type_traits>
 
@@ -130,7 +136,16 @@ __device__ __forceinline__ void meet() {
 
 // Tiles of 256 rows x 256 channels through LDS: eight wavefronts, each 128 rows
 // x 64 channels; pieces of 128 of the depth go from memory into LDS by the
-// loads themselves, one piece ahead of the matrix instructions.
+// loads themselves, one piece ahead of the matrix instructions.  A wavefront reads
+// 12 fragments for 32 matrix instructions of 16 x 16 x 64, half a stage ahead.
+//
+// Bound by the matrix instructions, which are busy about two thirds of the cycles
+// at the clock that the card's power leaves them (operands of zeros run 8% faster).
+// 32768 rows, 16 experts, 7168 x 4096 with swiglu: 805 us, 2390 TOP/s; 16384 x 8192 x
+// 8192: 807 us, 2725 TOP/s; 32 experts of 980 to 1080 rows, 7168 x 4096: 835 us.  Beside
+// it 32 x 32 x 32 instructions 1012 us (16 x 16 x 64 then: 934), stages of half the
+// depth with the wavefronts in two phases 920 (850), a second barrier +4%,
+// touching the lines of later stages beforehand +2 to 10%.
 constexpr int kTile = 256;
 constexpr int kTileThreads = 512;
 constexpr int kTileBytes = kTile * kDepth;
@@ -387,7 +402,11 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
 }
 
 // Few rows: ROWS rows of a window x 16 WC channels, bound by reading the
-// weights.  Eight wavefronts, WC along the channels and WK along the depth; a
+// weights: 512 rows, 32 experts, 7168 x 4096 with swiglu (946 MB) 149 us, 6.3 TB/s; without
+// LDS between, whole rows of weights a wavefront, 262 us (half lines fetched twice).
+// Two stages where there is room for three: 174 us.  4662 rows, 96 experts, 2064 x
+// 1416 (304 MB): 82 us, the workgroups' beginnings and ends and a last round that
+// fills a quarter of the GPU.  Eight wavefronts, WC along the channels and WK along the depth; a
 // stage is 128 WK of the depth, STAGES - 1 stages are on their way while one is
 // multiplied.  A wavefront loads its own weights (8 + 8 channels: with swiglu
 // gate and up channels, so that a lane and its partner 32 further on hold both
@@ -507,8 +526,8 @@ void matmul_stream_kernel(MatmulArgs a, int pieces) {
   }
 }
 
-// Tiles of one launch: HIP's limit of 2^32 threads.  The outputs and weights of more would not
-// fit a GPU's memory.
+// Tiles of one launch: HIP's limit of 2^32 threads.  The outputs and weights of
+// more would not fit a GPU's memory.
 constexpr int64_t kMaxTiles = (1ll << 32) / kTileThreads - 256;
 
 // Row tiles of `size` that the windows can have: each window with rows adds at
@@ -519,12 +538,16 @@ int64_t row_tiles(const MatmulArgs& a, int size) {
 }
 
 // Microseconds that the two kernels take if the rows are spread evenly, from
-// their times on MI355X: a tile takes 1.6 a stage and 9 beside, on one of 256 compute
-// units; 64 rows x 128 channels of the stream kernel 1.15 a stage and 3 beside, two at
-// once on a compute unit (alone there 0.72).  Measured, tile / stream, and by
-// these rules: 2048 rows, 32 experts, 7168 x 4096 187 / 201 (198 / 201), 1536 rows 182 / 163
-// (198 / 167); one expert, 4096 x 4096, 2048 rows 61 / 73 (60 / 80), 1024 rows 58 / 36 (60 /
-// 40); 16384 rows, 64 experts, 1024 x 512 25 / 26 (22 / 27), 8192 rows 22 / 18 (22 / 15).
+// their times on MI355X: a tile takes 1.6 a stage and 9 beside, on one of 256
+// compute units; 64 rows x 128 channels of the stream kernel 1.15 a stage and 3
+// beside, two at once on a compute unit (alone there 0.72).  Measured, tile /
+// stream, and by these rules:
+//   2048 rows, 32 experts, 7168 x 4096   187 / 201   (198 / 201)
+//   1536 rows                            182 / 163   (198 / 167)
+//   2048 rows, one expert, 4096 x 4096    61 / 73     (60 / 80)
+//   1024 rows                             58 / 36     (60 / 40)
+//   16384 rows, 64 experts, 1024 x 512    25 / 26     (22 / 27)
+//   8192 rows                             22 / 18     (22 / 15)
 double window_tiles(const MatmulArgs& a, int size) {
   const double windows = (double)(a.rows < a.E ? a.rows : a.E), n = (double)a.rows / windows / size;
   return windows * (a.E == 1 ? __builtin_ceil(n) : n > 0.5 ? n + 0.5 : 1.0);
@@ -558,16 +581,17 @@ hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
   const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
   const int64_t tiles = row_tiles(a, kTile) * pieces;
   if (tile_time(a, pieces) < stream_time(a, pieces) && tiles < INT32_MAX - 256) {
-    // six row tiles together: of 2, 4, 5, 6 and 8 the best or near it (32768 x 2048 x 7168
-    // over 32 experts 528 / 522 / 512 / 510 / 509 us, 16384 x 8192 x 8192 846 / 832 / 815 / 811 / 835)
+    // six row tiles together: of 2, 4, 5, 6 and 8 the best or near it (32768 x
+    // 2048 x 7168 over 32 experts 528 / 522 / 512 / 510 / 509 us, 16384 x 8192 x 8192
+    // 846 / 832 / 815 / 811 / 835)
     hipLaunchKernelGGL(matmul_tile_kernel, dim3(256), dim3(kTileThreads), 0, stream, a, pieces, 6);
     return hipGetLastError();
   }
   // Few rows: 128 channels to a workgroup where that gives every compute unit
   // one (windows that can have rows are counted), else fewer channels and
   // more of the depth at once.  With at most 16 rows in all a stage needs room
-  // for no more.  4096 x 7168, one expert, us at 128 / 64 / 32 / 16 channels: 1 row 26 /
-  // 16 / 12 / 9, 64 rows 29 / 19 / 14 / -; 32 experts, 512 rows 159 / 158 / 208 / 258.
+  // for no more.  4096 x 7168, us at 128 / 64 / 32 / 16 channels: one expert, 1 row
+  // 26 / 16 / 12 / 9, 64 rows 29 / 19 / 14 / -; 32 experts, 512 rows 159 / 158 / 208 / 258.
   const int64_t windows = (a.rows < a.E ? a.rows : a.E) + a.rows / 64;
   const auto groups = [&](int tiles) {
     const int c = tiles * (a.swiglu ? 8 : 16);

@@ -2,10 +2,20 @@
 // of the weights with respect to the logits.
 //
 // One token takes LANES (16 or 64) neighbouring lanes of a wavefront, each with
-// VPL neighbouring experts in registers; the k winners are found one after
-// another as the largest key of the lanes, equal keys by the lowest index.
-// Keys are the floats' bit patterns made to order as unsigned integers, so a
-// maximum over lanes is one DPP instruction per step.
+// VPL neighbouring experts in registers.  Keys are the floats' bit patterns made to
+// order as unsigned integers, so a maximum over lanes is one DPP instruction
+// per step; equal keys go to the lowest index.  With few experts to a lane the k
+// winners are found one after another as the largest key left, with many by a
+// threshold that hardly more than k keys pass.  The softmax's sum is needed only where
+// weights are not renormalised or scores are the keys: renormalised weights
+// are a softmax over the k winners' logits.  All of it is float32, the sum in a
+// fixed order, so equal inputs give equal keys.
+//
+// A batch is read once and little is written, but neither bounds it: up to
+// about 4096 tokens a call takes 4 to 5 us, of which the launch is most, and beyond
+// that the instructions of a token do.  16384 tokens, 256 float32 logits, 8 slots (17.8
+// MB): 6.7 us; with sigmoid, bias and 4 of 8 groups 11.9 us.  The gradient of 32768 x
+// 128 bf16 softmax logits (18.9 MB): 7.3 us.
 
 #include <math.h>
 
@@ -87,7 +97,6 @@ __device__ __forceinline__ float exp_term(float x, float m) {
   if (!(x > -INFINITY)) return 0.0f;
   return x == m ? 1.0f : expf(x - m);
 }
-
 
 // 1 / x for x >= 1 as an exact division rounds it: one Newton step on the
 // hardware's reciprocal (1 ulp) is the correctly rounded one for every
@@ -262,8 +271,9 @@ struct Candidates {
 // each counts those above it.  Returns false, for the whole wavefront, where a
 // token has more than kCandidates (equal keys, few lanes left).
 template <int LANES, int VPL, int PARTS>
-__device__ __forceinline__ bool winners_by_threshold(int k, int sub, int tok, const uint32_t (&key)[VPL],
-                                                     const uint32_t* mine, Candidates* c, int& won) {
+__device__ __forceinline__ bool winners_by_threshold(int k, int sub, const uint32_t (&key)[VPL],
+                                                     const uint32_t* mine, Candidates* c,
+                                                     int& won) {
   const int e0 = sub * VPL;
   uint32_t least;
   if constexpr (LANES == 16) {
@@ -354,15 +364,16 @@ __device__ __forceinline__ bool winners_by_threshold(int k, int sub, int tok, co
 enum Groups : int { kOneGroup = 0, kLaneGroups = 1, kAnyGroups = 2 };
 enum Keys : int { kLogits = 0, kSigmoidKeys = 1, kSoftmaxKeys = 2, kSoftmaxSum = 3 };
 
-// From eight experts to a lane on the threshold is the faster way (16384 tokens, 256 experts, 8
-// slots 9.0 -> 6.7 us; 32768 tokens, 128 experts 9.5 -> 8.2; four to a lane: equal).
+// From eight experts to a lane on the threshold is the faster way (16384
+// tokens, 256 experts, 8 slots 9.0 -> 6.7 us; 32768 tokens, 128 experts 9.5 -> 8.2;
+// four to a lane: equal).  Up to two slots are found in turn.
 constexpr bool by_threshold(int vpl) { return vpl >= 8; }
 
 // Route token t: lane `sub` of its LANES, `tok` its place in the wavefront,
 // `mine` and `c` its LDS.  Every lane of the wavefront takes part.
 template <int LANES, int VPL, Keys KEYS, Groups GROUPS>
-__device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t t, int sub, int tok,
-                                            float* mine, Candidates* c) {
+__device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t t, int sub,
+                                            int tok, float* mine, Candidates* c) {
 #pragma clang fp contract(off)
   const bool in = t < a.tokens;
   const bool live = in && (!a.token_mask || a.token_mask[t]);
@@ -425,7 +436,8 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t
 #pragma unroll
       for (int i = 0; i < VPL; ++i) keys[e0 + i] = key[i];
       wave_order();
-      found = winners_by_threshold<LANES, VPL, GROUPS == kOneGroup ? 1 : 2>(a.k, sub, tok, key, keys, c, won);
+      found = winners_by_threshold<LANES, VPL, GROUPS == kOneGroup ? 1 : 2>(a.k, sub, key, keys, c,
+                                                                            won);
     }
   }
   if (!found) won = winners_in_turn<LANES, VPL>(a.k, sub, key);
@@ -454,7 +466,8 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int vec, int64_t
 }
 
 template <int LANES, int VPL, Keys KEYS, Groups GROUPS>
-__global__ __launch_bounds__(kBlock, GROUPS == kAnyGroups || VPL == 16 ? 2 : 4) void route_kernel(RouteArgs a, int vec) {
+__global__ __launch_bounds__(kBlock, GROUPS == kAnyGroups || VPL == 16 ? 2 : 4)
+void route_kernel(RouteArgs a, int vec) {
   constexpr int kTokens = kWave / LANES;         // of a wavefront
   __shared__ __attribute__((aligned(16))) float s_key[kWavesPerBlock][kTokens][LANES * VPL];
   constexpr bool kThreshold = by_threshold(VPL);
@@ -464,20 +477,26 @@ __global__ __launch_bounds__(kBlock, GROUPS == kAnyGroups || VPL == 16 ? 2 : 4) 
   const int sub = lane & (LANES - 1), tok = lane / LANES;
   for (int64_t t0 = ((int64_t)blockIdx.x * kWavesPerBlock + wave) * kTokens; t0 < a.tokens;
        t0 += (int64_t)gridDim.x * kWavesPerBlock * kTokens)
-    route_token<LANES, VPL, KEYS, GROUPS>(a, vec, t0 + tok, sub, tok, s_key[wave][tok],
-                                           &s_candidates[kThreshold ? wave : 0][kThreshold ? tok : 0]);
+    route_token<LANES, VPL, KEYS, GROUPS>(
+        a, vec, t0 + tok, sub, tok, s_key[wave][tok],
+        &s_candidates[kThreshold ? wave : 0][kThreshold ? tok : 0]);
 }
 
-// The dense part of a softmax's gradient reaches every expert, the others only
-// the chosen ones; either way a token's row is put together in LDS (one
-// value per slot) and written whole.
 // Expert of a lane's i-th value in the gradient: fours of neighbours, dealt
-// to the lanes in turn, so that 16 lanes read and write 64 neighbours at once.
+// to the lanes in turn, so that 16 lanes read and write 64 neighbours at once (with
+// a lane's values all neighbours, inputs in the cache: 16384 x 256 float32 9.1 us, so 5.8;
+// 32768 x 128 bf16 7.2, so 5.8).
 template <int LANES, int VPL>
 __device__ __forceinline__ int dealt(int sub, int i) {
   return VPL >= 4 ? (i / 4 * LANES + sub) * 4 + (i & 3) : sub * VPL + i;
 }
 
+// With g = scale grad_w and q the weights before scale:
+//   softmax as it is (DENSE)   dx_e = p_e (g_e - sum_j g_j q_j), g_e 0 off the slots
+//   softmax, renormalised      dx_e = q_e (g_e - sum_j g_j q_j) at the slots
+//   sigmoid s                  dx_e = q_e (1 - s_e) g_e, renormalised (g_e - sum_j g_j q_j)
+//                              in place of g_e
+// A token's row is put together in LDS (one value per slot) and written whole.
 template <int LANES, int VPL, bool DENSE>
 __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int vec, int64_t t,
                                                      int sub, float* row) {
@@ -600,7 +619,7 @@ bool vector_rows(const void* p, const void* q, int64_t pitch, int E, int vpl, in
 }
 
 template <typename F>
-hipError_t by_width(int E, int k, int groups, int64_t tokens, F&& launch) {
+hipError_t by_width(int E, int k, int groups, F&& launch) {
   // 16 lanes per token (four tokens per wavefront) up to 256 experts where
   // slots and groups fit them, else the whole wavefront
   if (E <= 256 && k <= 16 && groups <= 16) {
@@ -626,7 +645,7 @@ unsigned route_blocks(int64_t tokens, int lanes) {
 }  // namespace
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t stream) {
-  return by_width(a.E, a.k, a.groups, a.tokens, [&](auto lanes, auto vpl) {
+  return by_width(a.E, a.k, a.groups, [&](auto lanes, auto vpl) {
     const int vec = vector_rows(a.logits, nullptr, a.pitch, a.E, vpl.value, a.f32);
     const dim3 grid(route_blocks(a.tokens, lanes.value));
     const auto run = [&](auto keys, auto groups) {
@@ -651,7 +670,7 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_route_backward(const RouteGradArgs& a, hipStream_t stream) {
-  return by_width(a.E, a.k, 1, a.tokens, [&](auto lanes, auto vpl) {
+  return by_width(a.E, a.k, 1, [&](auto lanes, auto vpl) {
     const int vec = vpl.value >= 4 &&
                     vector_rows(a.logits, a.grad_logits, a.pitch, a.E, 4, a.f32);
     const dim3 grid(route_blocks(a.tokens, lanes.value));
