@@ -2,8 +2,9 @@
 //   v[r,n] = (sum_k a[r,k] w[e,n,k]) a_scale[r] w_scale[e,n], y = bf16(v), or with
 //   swiglu y[r,i] = bf16(silu(v[r,i]) v[r,N/2+i]).
 // int32 sums by matrix instructions, exact in any order, scaled and rounded to
-// bf16 once.  Two kernels: tiles of 256 x 256 where arithmetic bounds the call,
-// 64 rows or fewer x 128 channels or fewer where reading the weights does.
+// bf16 once.  Two kernels: tiles of 256 or 128 rows x 256 channels where
+// arithmetic bounds the call, 64 rows or fewer x 128 channels or fewer where reading
+// the weights does.
 // Windows are on the GPU, so a launch covers every tile that they can have;
 // workgroups find theirs by a scan of the counts.
 
@@ -134,10 +135,14 @@ __device__ __forceinline__ void meet() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Tiles of 256 rows x 256 channels through LDS: eight wavefronts, each 128 rows
-// x 64 channels; pieces of 128 of the depth go from memory into LDS by the
-// loads themselves, one piece ahead of the matrix instructions.  A wavefront reads
-// 12 fragments for 32 matrix instructions of 16 x 16 x 64, half a stage ahead.
+// Tiles of 256 or 128 rows x 256 channels through LDS: eight wavefronts, each half
+// the rows x 64 channels; stages of 128 of the depth go from memory into LDS by
+// the loads themselves, one stage ahead of the matrix instructions, two with 128 rows.
+// A wavefront of 128 rows reads 12 fragments for 32 matrix instructions of 16 x 16 x
+// 64, half a stage ahead.  Tiles of 128 rows are for calls that make few of 256: a tile
+// alone waits for memory 1.6 us a stage with 256 rows and one stage ahead, 1.05 us with
+// 128 and two (4096 rows, 32 experts, 7168 x 4096 with swiglu 275 and 209 us; with one
+// stage ahead 128 rows took 259).
 //
 // Bound by the matrix instructions, which are busy about two thirds of the cycles
 // at the clock that the card's power leaves them (operands of zeros run 8% faster).
@@ -148,8 +153,18 @@ __device__ __forceinline__ void meet() {
 // touching the lines of later stages beforehand +2 to 10%.
 constexpr int kTile = 256;
 constexpr int kTileThreads = 512;
-constexpr int kTileBytes = kTile * kDepth;
-constexpr int kStageBytes = 2 * kTileBytes;
+
+// LDS of the kernel of tiles of HEIGHT rows: stages of rows and weights, the scales
+// of this tile and the next, and the windows.
+template <int HEIGHT>
+struct TileLds {
+  static constexpr int kStages = HEIGHT == 256 ? 2 : 3;
+  static constexpr int kRowBytes = HEIGHT * kDepth, kStageBytes = kRowBytes + kTile * kDepth;
+  static constexpr int kScaleAt = kStages * kStageBytes;
+  static constexpr int kWindowAt = kScaleAt + 2 * 2 * kTile * 4;
+  static constexpr int kBytes = kWindowAt + 3 * MOE_MAX_EXPERTS * 4;
+  static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
+};
 
 // Instruction classes of the scheduler's groups.
 constexpr int kIssueMatrix = 0x008, kIssueLdsRead = 0x100;
@@ -176,7 +191,9 @@ __device__ __forceinline__ int channel_of(int r, bool swiglu) {
 }
 
 // What a wavefront loads of a tile.
+template <int HEIGHT>
 struct TileLoads {
+  using Lds = TileLds<HEIGHT>;
   Rsrc ra, rw;
   uint32_t ao, wo;             // of instruction 0
   int a_step, w_step;          // from one instruction to the next
@@ -204,7 +221,7 @@ struct TileLoads {
 
   // A stage into LDS; past the depth and past the tile's rows and channels:
   // zeros.  ROW_LOADS: as many 64 rows as the tile multiplies.
-  template <int ROW_LOADS>
+  template <int ROW_LOADS = HEIGHT / 64>
   __device__ __forceinline__ void stage(int k0, uint32_t buf) const {
     const bool in = k0 + chunk * 16 < K;
 #pragma unroll
@@ -213,7 +230,7 @@ struct TileLoads {
         load_to_lds(ra, in ? ao + (k0 + j * a_step) : kOutside,
                     (lds_u8*)(s_tile + buf + (j * 8 + wave) * 1024));
       load_to_lds(rw, in ? wo + (k0 + j * w_step) : kOutside,
-                  (lds_u8*)(s_tile + buf + kTileBytes + (j * 8 + wave) * 1024));
+                  (lds_u8*)(s_tile + buf + Lds::kRowBytes + (j * 8 + wave) * 1024));
     }
   }
 };
@@ -228,29 +245,26 @@ __device__ __forceinline__ float tile_scale(const MatmulArgs& a, const Tile& t, 
   return c < out ? a.w_scales[(int64_t)t.expert * a.N + c + (up ? out : 0)] : 0.0f;
 }
 
-// LDS of the tile kernel: two stages of rows and weights, the scales of this tile and
-// the next, and the windows.
-constexpr int kScaleAt = 2 * kStageBytes, kWindowAt = kScaleAt + 2 * 2 * kTile * 4;
-constexpr int kTileLds = kWindowAt + 3 * MOE_MAX_EXPERTS * 4;
-
 // One tile whose wavefronts take MT x 16 rows each: 8 for a full tile, 4 or 2
 // for the last rows of a window (as long as reading the weights, but half or
-// a quarter of the products).  Its first two stages have been asked for; those
-// of `next` are before its own outputs are computed and stored.
-template <int MT>
+// a quarter of the products).  Its first stages have been asked for; those of
+// `next` are before its own outputs are computed and stored.
+template <int HEIGHT, int MT>
 __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t, const Tile& next,
                                               int tid, uint8_t* s_tile, int slot, float& scale) {
+  using Lds = TileLds<HEIGHT>;
   constexpr int NT = 4;
-  float* s_scale = reinterpret_cast<float*>(s_tile + kScaleAt) + slot * 2 * kTile;
+  constexpr int kLoads = MT / 2 + 4;                   // of a wavefront and stage
+  float* s_scale = reinterpret_cast<float*>(s_tile + Lds::kScaleAt) + slot * 2 * kTile;
   const int lane = tid & (kWave - 1), wave = uniform(tid / kWave);
-  const TileLoads loads(a, t, tid, s_tile);
+  const TileLoads<HEIGHT> loads(a, t, tid, s_tile);
   s_scale[tid] = scale;
 
   const int wm = wave / 4, wn = wave % 4;              // 2 x 4 wavefronts
   const int row = lane & 15, quarter = lane / 16;
   const uint32_t place = row * kDepth + ((quarter ^ (row & 7)) * 16);
   const uint32_t at_a = wm * (MT * 16 * kDepth) + place;
-  const uint32_t at_w = kTileBytes + wn * (64 * kDepth) + place;
+  const uint32_t at_w = Lds::kRowBytes + wn * (64 * kDepth) + place;
   i32x4 acc[MT][NT] = {};
 
   i32x4 av[2][MT], wv[2][NT];
@@ -270,21 +284,22 @@ __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t
         acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[h][j], av[h][i], acc[i][j], 0, 0, 0);
   };
 
-  // Stage s is in LDS half s % 2.  Within a turn the wavefronts meet once: by
+  // Stage s is in LDS at s % kStages.  Within a turn the wavefronts meet once: by
   // then each has read the last of stage s into registers, and its loads of
-  // stage s + 1, asked for a turn ago, have arrived.  Half of the matrix
+  // stage s + 1, asked for kStages - 1 turns ago, have arrived.  Half of the matrix
   // instructions of a register set stand on either side of the barrier.
-  meet<0>();                                           // the first two stages are there
+  meet<0>();                                           // the first stages are there
   uint32_t buf = 0;
   read(0, 0);
   for (int k0 = 0; k0 < a.K; k0 += kDepth) {
     read(1, buf);
     multiply(0, 0, MT / 2);
     interleave<kIssueLdsRead, MT + NT, 1>();
-    meet<0>();
-    loads.stage<MT / 2>(k0 + 2 * kDepth, buf);
+    meet<(Lds::kStages - 2) * kLoads>();
+    loads.template stage<MT / 2>(k0 + Lds::kStages * kDepth, buf);
     multiply(0, MT / 2, MT);
-    buf ^= kStageBytes;
+    if constexpr (Lds::kStages == 2) buf ^= Lds::kStageBytes;
+    else buf = buf + Lds::kStageBytes == Lds::kScaleAt ? 0 : buf + Lds::kStageBytes;
     __builtin_amdgcn_sched_barrier(0);
     read(0, buf);
     multiply(1, 0, MT);
@@ -297,9 +312,9 @@ __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t
 
   if (next.rows) {
     scale = tile_scale(a, next, tid);
-    const TileLoads first(a, next, tid, s_tile);
-    first.stage<4>(0, 0);
-    first.stage<4>(kDepth, kStageBytes);
+    const TileLoads<HEIGHT> first(a, next, tid, s_tile);
+#pragma unroll
+    for (int n = 0; n < Lds::kStages; ++n) first.stage(n * kDepth, n * Lds::kStageBytes);
   }
 
   typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -344,10 +359,12 @@ __device__ __forceinline__ void multiply_tile(const MatmulArgs& a, const Tile& t
 // A workgroup to each compute unit takes the tiles blockIdx.x, + 256, ... of
 // an order in which the 32 tiles that an XCD's compute units hold together are
 // neighbours.
+template <int HEIGHT>
 __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
-  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[kTileLds];
-  int* s_end = reinterpret_cast<int*>(s_tile + kWindowAt);   // row tiles up to and with a window
+  using Lds = TileLds<HEIGHT>;
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[Lds::kBytes];
+  int* s_end = reinterpret_cast<int*>(s_tile + Lds::kWindowAt);  // row tiles to a window's end
   int* s_start = s_end + MOE_MAX_EXPERTS;
   int* s_rows = s_start + MOE_MAX_EXPERTS;
   const int lane = threadIdx.x & (kWave - 1);
@@ -358,7 +375,7 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
       int s = 0, m = (int)a.rows;
       if (a.offset) window_of(a, e0 + lane < a.E ? e0 + lane : a.E - 1, first, s, m);
       if (e0 + lane >= a.E) m = 0;
-      const int end = before + scan_add((m + kTile - 1) / kTile);
+      const int end = before + scan_add((m + HEIGHT - 1) / HEIGHT);
       s_end[e0 + lane] = end;                          // E is at most 16 times 64
       s_start[e0 + lane] = s;
       s_rows[e0 + lane] = m;
@@ -373,8 +390,8 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
       if (!hit) continue;
       const int e = e0 + __builtin_ctzll(hit);
       const int before = e ? uniform(s_end[e - 1]) : 0;
-      return tile_of(e, uniform(s_start[e]), uniform(s_rows[e]), id - before * pieces, kTile, pieces,
-                     group);
+      return tile_of(e, uniform(s_start[e]), uniform(s_rows[e]), id - before * pieces, HEIGHT,
+                     pieces, group);
     }
     return {0, 0, 0, 0};
   };
@@ -384,18 +401,19 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
   int tid = threadIdx.x;
   float scale = tile_scale(a, t, tid);
   {
-    const TileLoads first(a, t, tid, s_tile);
-    first.stage<4>(0, 0);
-    first.stage<4>(kDepth, kStageBytes);
+    const TileLoads<HEIGHT> first(a, t, tid, s_tile);
+#pragma unroll
+    for (int n = 0; n < Lds::kStages; ++n) first.stage(n * kDepth, n * Lds::kStageBytes);
   }
   for (int n = 1;; ++n) {
     const Tile next = tile_at(n);
     // what follows from the thread's number is worked out anew for each tile:
     // kept over the loop it would not fit the registers
     asm volatile("" : "+v"(tid));
-    if (t.rows > 128) multiply_tile<8>(a, t, next, tid, s_tile, n & 1, scale);
-    else if (t.rows > 64) multiply_tile<4>(a, t, next, tid, s_tile, n & 1, scale);
-    else multiply_tile<2>(a, t, next, tid, s_tile, n & 1, scale);
+    if (HEIGHT > 128 && t.rows > 128)
+      multiply_tile<HEIGHT, HEIGHT / 32>(a, t, next, tid, s_tile, n & 1, scale);
+    else if (t.rows > 64) multiply_tile<HEIGHT, 4>(a, t, next, tid, s_tile, n & 1, scale);
+    else multiply_tile<HEIGHT, 2>(a, t, next, tid, s_tile, n & 1, scale);
     if (next.rows == 0) return;
     t = next;
   }
@@ -537,30 +555,65 @@ int64_t row_tiles(const MatmulArgs& a, int size) {
   return a.rows / size + (a.rows < a.E ? a.rows : a.E);
 }
 
-// Microseconds that the two kernels take if the rows are spread evenly, from
-// their times on MI355X: a tile takes 1.6 a stage and 9 beside, on one of 256
-// compute units; 64 rows x 128 channels of the stream kernel 1.15 a stage and 3
-// beside, two at once on a compute unit (alone there 0.72).  Measured, tile /
-// stream, and by these rules:
-//   2048 rows, 32 experts, 7168 x 4096   187 / 201   (198 / 201)
-//   1536 rows                            182 / 163   (198 / 167)
-//   2048 rows, one expert, 4096 x 4096    61 / 73     (60 / 80)
-//   1024 rows                             58 / 36     (60 / 40)
-//   16384 rows, 64 experts, 1024 x 512    25 / 26     (22 / 27)
-//   8192 rows                             22 / 18     (22 / 15)
-double window_tiles(const MatmulArgs& a, int size) {
+// Row tiles of `size` if the rows are spread about evenly.
+double even_tiles(const MatmulArgs& a, int size) {
   const double windows = (double)(a.rows < a.E ? a.rows : a.E), n = (double)a.rows / windows / size;
-  return windows * (a.E == 1 ? __builtin_ceil(n) : n > 0.5 ? n + 0.5 : 1.0);
+  return windows * (a.E == 1 ? __builtin_ceil(n) : n > 0.8 ? n + 0.5 : 1.0);
 }
-double tile_time(const MatmulArgs& a, int pieces) {
-  const double rounds = window_tiles(a, kTile) * pieces / 256.0;
-  return (rounds < 1.0 ? 1.0 : rounds) * (9.0 + 1.6 * ((a.K + kDepth - 1) / kDepth));
+
+// One way to compute a call, and what its workgroups took on MI355X: `start`
+// microseconds beside the stages, a stage `alone` on a compute unit or `shared`
+// with a second workgroup, and the rate of the weights from memory.
+struct Way {
+  int rows, channels, depth;                           // of a workgroup; depth of a stage
+  int resident;                                        // workgroups on the GPU at once
+  double start, alone, shared;                         // us
+  double rate;                                         // bytes / us
+};
+enum WayName { kTile256, kTile128, kWide, kHalf, kHalfTwo, kNarrow, kFewRows, kOneRow, kWays };
+constexpr Way kWay[kWays] = {
+    {256, 256, 128, 256, 9.0, 1.60, 1.60, 4.85e6},     // matmul_tile_kernel<256>
+    {128, 256, 128, 256, 6.0, 1.05, 1.05, 4.85e6},     // matmul_tile_kernel<128>
+    {64, 128, 128, 512, 3.0, 0.72, 1.15, 5.9e6},       // matmul_stream_kernel<64, 8, 1, 3>
+    {64, 64, 256, 256, 3.0, 0.65, 0.65, 4.5e6},        // <64, 4, 2, 3>
+    {64, 64, 256, 512, 3.0, 0.95, 1.00, 4.5e6},        // <64, 4, 2, 2>
+    {64, 32, 512, 256, 3.0, 0.68, 0.68, 4.5e6},        // <64, 2, 4, 3>
+    {16, 32, 512, 512, 3.0, 0.65, 0.80, 4.5e6},        // <16, 2, 4, 3>
+    {16, 16, 1024, 512, 3.0, 0.80, 1.00, 4.5e6},       // <16, 1, 8, 2>
+};
+
+// Microseconds of a call: its rounds of workgroups, the last one counted for the
+// larger part also where it is not full, and the reading of the weights, which partly
+// hides behind them.  Measured where two ways are near each other, us:
+//   rows, experts, K x N                   256   128    64 x 128  64 x 64 (three, two stages)
+//   13483, 3, 5952 x 4752, swiglu          357   402    858       946   881
+//   2048, 1, 4096 x 4096                    58    37     76        94    66
+//   4096, 32, 7168 x 4096, swiglu          275   212    316       389   359
+//   4662, 96, 2064 x 1416                  105    88     84       100    95
+//   512, 1, 4096 x 4096                     46    35     24        26    19
+//   256, 1, 4096 x 4096                     42    29     23        15    17
+// and of few rows             64 x 128  64 x 64  64 x 32  16 x 32  16 x 16
+//   64, 1, 7168 x 4096               28       17       13       16       18
+//   64, 8, 2048 x 1024               11      8.6      7.3      5.6      6.2
+//   1, 1, 7168 x 4096                26       16        -       12        9
+double way_time(const MatmulArgs& a, const Way& w) {
+  const int out = a.swiglu ? a.N / 2 : a.N, per = a.swiglu ? w.channels / 2 : w.channels;
+  const double groups = even_tiles(a, w.rows) * ((out + per - 1) / per);
+  const double full = groups / w.resident;
+  const double rounds = full < 1.0 ? 1.0 : full + 0.75 * (__builtin_ceil(full) - full);
+  const int stages = (a.K + w.depth - 1) / w.depth;
+  const double work = rounds * (w.start + stages * (groups <= 256.0 ? w.alone : w.shared));
+  const double read = (double)(a.rows < a.E ? a.rows : a.E) * a.N * a.K / w.rate;
+  return __builtin_sqrt(work * work + read * read);
 }
-double stream_time(const MatmulArgs& a, int pieces) {
-  const double stages = (a.K + kDepth - 1) / kDepth;
-  const double groups = window_tiles(a, 64) * 2.0 * pieces;
-  return groups <= 256.0 ? 3.0 + 0.72 * stages
-                         : (groups < 512.0 ? 1.0 : groups / 512.0) * (3.0 + 1.15 * stages);
+
+template <int HEIGHT>
+hipError_t launch_tile(const MatmulArgs& a, int out, int group, hipStream_t stream) {
+  const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
+  if (row_tiles(a, HEIGHT) * pieces >= INT32_MAX - 256) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((matmul_tile_kernel<HEIGHT>), dim3(256), dim3(kTileThreads), 0, stream, a,
+                     pieces, group);
+  return hipGetLastError();
 }
 
 template <int ROWS, int WC, int WK, int STAGES>
@@ -578,30 +631,28 @@ hipError_t launch_stream(const MatmulArgs& a, int out, hipStream_t stream) {
 
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
   const int out = a.swiglu ? a.N / 2 : a.N;
-  const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
-  const int64_t tiles = row_tiles(a, kTile) * pieces;
-  if (tile_time(a, pieces) < stream_time(a, pieces) && tiles < INT32_MAX - 256) {
+  int best = kTile256;
+  double least = way_time(a, kWay[best]);
+  for (int n = best + 1; n < kWays; ++n) {
+    const double t = way_time(a, kWay[n]);
+    if (t < least) {
+      least = t;
+      best = n;
+    }
+  }
+  switch (best) {
     // six row tiles together: of 2, 4, 5, 6 and 8 the best or near it (32768 x
     // 2048 x 7168 over 32 experts 528 / 522 / 512 / 510 / 509 us, 16384 x 8192 x 8192
-    // 846 / 832 / 815 / 811 / 835)
-    hipLaunchKernelGGL(matmul_tile_kernel, dim3(256), dim3(kTileThreads), 0, stream, a, pieces, 6);
-    return hipGetLastError();
+    // 846 / 832 / 815 / 811 / 835); of 128 rows six or twelve make no difference
+    case kTile256: return launch_tile<256>(a, out, 6, stream);
+    case kTile128: return launch_tile<128>(a, out, 6, stream);
+    case kWide: return launch_stream<64, 8, 1, 3>(a, out, stream);
+    case kHalf: return launch_stream<64, 4, 2, 3>(a, out, stream);
+    case kHalfTwo: return launch_stream<64, 4, 2, 2>(a, out, stream);
+    case kNarrow: return launch_stream<64, 2, 4, 3>(a, out, stream);
+    case kFewRows: return launch_stream<16, 2, 4, 3>(a, out, stream);
+    default: return launch_stream<16, 1, 8, 2>(a, out, stream);
   }
-  // Few rows: 128 channels to a workgroup where that gives every compute unit
-  // one (windows that can have rows are counted), else fewer channels and
-  // more of the depth at once.  With at most 16 rows in all a stage needs room
-  // for no more.  4096 x 7168, us at 128 / 64 / 32 / 16 channels: one expert, 1 row
-  // 26 / 16 / 12 / 9, 64 rows 29 / 19 / 14 / -; 32 experts, 512 rows 159 / 158 / 208 / 258.
-  const int64_t windows = (a.rows < a.E ? a.rows : a.E) + a.rows / 64;
-  const auto groups = [&](int tiles) {
-    const int c = tiles * (a.swiglu ? 8 : 16);
-    return windows * ((out + c - 1) / c);
-  };
-  if (groups(8) >= 256) return launch_stream<64, 8, 1, 3>(a, out, stream);
-  if (groups(4) >= 256) return launch_stream<32, 4, 2, 3>(a, out, stream);
-  if (a.rows > 16) return launch_stream<64, 2, 4, 3>(a, out, stream);
-  if (groups(2) >= 256) return launch_stream<16, 2, 4, 3>(a, out, stream);
-  return launch_stream<16, 1, 8, 2>(a, out, stream);
 }
 
 }  // namespace moe

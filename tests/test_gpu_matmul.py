@@ -144,6 +144,23 @@ def test_many_tiles(counts, N, K, swiglu):
     if E > 1:
         assert torch.equal(_run(*t, offset, None, swiglu), y)
 
+# Sizes in between, each of which another kernel or size of tile takes: 128 rows,
+# 64 rows x 128 channels, 64 x 64 with two stages, 64 x 32.
+@pytest.mark.parametrize("counts,N,K", [([4161], 1040, 2064),
+                                        ([129, 0, 64, 1, 127, 128, 65, 190] * 5, 1056, 528),
+                                        ([1000], 4112, 528),
+                                        ([63, 64, 65, 1, 0, 129] * 4, 2064, 1040),
+                                        ([30] * 50, 2064, 400),
+                                        ([230, 400, 70], 1424, 2064), ([512], 4112, 1552),
+                                        ([139, 1], 1040, 2064), ([65, 17, 98], 1040, 2064)])
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_tiles_in_between(counts, N, K, swiglu):
+    E, rows = len(counts), sum(counts)
+    N -= 0 if swiglu else 8
+    offset, windows = _packed(counts)
+    t = _inputs(rows, E, N, K, seed=rows)
+    _check(_run(*t, offset, counts, swiglu), *t, windows, swiglu)
+
 
 @pytest.mark.parametrize("swiglu", [False, True])
 def test_many_tiles_fixed_windows(swiglu):
