@@ -141,16 +141,17 @@ __device__ __forceinline__ void meet() {
 // A wavefront of 128 rows reads 12 fragments for 32 matrix instructions of 16 x 16 x
 // 64, half a stage ahead.  Tiles of 128 rows are for calls that make few of 256: a tile
 // alone waits for memory 1.6 us a stage with 256 rows and one stage ahead, 1.05 us with
-// 128 and two (4096 rows, 32 experts, 7168 x 4096 with swiglu 275 and 209 us; with one
+// 128 and two (4096 rows, 32 experts, 7168 x 4096 with swiglu 275 and 207 us; with one
 // stage ahead 128 rows took 259).
 //
 // Bound by the matrix instructions, which are busy about two thirds of the cycles
 // at the clock that the card's power leaves them (operands of zeros run 8% faster).
-// 32768 rows, 16 experts, 7168 x 4096 with swiglu: 805 us, 2390 TOP/s; 16384 x 8192 x
-// 8192: 807 us, 2725 TOP/s; 32 experts of 980 to 1080 rows, 7168 x 4096: 835 us.  Beside
-// it 32 x 32 x 32 instructions 1012 us (16 x 16 x 64 then: 934), stages of half the
-// depth with the wavefronts in two phases 920 (850), a second barrier +4%,
-// touching the lines of later stages beforehand +2 to 10%.
+// 32768 rows, 16 experts, 7168 x 4096 with swiglu: 805 to 847 us by card, 2270 to
+// 2390 TOP/s; 16384 x 8192 x 8192: 807 to 842 us, 2610 to 2725 TOP/s; 32 experts of 980
+// to 1080 rows, 7168 x 4096: 835 us.  Beside it 32 x 32 x 32 instructions 1012 us (16 x
+// 16 x 64 then: 934), stages of half the depth with the wavefronts in two phases
+// 920 (850), a second barrier +4%, touching the lines of later stages beforehand +2
+// to 10%.
 constexpr int kTile = 256;
 constexpr int kTileThreads = 512;
 

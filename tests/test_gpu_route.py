@@ -114,6 +114,25 @@ def test_route_groups(T, E, k, groups, top, score, bias, two):
     _check(x, idx, w, k, bias=b, **opt)
 
 
+@pytest.mark.parametrize("T,E,k,groups,top", [(13, 512, 8, 4, 2), (10, 384, 8, 8, 4), (9, 1000, 20, 8, 3),
+                                              (7, 1024, 8, 32, 8), (8, 300, 6, 3, 2), (6, 340, 4, 17, 5),
+                                              (5, 20, 20, 2, 2), (9, 264, 5, 24, 4)])
+@pytest.mark.parametrize("score,bias,two", [(0, False, 1), (1, True, 2), (0, True, 2)])
+def test_groups_of_a_whole_wavefront(T, E, k, groups, top, score, bias, two):
+    """More than 256 experts or 16 slots: several lanes look over a group; some groups
+    and experts masked."""
+    x = _draw(T, E, True, seed=E + groups)
+    x[0, : E // groups] = -math.inf
+    x[1, ::3] = -math.inf
+    x[2] = -math.inf
+    x[2, E - 1] = 0.5
+    b = _draw(1, E, True, seed=3, spread=0.1)[0] if bias else None
+    opt = dict(score=score, groups=groups, top_groups=top, group_top=two)
+    idx, w = _route(x, k, bias=b, **opt)
+    _check(x, idx, w, k, bias=b, **opt)
+    assert idx[2].tolist() == [E - 1] + [-1] * (k - 1)
+
+
 @pytest.mark.parametrize("E,k", [(16, 4), (100, 8), (256, 8), (700, 20)])
 @pytest.mark.parametrize("score,renorm", [(0, True), (0, False), (1, True), (1, False)])
 @pytest.mark.parametrize("groups", [1, 4])
