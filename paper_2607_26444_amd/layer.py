@@ -18,6 +18,7 @@ python -m paper_2607_26444_amd.layer [--tokens N ...] runs it on random inputs.
 from __future__ import annotations
 
 import argparse
+import contextlib
 import sys
 
 import torch
@@ -81,7 +82,9 @@ class MoeLayer:
         """x, residual [T,H] bf16 -> y [T,H] bf16, the layer's addition to the
         residual stream, which is left in `sum` (x + residual).  logits [T,E]
         float32 or bf16: a tensor, or a function of the normed rows [T,H] that
-        makes it (the gate's product).  token_mask [T] uint8: 0 for padding."""
+        makes it (the gate's product; its work goes to `stream` as well).
+        token_mask [T] uint8: 0 for padding.  What is passed in has to be ready on
+        `stream` and to stay until it has been read there."""
         T, H, I, E = self.T, self.H, self.I, self.E
         for name, t in (("x", x), ("residual", residual)):
             if tuple(t.shape) != (T, H) or t.dtype != torch.bfloat16 or not t.is_contiguous():
@@ -92,7 +95,8 @@ class MoeLayer:
                         moe.MOE_DTYPE_INT8, self.q, self.q_scale, None, self.q_scale.shape[1],
                         stream)
         if callable(logits):
-            logits = logits(self.normed)
+            with _current(stream):
+                logits = logits(self.normed)
         if tuple(logits.shape) != (T, E) or logits.stride(1) != 1:
             raise ValueError(f"logits: rows of {E} neighbouring values for {T} tokens are needed")
         if token_mask is not None and (tuple(token_mask.shape) != (T,) or
@@ -115,6 +119,17 @@ class MoeLayer:
         moe.moe_combine(self.out_table, self.topk_w, H, E, 1, self.topk_idx, lay.pos,
                         lay.rank_offset, self.cap, self.y, lay.workspace, lay.status, stream)
         return self.y
+
+
+def _current(stream):
+    """Makes the stream that the calls are given torch's current one: what a
+    function of the caller enqueues then lies between the calls, and what it
+    allocates is not handed out again before the stream has read it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    return torch.cuda.stream(stream)
 
 
 def _dtype(t):

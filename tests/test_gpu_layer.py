@@ -154,3 +154,31 @@ def test_refused_arguments():
     with pytest.raises(ValueError):
         mod.MoeLayer(8, 256, 64, 4, 2, layer.norm_weight, layer.w13, layer.w13_scale,
                      layer.w2[:2], layer.w2_scale)
+
+
+def test_gate_as_a_function_on_a_stream_of_its_own():
+    """Behind work that takes milliseconds: a gate that ran beside the stream would read
+    the rows of the batch before, and its logits' memory would be given to the tensors
+    that the current stream fills meanwhile."""
+    from paper_2607_26444_amd.layer import random_layer
+    T, H, E = 200, 512, 8
+    layer = random_layer(T, H, 128, E, 2)
+    gate = torch.randn(H, E, device="cuda").bfloat16() / 16
+    x, r, _ = _inputs(T, H, E, seed=6)
+    want = layer.forward(x, r, lambda normed: normed @ gate).clone()
+    chosen = layer.topk_idx.clone()
+    layer.forward(*_inputs(T, H, E, seed=7)[:2], lambda normed: normed @ gate)
+    layer.topk_idx.fill_(-1)
+    slow = torch.randn(8192, 8192, device="cuda").bfloat16()
+    s = torch.cuda.Stream()
+    out = torch.empty_like(slow)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for _ in range(10):
+            torch.mm(slow, slow, out=out)
+    y = layer.forward(x, r, lambda normed: normed @ gate, stream=s)
+    assert torch.cuda.current_stream() != s
+    junk = [torch.full((T, E), 50.0 + n, dtype=torch.bfloat16, device="cuda") for n in range(64)]
+    s.synchronize()
+    assert torch.equal(layer.topk_idx, chosen) and torch.equal(y, want)
+    assert len(junk) == 64

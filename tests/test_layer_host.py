@@ -1,0 +1,98 @@
+"""MoeLayer's own decisions without a GPU: which stream its work is given to and
+which tensors it takes.  The library's calls are recorded instead of made, so
+tensors on the CPU stand in for the device's."""
+import inspect
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2607_26444_amd import layer as mod  # noqa: E402
+from paper_2607_26444_amd import moe  # noqa: E402
+
+CALLS = ("moe_rmsnorm", "moe_route", "moe_layout", "moe_dispatch", "moe_expert_matmul",
+         "moe_quantize", "moe_combine")
+T, H, I, E, K = 6, 256, 32, 8, 2
+
+
+class Stream:
+    """A stream of another library: an address, as the binding takes it."""
+    cuda_stream = 0x7F00DEADB000
+
+
+class Record(list):
+    """(name, arguments by name, torch's current stream) of every call."""
+    current = None
+
+    def names(self):
+        return [name for name, _, _ in self]
+
+    def arguments(self, name):
+        return next(args for n, args, _ in self if n == name)
+
+
+@pytest.fixture
+def record(monkeypatch):
+    calls = Record()
+
+    def stand_in(name):
+        signature = inspect.signature(getattr(moe, name))
+
+        def call(*args, **kw):
+            bound = signature.bind(*args, **kw)
+            bound.apply_defaults()
+            calls.append((name, bound.arguments, calls.current))
+        return call
+
+    class Current:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            self.before, calls.current = calls.current, self.stream.cuda_stream
+
+        def __exit__(self, *_):
+            calls.current = self.before
+
+    class External:
+        def __init__(self, address, **_):
+            self.cuda_stream = address
+
+    for name in CALLS:
+        monkeypatch.setattr(moe, name, stand_in(name))
+    # host memory has not the alignment of a workspace; an empty one has
+    monkeypatch.setattr(moe, "moe_layout_workspace_bytes", lambda *_: 0)
+    monkeypatch.setattr(torch.cuda, "stream", Current)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", External)
+    return calls
+
+
+def _layer(T=T, E=E):
+    def int8(*shape):
+        return torch.ones(*shape, dtype=torch.int8)
+    return mod.MoeLayer(T, H, I, E, K, torch.ones(H), int8(E, 2 * I, H), torch.ones(E, 2 * I),
+                        int8(E, H, I), torch.ones(E, H), device="cpu")
+
+
+def _rows(T=T):
+    return [torch.zeros(T, H, dtype=torch.bfloat16) for _ in range(2)]
+
+
+@pytest.mark.parametrize("stream", [None, Stream()])
+def test_a_gate_runs_on_the_stream_of_the_calls(record, stream):
+    """The gate reads what the norm left and the routing reads what it returns:
+    torch's work has to be on the stream that both are enqueued on, after the
+    one and before the other."""
+    layer = _layer()
+
+    def gate(normed):
+        assert normed is layer.normed
+        record.append(("gate", {}, record.current))
+        return torch.zeros(T, E)
+    layer.forward(*_rows(), gate, stream=stream)
+    names = record.names()
+    assert names.index("moe_rmsnorm") < names.index("gate") < names.index("moe_route")
+    assert all(args["stream"] is stream for name, args, _ in record if name != "gate")
+    want = None if stream is None else stream.cuda_stream
+    assert [on for name, _, on in record if name == "gate"] == [want]
+    assert record.current is None              # the caller's stream is current again
