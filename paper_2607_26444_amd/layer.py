@@ -97,13 +97,16 @@ class MoeLayer:
         if callable(logits):
             with _current(stream):
                 logits = logits(self.normed)
-        if tuple(logits.shape) != (T, E) or logits.stride(1) != 1:
+        # strides of single rows and columns say nothing; a pitch under E would be
+        # rows that lie on each other (0, an expanded row, means packed to the call)
+        pitch = logits.stride(0) if T > 1 and logits.dim() == 2 else E
+        if tuple(logits.shape) != (T, E) or (E > 1 and logits.stride(1) != 1) or pitch < E:
             raise ValueError(f"logits: rows of {E} neighbouring values for {T} tokens are needed")
         if token_mask is not None and (tuple(token_mask.shape) != (T,) or
                                        token_mask.dtype != torch.uint8):
             raise ValueError(f"token_mask: a uint8 tensor of {T} values is needed")
         moe.moe_route(logits, _dtype(logits), E, self.bias, token_mask, self.topk_idx,
-                      self.topk_w, stream=stream, logits_pitch=logits.stride(0), **self.options)
+                      self.topk_w, stream=stream, logits_pitch=pitch, **self.options)
         lay.run(self.topk_idx, stream)
         moe.moe_dispatch(self.q, self.q_scale, moe.MOE_DTYPE_FP8_E4M3, H, E, 1, self.topk_idx,
                          lay.pos, lay.rank_offset, self.row_table, self.scale_table, self.cap,

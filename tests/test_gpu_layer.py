@@ -182,3 +182,19 @@ def test_gate_as_a_function_on_a_stream_of_its_own():
     s.synchronize()
     assert torch.equal(layer.topk_idx, chosen) and torch.equal(y, want)
     assert len(junk) == 64
+
+
+def test_logits_strides():
+    """Rows with a pitch, a transposed single row, a transposed single column."""
+    from paper_2607_26444_amd.layer import random_layer
+    for T, E, k in ((1, 8, 2), (50, 8, 2), (50, 1, 1)):
+        layer = random_layer(T, 256, 64, E, k, seed=T)
+        x, r, logits = _inputs(T, 256, E, seed=8)
+        want = layer.forward(x, r, logits).clone()
+        wide = torch.full((T, E + 5), 9.0, device="cuda")
+        wide[:, 2:2 + E] = logits
+        views = [wide[:, 2:2 + E]] + ([logits.t().contiguous().t()] if T == 1 or E == 1 else [])
+        for view in views:
+            assert torch.equal(layer.forward(x, r, view), want), (T, E, view.stride())
+    with pytest.raises(ValueError, match="logits"):
+        layer.forward(x, r, torch.zeros(1, device="cuda").expand(50, 1))

@@ -67,7 +67,7 @@ def record(monkeypatch):
     return calls
 
 
-def _layer(T=T, E=E):
+def _layer(T=T, E=E, K=K):
     def int8(*shape):
         return torch.ones(*shape, dtype=torch.int8)
     return mod.MoeLayer(T, H, I, E, K, torch.ones(H), int8(E, 2 * I, H), torch.ones(E, 2 * I),
@@ -96,3 +96,42 @@ def test_a_gate_runs_on_the_stream_of_the_calls(record, stream):
     want = None if stream is None else stream.cuda_stream
     assert [on for name, _, on in record if name == "gate"] == [want]
     assert record.current is None              # the caller's stream is current again
+
+
+def test_logits_whose_rows_lie_on_each_other(record):
+    """A row expanded to all tokens has row pitch 0, which the call takes as packed rows:
+    it would read T times the storage.  Overlapping rows have a pitch under E."""
+    layer = _layer()
+    storage = torch.zeros(T + E)
+    for logits in (storage[:E].expand(T, E), storage.as_strided((T, E), (1, 1)),
+                   storage[:1].expand(T, E), torch.zeros(E, T).t()):
+        with pytest.raises(ValueError, match="logits"):
+            layer.forward(*_rows(), logits)
+        assert "moe_route" not in record.names()
+
+
+@pytest.mark.parametrize("tokens,experts", [(1, E), (T, K), (1, K)])
+def test_logits_pitch(record, tokens, experts):
+    """The pitch is that of the rows; of one row the stride says nothing."""
+    layer = _layer(T=tokens, E=experts)
+    wide = torch.zeros(tokens, experts + 3)
+    for logits, pitch in ((torch.zeros(tokens, experts), experts), (wide[:, 2:2 + experts], experts + 3)):
+        record.clear()
+        layer.forward(*_rows(tokens), logits)
+        got = record.arguments("moe_route")["logits_pitch"]
+        assert got == pitch if tokens > 1 else got >= experts
+    if tokens == 1:
+        for logits in (torch.zeros(experts, 1).t(), torch.zeros(experts).expand(1, experts),
+                       torch.zeros(experts).as_strided((1, experts), (0, 1))):
+            record.clear()
+            layer.forward(*_rows(tokens), logits)
+            assert record.arguments("moe_route")["logits_pitch"] == experts
+
+
+def test_logits_of_one_expert(record):
+    """Of one column the stride says nothing either."""
+    layer = _layer(E=1, K=1)
+    for logits, pitch in ((torch.zeros(1, T).t(), 1), (torch.zeros(T, 5)[:, 3:4], 5)):
+        record.clear()
+        layer.forward(*_rows(), logits)
+        assert record.arguments("moe_route")["logits_pitch"] == pitch
