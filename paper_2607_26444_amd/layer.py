@@ -103,8 +103,9 @@ class MoeLayer:
         if tuple(logits.shape) != (T, E) or (E > 1 and logits.stride(1) != 1) or pitch < E:
             raise ValueError(f"logits: rows of {E} neighbouring values for {T} tokens are needed")
         if token_mask is not None and (tuple(token_mask.shape) != (T,) or
-                                       token_mask.dtype != torch.uint8):
-            raise ValueError(f"token_mask: a uint8 tensor of {T} values is needed")
+                                       token_mask.dtype != torch.uint8 or
+                                       not token_mask.is_contiguous()):
+            raise ValueError(f"token_mask: a contiguous uint8 tensor of {T} values is needed")
         moe.moe_route(logits, _dtype(logits), E, self.bias, token_mask, self.topk_idx,
                       self.topk_w, stream=stream, logits_pitch=pitch, **self.options)
         lay.run(self.topk_idx, stream)

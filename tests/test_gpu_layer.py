@@ -198,3 +198,15 @@ def test_logits_strides():
             assert torch.equal(layer.forward(x, r, view), want), (T, E, view.stride())
     with pytest.raises(ValueError, match="logits"):
         layer.forward(x, r, torch.zeros(1, device="cuda").expand(50, 1))
+
+
+def test_token_mask_strides():
+    from paper_2607_26444_amd.layer import random_layer
+    layer = random_layer(20, 256, 64, 8, 2)
+    x, r, logits = _inputs(20, 256, 8, seed=9)
+    table = (torch.arange(60, device="cuda").view(20, 3) % 4 != 0).to(torch.uint8)
+    for bad in (table[:, 1], table[0, :1].expand(20)):
+        with pytest.raises(ValueError, match="token_mask"):
+            layer.forward(x, r, logits, token_mask=bad)
+    layer.forward(x, r, logits, token_mask=table[:, 1].contiguous())
+    assert torch.equal((layer.topk_idx[:, 0] >= 0).to(torch.uint8), table[:, 1])

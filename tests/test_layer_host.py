@@ -135,3 +135,26 @@ def test_logits_of_one_expert(record):
         record.clear()
         layer.forward(*_rows(), logits)
         assert record.arguments("moe_route")["logits_pitch"] == pitch
+
+
+def test_token_mask_strides(record):
+    """The call reads T neighbouring bytes: a column of a table would give other
+    tokens' bytes, an expanded one bytes past its storage."""
+    layer = _layer()
+    table = torch.ones(T, 3, dtype=torch.uint8)
+    for mask in (table[:, 1], table[0, :1].expand(T), torch.ones(2 * T, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="token_mask"):
+            layer.forward(*_rows(), torch.zeros(T, E), token_mask=mask)
+        assert "moe_route" not in record.names()
+    good = table.t().contiguous()[1]
+    layer.forward(*_rows(), torch.zeros(T, E), token_mask=good)
+    assert record.arguments("moe_route")["token_mask"] is good
+
+
+@pytest.mark.parametrize("stride", [0, 7])
+def test_token_mask_of_one_token(record, stride):
+    """Of one token the stride says nothing."""
+    layer = _layer(T=1)
+    mask = torch.ones(9, dtype=torch.uint8).as_strided((1,), (stride,))
+    layer.forward(*_rows(1), torch.zeros(1, E), token_mask=mask)
+    assert record.arguments("moe_route")["token_mask"] is mask
