@@ -10,7 +10,7 @@
 
 #include <type_traits>
 
-#include "layer.h"
+#include "matmul_rule.h"
 
 namespace moe {
 namespace {
@@ -152,8 +152,6 @@ __device__ __forceinline__ void meet() {
 // 16 x 64 then: 934), stages of half the depth with the wavefronts in two phases
 // 920 (850), a second barrier +4%, touching the lines of later stages beforehand +2
 // to 10%.
-constexpr int kTile = 256;
-constexpr int kTileThreads = 512;
 
 // LDS of the kernel of tiles of HEIGHT rows: stages of rows and weights, the scales
 // of this tile and the next, and the windows.
@@ -545,114 +543,42 @@ void matmul_stream_kernel(MatmulArgs a, int pieces) {
   }
 }
 
-// Tiles of one launch: HIP's limit of 2^32 threads.  The outputs and weights of
-// more would not fit a GPU's memory.
-constexpr int64_t kMaxTiles = (1ll << 32) / kTileThreads - 256;
-
-// Row tiles of `size` that the windows can have: each window with rows adds at
-// most one that is not full.
-int64_t row_tiles(const MatmulArgs& a, int size) {
-  if (!a.offset) return (a.rows + size - 1) / size;
-  return a.rows / size + (a.rows < a.E ? a.rows : a.E);
-}
-
-// Row tiles of `size` if the rows are spread about evenly.
-double even_tiles(const MatmulArgs& a, int size) {
-  const double windows = (double)(a.rows < a.E ? a.rows : a.E), n = (double)a.rows / windows / size;
-  return windows * (a.E == 1 ? __builtin_ceil(n) : n > 0.8 ? n + 0.5 : 1.0);
-}
-
-// One way to compute a call, and what its workgroups took on MI355X: `start`
-// microseconds beside the stages, a stage `alone` on a compute unit or `shared`
-// with a second workgroup, and the rate of the weights from memory.
-struct Way {
-  int rows, channels, depth;                           // of a workgroup; depth of a stage
-  int resident;                                        // workgroups on the GPU at once
-  double start, alone, shared;                         // us
-  double rate;                                         // bytes / us
-};
-enum WayName { kTile256, kTile128, kWide, kHalf, kHalfTwo, kNarrow, kFewRows, kOneRow, kWays };
-constexpr Way kWay[kWays] = {
-    {256, 256, 128, 256, 9.0, 1.60, 1.60, 4.85e6},     // matmul_tile_kernel<256>
-    {128, 256, 128, 256, 6.0, 1.05, 1.05, 4.85e6},     // matmul_tile_kernel<128>
-    {64, 128, 128, 512, 3.0, 0.72, 1.15, 5.9e6},       // matmul_stream_kernel<64, 8, 1, 3>
-    {64, 64, 256, 256, 3.0, 0.65, 0.65, 4.5e6},        // <64, 4, 2, 3>
-    {64, 64, 256, 512, 3.0, 0.95, 1.00, 4.5e6},        // <64, 4, 2, 2>
-    {64, 32, 512, 256, 3.0, 0.68, 0.68, 4.5e6},        // <64, 2, 4, 3>
-    {16, 32, 512, 512, 3.0, 0.65, 0.80, 4.5e6},        // <16, 2, 4, 3>
-    {16, 16, 1024, 512, 3.0, 0.80, 1.00, 4.5e6},       // <16, 1, 8, 2>
-};
-
-// Microseconds of a call: its rounds of workgroups, the last one counted for the
-// larger part also where it is not full, and the reading of the weights, which partly
-// hides behind them.  Measured where two ways are near each other, us:
-//   rows, experts, K x N                   256   128    64 x 128  64 x 64 (three, two stages)
-//   13483, 3, 5952 x 4752, swiglu          357   402    858       946   881
-//   2048, 1, 4096 x 4096                    58    37     76        94    66
-//   4096, 32, 7168 x 4096, swiglu          275   212    316       389   359
-//   4662, 96, 2064 x 1416                  105    88     84       100    95
-//   512, 1, 4096 x 4096                     46    35     24        26    19
-//   256, 1, 4096 x 4096                     42    29     23        15    17
-// and of few rows             64 x 128  64 x 64  64 x 32  16 x 32  16 x 16
-//   64, 1, 7168 x 4096               28       17       13       16       18
-//   64, 8, 2048 x 1024               11      8.6      7.3      5.6      6.2
-//   1, 1, 7168 x 4096                26       16        -       12        9
-double way_time(const MatmulArgs& a, const Way& w) {
-  const int out = a.swiglu ? a.N / 2 : a.N, per = a.swiglu ? w.channels / 2 : w.channels;
-  const double groups = even_tiles(a, w.rows) * ((out + per - 1) / per);
-  const double full = groups / w.resident;
-  const double rounds = full < 1.0 ? 1.0 : full + 0.75 * (__builtin_ceil(full) - full);
-  const int stages = (a.K + w.depth - 1) / w.depth;
-  const double work = rounds * (w.start + stages * (groups <= 256.0 ? w.alone : w.shared));
-  const double read = (double)(a.rows < a.E ? a.rows : a.E) * a.N * a.K / w.rate;
-  return __builtin_sqrt(work * work + read * read);
-}
-
-template <int HEIGHT>
-hipError_t launch_tile(const MatmulArgs& a, int out, int group, hipStream_t stream) {
-  const int per = a.swiglu ? kTile / 2 : kTile, pieces = (out + per - 1) / per;
-  if (row_tiles(a, HEIGHT) * pieces >= INT32_MAX - 256) return hipErrorInvalidConfiguration;
+template <int HEIGHT, int WAY>
+hipError_t launch_tile(const MatmulArgs& a, int group, hipStream_t stream) {
+  constexpr Way w = kWay[WAY];
+  static_assert(w.rows == HEIGHT && w.channels == kTile, "the rule's tile");
   hipLaunchKernelGGL((matmul_tile_kernel<HEIGHT>), dim3(256), dim3(kTileThreads), 0, stream, a,
-                     pieces, group);
+                     pieces_of(a, w), group);
   return hipGetLastError();
 }
 
-template <int ROWS, int WC, int WK, int STAGES>
-hipError_t launch_stream(const MatmulArgs& a, int out, hipStream_t stream) {
-  const int per = WC * (a.swiglu ? 8 : 16), pieces = (out + per - 1) / per;
-  const int64_t tiles = row_tiles(a, ROWS) * pieces;
-  if (tiles > kMaxTiles) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((matmul_stream_kernel<ROWS, WC, WK, STAGES>),
-                     dim3((unsigned)((tiles + 255) / 256 * 256)), dim3(kTileThreads), 0, stream, a,
-                     pieces);
+template <int ROWS, int WC, int WK, int STAGES, int WAY>
+hipError_t launch_stream(const MatmulArgs& a, hipStream_t stream) {
+  constexpr Way w = kWay[WAY];
+  static_assert(w.rows == ROWS && w.channels == 16 * WC && w.depth == kDepth * WK,
+                "the rule's tile");
+  const int64_t groups = (tiles_of(a, w) + 255) / 256 * 256;
+  hipLaunchKernelGGL((matmul_stream_kernel<ROWS, WC, WK, STAGES>), dim3((unsigned)groups),
+                     dim3(kTileThreads), 0, stream, a, pieces_of(a, w));
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream) {
-  const int out = a.swiglu ? a.N / 2 : a.N;
-  int best = kTile256;
-  double least = way_time(a, kWay[best]);
-  for (int n = best + 1; n < kWays; ++n) {
-    const double t = way_time(a, kWay[n]);
-    if (t < least) {
-      least = t;
-      best = n;
-    }
-  }
-  switch (best) {
+  switch (choose_way(a)) {
     // six row tiles together: of 2, 4, 5, 6 and 8 the best or near it (32768 x
     // 2048 x 7168 over 32 experts 528 / 522 / 512 / 510 / 509 us, 16384 x 8192 x 8192
     // 846 / 832 / 815 / 811 / 835); of 128 rows six or twelve make no difference
-    case kTile256: return launch_tile<256>(a, out, 6, stream);
-    case kTile128: return launch_tile<128>(a, out, 6, stream);
-    case kWide: return launch_stream<64, 8, 1, 3>(a, out, stream);
-    case kHalf: return launch_stream<64, 4, 2, 3>(a, out, stream);
-    case kHalfTwo: return launch_stream<64, 4, 2, 2>(a, out, stream);
-    case kNarrow: return launch_stream<64, 2, 4, 3>(a, out, stream);
-    case kFewRows: return launch_stream<16, 2, 4, 3>(a, out, stream);
-    default: return launch_stream<16, 1, 8, 2>(a, out, stream);
+    case kTile256: return launch_tile<256, kTile256>(a, 6, stream);
+    case kTile128: return launch_tile<128, kTile128>(a, 6, stream);
+    case kWide: return launch_stream<64, 8, 1, 3, kWide>(a, stream);
+    case kHalf: return launch_stream<64, 4, 2, 3, kHalf>(a, stream);
+    case kHalfTwo: return launch_stream<64, 4, 2, 2, kHalfTwo>(a, stream);
+    case kNarrow: return launch_stream<64, 2, 4, 3, kNarrow>(a, stream);
+    case kFewRows: return launch_stream<16, 2, 4, 3, kFewRows>(a, stream);
+    case kOneRow: return launch_stream<16, 1, 8, 2, kOneRow>(a, stream);
+    default: return hipErrorInvalidConfiguration;
   }
 }
 

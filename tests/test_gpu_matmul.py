@@ -257,3 +257,28 @@ def test_other_streams():
                               moe.MOE_ACT_NONE, y)
     s.synchronize()
     _check(y.cpu(), a, sa, w, sw, [(0, 130)], False)
+
+
+def test_more_rows_than_one_launch_has_workgroups():
+    """600 million rows of a narrow product: tiles of 64 rows would need more workgroups than
+    a launch has.  Sums of 16 products are exact in float32; checked in pieces on the GPU,
+    the rounding to bf16 as for the others."""
+    moe = _moe()
+    rows, N, K = 600_000_000, 8, 16
+    if torch.cuda.mem_get_info()[0] < 40e9:
+        pytest.skip("not enough memory free")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    a = torch.empty(rows, K, dtype=torch.int8, device="cuda")
+    step = 50_000_000
+    for i in range(0, rows, step):
+        a[i:i + step] = torch.randint(-128, 128, (step, K), generator=g, device="cuda",
+                                      dtype=torch.int8)
+    w = torch.randint(-128, 128, (1, N, K), generator=g, device="cuda", dtype=torch.int8)
+    sa = torch.rand(rows, generator=g, device="cuda") + 0.5
+    sw = torch.rand(1, N, generator=g, device="cuda") + 0.5
+    y = torch.empty(rows, N, dtype=torch.bfloat16, device="cuda")
+    moe.moe_expert_matmul(a, sa, rows, w, sw, 1, N, K, None, None, moe.MOE_ACT_NONE, y)
+    for i in range(0, rows, step):
+        want = (a[i:i + step].float() @ w[0].float().T.contiguous()) * sa[i:i + step, None] * sw
+        assert bool(((y[i:i + step].float() - want).abs() <= BF16 * want.abs()).all()), i
