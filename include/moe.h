@@ -537,8 +537,9 @@ int moe_expert_scale(const uint64_t* recv_x, const uint64_t* recv_scales, int sc
  *
  * groups > 1: the experts form `groups` blocks of E/groups neighbours; a
  * block's key is the sum of its group_top (1 or 2) highest keys (of those it
- * has; a block without eligible experts is never kept), and the experts of the
- * top_groups best blocks, equal ones in the order of their index, take part.
+ * has; halves are added, so that the sum may pass float32's range; a block without
+ * eligible experts is never kept), and the experts of the top_groups best
+ * blocks, equal ones in the order of their index, take part.
  *
  * w = s (renorm 0), or s divided by the sum over the chosen (renorm 1; 0 if
  * that sum is 0), times scale.  A slot without an eligible expert, and every

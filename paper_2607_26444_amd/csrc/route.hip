@@ -161,8 +161,12 @@ struct TopTwo {
   }
 };
 
+// Half the sum of the two highest: it orders as the sum does, which may lie outside
+// float32 (two biases of the lowest value), where a group with eligible experts would
+// look like one without.
 __device__ __forceinline__ float group_key(const TopTwo& g, int group_top) {
-  return group_top > 1 && g.second > -INFINITY ? g.best + g.second : g.best;
+  if (group_top == 1) return g.best;
+  return 0.5f * g.best + (g.second > -INFINITY ? 0.5f * g.second : 0.0f);
 }
 
 // Groups of whole lanes, a power of two of them, that fill the token's 16 lanes

@@ -326,3 +326,30 @@ def test_gradient_of_unused_and_foreign_slots():
                               score == 1, renorm, 1.0)
         assert torch.all((got - want).abs() <= 8 * W_TOL)
         assert torch.all(got[0] == 0)
+
+
+@pytest.mark.parametrize("E,groups", [(16, 4), (64, 8), (60, 6), (256, 16), (160, 8), (512, 8), (300, 3)])
+@pytest.mark.parametrize("score", [0, 1])
+def test_group_of_experts_at_the_lowest_value(E, groups, score):
+    """A bias of the type's lowest value leaves an expert eligible, and so its group,
+    though the sum of two such keys is below every float32: it comes behind all
+    others, before groups that have no eligible expert.  The keys are equal there (a
+    score is far below the bias's last bit), so the index decides."""
+    size, lowest = E // groups, torch.finfo(torch.float32).min
+    x = _draw(9, E, True, seed=E)
+    b = torch.full((E,), lowest)
+    b[:size] = -math.inf                       # the first group is ruled out
+    opt = dict(score=score, groups=groups, group_top=2)
+    idx, w = _route(x, 2, bias=b, top_groups=1, **opt)
+    assert torch.equal(idx, torch.tensor([[size, size + 1]] * 9, dtype=torch.int32))
+    _check(x, idx, w, 2, bias=b, top_groups=1, **opt)
+    b[-size:] = 0.0                            # the last one stands above
+    idx, w = _route(x, 3, bias=b, top_groups=2, **opt)
+    live = idx >= E - size
+    assert torch.all(live[:, :min(3, size)])
+    b[-size + 1:] = lowest                     # ... by one expert
+    idx, w = _route(x, 3, bias=b, top_groups=1, **opt)
+    assert torch.all(idx[:, 0] == E - size) and torch.all(idx[:, 1] == E - size + 1)
+    b[:] = -math.inf
+    idx, w = _route(x, 3, bias=b, top_groups=2, **opt)
+    assert torch.all(idx == -1) and torch.all(w == 0)
