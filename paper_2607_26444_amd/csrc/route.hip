@@ -559,13 +559,12 @@ __device__ __forceinline__ void route_token_backward(const RouteGradArgs& a, int
     q = exp_term(xe, m) * inv;
     d = g;
   } else if (a.sigmoid) {
-    const float s = e >= 0 ? sigmoid(xe) : 0.0f;
-    q = s;
+    q = e >= 0 ? sigmoid(xe) : 0.0f;
     if (a.renorm) {
-      const float sum = reduce_sum<LANES>(s);
-      q = sum > 0.0f ? s / sum : 0.0f;
+      const float sum = reduce_sum<LANES>(q);
+      q = sum > 0.0f ? q / sum : 0.0f;
     }
-    d = q * (1.0f - s);
+    d = e >= 0 ? q * sigmoid(-xe) : 0.0f;          // 1 - s, also where s rounds to 1
   } else {
     const float one[1] = {xe};
     q = exp_term(xe, row_max<LANES, 1>(one));

@@ -353,3 +353,22 @@ def test_group_of_experts_at_the_lowest_value(E, groups, score):
     b[:] = -math.inf
     idx, w = _route(x, 3, bias=b, top_groups=2, **opt)
     assert torch.all(idx == -1) and torch.all(w == 0)
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+def test_sigmoid_gradient_of_large_logits(renorm):
+    """1 - s is sigmoid(-x), small beside s where x is large: the gradient keeps its
+    relative accuracy (W_TOL of its terms) there, also where s rounds to 1."""
+    T, E, k = 40, 48, 6
+    x = _draw(T, E, True, seed=31) + torch.linspace(-20, 60, T)[:, None]
+    idx, _ = _route(x, k, score=1, renorm=renorm)
+    gw = torch.randn(T, k, generator=torch.Generator().manual_seed(8))
+    got = _grad(x, idx, gw, 1, renorm, 1.5).double().gather(1, idx.long())
+    xw, g = x.double().gather(1, idx.long()), gw.double()
+    s, rest = torch.sigmoid(xw), torch.sigmoid(-xw)
+    q = s / s.sum(1, keepdim=True) if renorm else s
+    dot = (g * q).sum(1, keepdim=True) if renorm else torch.zeros(T, 1).double()
+    size = (g * q).abs().sum(1, keepdim=True) if renorm else dot
+    want = 1.5 * q * rest * (g - dot)
+    assert torch.all((got - want).abs() <= W_TOL * 1.5 * q * rest * (g.abs() + size))
+    assert torch.all(want[T // 2:].abs() < 1e-4)      # the rows of large logits are there
