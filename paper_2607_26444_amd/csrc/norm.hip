@@ -165,7 +165,9 @@ __device__ __forceinline__ void finish_row(const NormArgs& a, int64_t r, int at,
     }
   }
 
-  float sum = 0.0f, rstd = 1.0f;
+  // One reduction gives the sum of squares and the largest |h weight|, which is
+  // max |v| / rstd to float32's rounding.
+  float sum = 0.0f, amax = 0.0f;
   uint32_t top = 0u;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -174,19 +176,35 @@ __device__ __forceinline__ void finish_row(const NormArgs& a, int64_t r, int at,
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       sum = __builtin_fmaf(h[i].f[j], h[i].f[j], sum);
-      if (WEIGHT != kNone) h[i].f[j] *= w.f[j];
-      top = umax(top, abs_key(h[i].f[j]));
+      top = umax(top, abs_key(WEIGHT != kNone ? h[i].f[j] * w.f[j] : h[i].f[j]));
     }
   }
   if (WEIGHT != kNone || a.quant == kQuantInt8)
     row_reduce(sum, top, waves, wave, lane, s_sum, s_top);
+  amax = __uint_as_float(top);
   if constexpr (WEIGHT != kNone) {
-    rstd = 1.0f / sqrtf(sum / (float)a.H + a.eps);
+    const float rstd = 1.0f / sqrtf(sum / (float)a.H + a.eps);
     if (a.rstd && at == 0) a.rstd[r] = rstd;
+    const bool normal = top - 0x00800000u < 0x7F000000u;   // neither 0, subnormal, infinite nor NaN
+    amax *= rstd;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      const Vec8 w = weight.get(i);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[i].f[j] *= rstd;
+      for (int j = 0; j < 8; ++j) h[i].f[j] = h[i].f[j] * rstd * w.f[j];
+    }
+    // h weight may lie outside the normal range where v does not: then the maximum of v
+    // itself (the row's threads agree on that)
+    if (!normal && a.quant == kQuantInt8) {
+      top = 0u;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = umax(top, abs_key(h[i].f[j]));
+      if (waves > 1) __syncthreads();            // the first results have been read
+      row_reduce(sum, top, waves, wave, lane, s_sum, s_top);
+      amax = __uint_as_float(top);
+    }
   }
 
   if (WEIGHT != kNone && a.y) {
@@ -200,7 +218,6 @@ __device__ __forceinline__ void finish_row(const NormArgs& a, int64_t r, int at,
     }
   }
   if (a.quant == kQuantInt8) {
-    const float amax = __uint_as_float(top) * rstd;
     const float inv = kInt8Max / usable_amax(amax);
     uint8_t* q = a.q + r * (int64_t)a.H;
 #pragma unroll

@@ -310,3 +310,26 @@ def test_weight_gradient_of_no_tokens_is_zero():
     z = torch.empty(0, 256).bfloat16()
     gx, gw = _back(z, z, torch.empty(0), torch.ones(256), None)
     assert torch.all(gw == 0)
+
+
+@pytest.mark.parametrize("T,H", [(5, 128), (6, 1024), (3, 4096), (4, 16384), (1100, 7168)])
+@pytest.mark.parametrize("exponents", [(40, 100), (-50, -90)])
+def test_products_of_row_and_weight_beyond_float32(T, H, exponents):
+    """v = (h rstd) weight lies within float32 where h weight does not, or is below the
+    normal range.  Every second row is an ordinary one (with 1100 rows a workgroup takes both
+    kinds), every fifth is zero."""
+    moe = _moe()
+    up_x, up_w = exponents
+    g = torch.Generator().manual_seed(H)
+    x = torch.randn(T, H, generator=g)
+    x[::2] *= 2.0 ** up_x
+    x[::5] = 0
+    x = x.bfloat16()
+    w = (1 + 0.1 * torch.randn(H, generator=g)) * 2.0 ** up_w
+    h, rstd, v = ref.rmsnorm(x.double(), None, w.double(), 1e-37)
+    for d in (None, moe.MOE_DTYPE_FP8_E4M3, moe.MOE_DTYPE_INT8):
+        out = _run(x, None, w, 1e-37, d)
+        assert torch.all((out["rstd"].double() - rstd).abs() <= F32 * rstd)
+        assert torch.all((out["y"].double() - v).abs() <= (BF16 + F32) * v.abs())
+        if d is not None:
+            _close_codes(out["q"], out["scales"], v, d == moe.MOE_DTYPE_FP8_E4M3)
