@@ -2,8 +2,8 @@
 // rows, and the norm's gradients.
 //
 //   h = x + residual, rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd weight
-//   grad_x = rstd (u - h rstd^2 mean(u h)) + grad_sum, u = grad_y weight
-//   grad_weight = sum over rows of grad_y h rstd
+//   with u = grad_y weight, n = h rstd:
+//   grad_x = rstd (u - n mean(u n)) + grad_sum, grad_weight = sum over rows of grad_y n
 // A row is held in registers by one workgroup (rows of up to 64 * NV vectors
 // of 8 values: by one wavefront, four rows to a workgroup), read once and
 // written once; every sum is float32.  h is rounded only where it is stored: the norm
@@ -362,8 +362,9 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormGradArgs a, int
     for (int i = 0; i < NV; ++i) {
       const Vec8 w = weight.get(i);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        dw[i].f[j] = __builtin_fmaf(u[i].f[j] * h[i].f[j], rs, dw[i].f[j]);
+      for (int j = 0; j < 8; ++j) {              // h rstd first: products stay inside float32
+        h[i].f[j] *= rs;
+        dw[i].f[j] = __builtin_fmaf(u[i].f[j], h[i].f[j], dw[i].f[j]);
         u[i].f[j] *= w.f[j];
         dot = __builtin_fmaf(u[i].f[j], h[i].f[j], dot);
       }
@@ -376,7 +377,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormGradArgs a, int
       for (int k = 0; k < waves; ++k) dot += s_sum[phase][k];
     }
     if (kLate) gs.load(a.grad_sum + r * wide, at, threads, nv, true);
-    const float c = dot / (float)a.H * rs * rs;
+    const float c = dot / (float)a.H;
     uint8_t* dx = a.grad_x + r * wide;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {

@@ -333,3 +333,26 @@ def test_products_of_row_and_weight_beyond_float32(T, H, exponents):
         assert torch.all((out["y"].double() - v).abs() <= (BF16 + F32) * v.abs())
         if d is not None:
             _close_codes(out["q"], out["scales"], v, d == moe.MOE_DTYPE_FP8_E4M3)
+
+
+@pytest.mark.parametrize("T,H", [(7, 256), (5, 4096), (900, 2048)])
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("exponents", [(40, 100), (-50, -90)])
+def test_gradients_of_products_beyond_float32(T, H, f32, exponents):
+    """The gradients lie within float32 where grad_y weight h does not, or is below the
+    normal range; bounds as for ordinary rows."""
+    up_h, up_w = exponents
+    dtype = torch.float32 if f32 else torch.bfloat16
+    h = (_draw(T, H, seed=H, dtype=torch.float32) * 2.0 ** up_h).to(dtype)
+    gy = _draw(T, H, seed=H + 1)
+    w = ((1 + 0.1 * _draw(1, H, seed=H + 2, dtype=torch.float32)[0]) * 2.0 ** up_w).to(dtype)
+    rstd = (1 / (h.double().square().mean(1) + 1e-37).sqrt()).float()
+    gx, gw = _back(gy, h, rstd, w, None)
+    d = [v.double() for v in (gy, h, rstd, w)]
+    want, want_w = ref.rmsnorm_grad(*d, None)
+    u, r = d[0] * d[3], d[2][:, None]
+    size = r * u.abs() + d[1].abs() * r ** 3 * (u * d[1]).abs().mean(1, keepdim=True)
+    tol = 80 * 2.0 ** -24 * size + (0 if f32 else BF16 * want.abs())
+    assert torch.all((gx.double() - want).abs() <= tol)
+    mag = (d[0] * d[1] * r).abs().sum(0)
+    assert torch.all((gw.double() - want_w).abs() <= 80 * 2.0 ** -24 * mag)
