@@ -22,12 +22,12 @@ int route_shape(int64_t T, int k, int E, int dtype, int64_t pitch, int score, fl
   return isfinite(scale) ? MOE_OK : MOE_EINVAL;
 }
 
-// Shape of 8-bit codes: their kind, and the scales of a row.
-int quant_shape(const void* q, const float* scales, int dtype, int H, int& cols,
+// Shape of 8-bit codes: their kind, and the scales of a row.  Of no rows codes and
+// scales may be null: that is the address of an empty tensor.
+int quant_shape(const void* q, const float* scales, int64_t rows, int dtype, int H, int& cols,
                 moe::QuantKind& kind) {
-  kind = moe::kQuantNone;
-  if (!q) return MOE_OK;
-  if (!scales || (dtype != MOE_DTYPE_FP8_E4M3 && dtype != MOE_DTYPE_INT8) || cols < 0)
+  if ((rows > 0 && (!q || !scales)) ||
+      (dtype != MOE_DTYPE_FP8_E4M3 && dtype != MOE_DTYPE_INT8) || cols < 0)
     return MOE_EINVAL;
   if (dtype == MOE_DTYPE_FP8_E4M3) {
     if (H % MOE_FP8_BLOCK != 0) return MOE_EALIGN;
@@ -113,13 +113,13 @@ int moe_rmsnorm(const uint16_t* x, int64_t x_pitch, const void* residual, int re
                 int scale_cols, float* rstd, void* stream) {
   if (T < 0 || T > INT32_MAX || H < 1 || H > MOE_MAX_ROW || !(eps >= 0.0f)) return MOE_EINVAL;
   if (!logit_dtype(weight_dtype) || !weight || (residual && !logit_dtype(residual_dtype)) ||
-      (sum_out && !residual))
+      (T > 0 && sum_out && !residual))
     return MOE_EINVAL;
   if ((x_pitch != 0 && x_pitch < H) || (residual_pitch != 0 && residual_pitch < H) ||
       x_pitch > INT32_MAX || residual_pitch > INT32_MAX)
     return MOE_EINVAL;
-  moe::NormArgs a = {};
-  const int rc = quant_shape(q, q_scales, q_dtype, H, scale_cols, a.quant);
+  moe::NormArgs a = {};                          // no codes
+  const int rc = q ? quant_shape(q, q_scales, T, q_dtype, H, scale_cols, a.quant) : MOE_OK;
   if (rc) return rc;
   const bool rf = residual && residual_dtype == MOE_DTYPE_F32;
   if (H % 8 != 0 || x_pitch % 8 != 0 || residual_pitch % (rf ? 4 : 8) != 0 || !aligned(x, 16) ||
@@ -152,11 +152,11 @@ int moe_rmsnorm(const uint16_t* x, int64_t x_pitch, const void* residual, int re
 
 int moe_quantize(const uint16_t* x, int64_t x_pitch, int64_t rows, int H, const int32_t* row_src,
                  int q_dtype, void* q, float* q_scales, int scale_cols, void* stream) {
-  if (rows < 0 || rows > INT32_MAX || H < 1 || H > MOE_MAX_ROW || !q ||
+  if (rows < 0 || rows > INT32_MAX || H < 1 || H > MOE_MAX_ROW ||
       (x_pitch != 0 && x_pitch < H) || x_pitch > INT32_MAX)
     return MOE_EINVAL;
   moe::NormArgs a = {};
-  const int rc = quant_shape(q, q_scales, q_dtype, H, scale_cols, a.quant);
+  const int rc = quant_shape(q, q_scales, rows, q_dtype, H, scale_cols, a.quant);
   if (rc) return rc;
   if (H % 8 != 0 || x_pitch % 8 != 0 || !aligned(x, 16) || !aligned(row_src, 4))
     return MOE_EALIGN;

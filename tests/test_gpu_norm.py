@@ -356,3 +356,13 @@ def test_gradients_of_products_beyond_float32(T, H, f32, exponents):
     assert torch.all((gx.double() - want).abs() <= tol)
     mag = (d[0] * d[1] * r).abs().sum(0)
     assert torch.all((gw.double() - want_w).abs() <= 80 * 2.0 ** -24 * mag)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_quantize_no_rows(fp8):
+    moe = _moe()
+    x = torch.empty(0, 256, dtype=torch.bfloat16, device="cuda")
+    moe.moe_quantize(x, 0, 256, moe.MOE_DTYPE_FP8_E4M3 if fp8 else moe.MOE_DTYPE_INT8,
+                     torch.empty(0, 256, dtype=torch.int8, device="cuda"),
+                     torch.empty(0, 2, device="cuda"), scale_cols=2)
+    torch.cuda.synchronize()

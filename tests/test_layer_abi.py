@@ -277,3 +277,26 @@ def test_a_library_without_the_layer_says_so(stub, tmp_path):
     with pytest.raises(RuntimeError, match="moe_route"):
         moe.moe_route(**_arguments("moe_route"))
     assert lib
+
+
+def test_calls_of_no_rows_take_empty_tensors():
+    """An empty tensor's address is null, whatever a program holds beside it: no call of
+    no rows may ask for it, and none starts anything."""
+    ok, L = moe.MOE_OK, moe.lib()
+    assert L.moe_quantize(None, 0, 0, 1024, None, 3, None, None, 0, None) == ok
+    assert L.moe_quantize(None, 0, 0, 1024, None, 3, A, None, 0, None) == ok
+    assert L.moe_quantize(None, 0, 0, 1024, None, 1, None, A, 0, None) == ok
+    good = dict(x=None, xp=0, r=A, rd=0, rp=0, w=A, wd=0, eps=1e-6, T=0, H=1024, s=A, y=A, qd=1, q=A,
+                qs=A, cols=0, rstd=A, stream=None)
+    for change in (dict(r=None), dict(qs=None), dict(q=None), dict(s=None, y=None, q=None, rstd=None)):
+        assert L.moe_rmsnorm(*dict(good, **change).values()) == ok, change
+    # what has nothing to do with the rows is still looked at
+    E, M = moe.MOE_EINVAL, moe.MOE_EALIGN
+    assert L.moe_quantize(None, 0, 0, 1024, None, 0, None, None, 0, None) == E
+    assert L.moe_quantize(None, 0, 0, 1032, None, 3, None, None, 0, None) == M
+    assert L.moe_quantize(None, 0, 0, 1040, None, 1, None, None, 0, None) == M
+    assert L.moe_quantize(None, 0, 0, 1024, None, 3, MIS, None, 0, None) == M
+    assert L.moe_quantize(None, 0, 0, 1024, None, 1, None, None, 9, None) == E
+    for change, code in ((dict(w=None), E), (dict(H=16392), E), (dict(eps=NAN), E), (dict(H=1032), M),
+                         (dict(qd=2), E), (dict(cols=9), E)):
+        assert L.moe_rmsnorm(*dict(good, **change).values()) == code, change
