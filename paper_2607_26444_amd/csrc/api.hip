@@ -170,8 +170,8 @@ int dispatch_common(const void* x, const float* x_scales, int dtype, int64_t T, 
   if (H < 1 || (dtype != MOE_DTYPE_BF16 && dtype != MOE_DTYPE_FP8_E4M3)) return MOE_EINVAL;
   const bool fp8 = dtype == MOE_DTYPE_FP8_E4M3;
   if (!recv_x || !recv_cap || !rank_offset || !workspace || !status) return MOE_EINVAL;
-  if (fp8 && (!x_scales || !recv_scales)) return MOE_EINVAL;
-  if (T > 0 && (!x || !topk_idx || !pos)) return MOE_EINVAL;
+  if (fp8 && !recv_scales) return MOE_EINVAL;
+  if (T > 0 && (!x || (fp8 && !x_scales) || !topk_idx || !pos)) return MOE_EINVAL;
   if (policy != MOE_POLICY_BALANCED && policy != MOE_POLICY_ROWS &&
       policy != MOE_POLICY_BY_RANK && policy != MOE_POLICY_DYNAMIC &&
       policy != MOE_POLICY_STATIC)

@@ -210,3 +210,13 @@ def test_token_mask_strides():
             layer.forward(x, r, logits, token_mask=bad)
     layer.forward(x, r, logits, token_mask=table[:, 1].contiguous())
     assert torch.equal((layer.topk_idx[:, 0] >= 0).to(torch.uint8), table[:, 1])
+
+
+def test_no_tokens():
+    from paper_2607_26444_amd.layer import random_layer
+    layer = random_layer(0, 256, 64, 8, 2)
+    x, r, logits = _inputs(0, 256, 8, seed=0)
+    for given in (logits, lambda normed: normed.float() @ torch.ones(256, 8, device="cuda")):
+        assert layer.forward(x, r, given).shape == (0, 256)
+    torch.cuda.synchronize()
+    assert int(layer.layout.status) == 0 and torch.all(layer.layout.expert_count == 0)

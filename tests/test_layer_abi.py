@@ -300,3 +300,11 @@ def test_calls_of_no_rows_take_empty_tensors():
     for change, code in ((dict(w=None), E), (dict(H=16392), E), (dict(eps=NAN), E), (dict(H=1032), M),
                          (dict(qd=2), E), (dict(cols=9), E)):
         assert L.moe_rmsnorm(*dict(good, **change).values()) == code, change
+
+
+def test_dispatch_of_no_tokens_takes_empty_scales():
+    good = dict(x=None, xs=None, dtype=1, T=0, H=1024, k=2, E=8, R=1, idx=None, pos=None, ro=A, rx=A,
+                rs=A, pitch=0, cap=A, ws=WS, n=1 << 30, status=A, stream=None)
+    assert moe.lib().moe_dispatch(*good.values()) == moe.MOE_OK
+    _refuses("moe_dispatch", good, [(dict(T=8, x=A, idx=A, pos=A), moe.MOE_EINVAL),
+                                    (dict(rs=None), moe.MOE_EINVAL)])
