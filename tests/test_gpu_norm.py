@@ -366,3 +366,46 @@ def test_quantize_no_rows(fp8):
                      torch.empty(0, 256, dtype=torch.int8, device="cuda"),
                      torch.empty(0, 2, device="cuda"), scale_cols=2)
     torch.cuda.synchronize()
+
+
+# More rows than stay on the GPU at once (4096 of 128, 1024 of 2064, 512 of 7168, 256 of 16384):
+# workgroups take a third row, some of them not, and ask for the next one early.
+@pytest.mark.parametrize("T,H", [(9001, 128), (2900, 2064), (1200, 7168), (600, 16384)])
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "int8"])
+@pytest.mark.parametrize("res", [None, torch.bfloat16, torch.float32])
+def test_norm_of_many_rows(T, H, kind, res):
+    moe = _moe()
+    if kind == "fp8" and H % 128:
+        H = H // 128 * 128
+    x = _draw(T, H, seed=T)
+    r = None if res is None else _draw(T, H, seed=T + 1, dtype=res)
+    w = _draw(1, H, seed=T + 2, dtype=torch.float32 if res == torch.float32 else torch.bfloat16)[0]
+    d = dict(bf16=None, fp8=moe.MOE_DTYPE_FP8_E4M3, int8=moe.MOE_DTYPE_INT8)[kind]
+    out = _run(x, r, w, 1e-6, d, want_y=kind != "fp8")
+    h, rstd, y = ref.rmsnorm(x.double(), None if r is None else r.double(), w.double(), 1e-6)
+    assert torch.all((out["rstd"].double() - rstd).abs() <= F32 * rstd)
+    if out["y"] is not None:
+        assert torch.all((out["y"].double() - y).abs() <= (BF16 + F32) * y.abs())
+    if d is not None:
+        _close_codes(out["q"], out["scales"], y, kind == "fp8")
+    if r is not None:
+        tol = 2.0 ** -24 if res == torch.float32 else BF16
+        assert torch.all((out["sum"].double() - h).abs() <= tol * h.abs() * 1.001)
+
+
+@pytest.mark.parametrize("T,H", [(9001, 128), (1200, 7168)])
+@pytest.mark.parametrize("res", [torch.bfloat16, torch.float32])
+def test_sum_over_the_residual_of_many_rows(T, H, res):
+    """Written in place while later rows' residuals are asked for: the same bits as beside it."""
+    moe = _moe()
+    x, r = _draw(T, H, seed=1).cuda(), _draw(T, H, seed=2, dtype=res).cuda()
+    w = _draw(1, H, seed=3)[0].cuda()
+    apart = [torch.empty(T, H, dtype=res, device="cuda"),
+             torch.empty(T, H, dtype=torch.bfloat16, device="cuda")]
+    moe.moe_rmsnorm(x, r, _dt(r), w, moe.MOE_DTYPE_BF16, 1e-6, T, H, *apart, 0, None, None, None)
+    y = torch.empty_like(apart[1])
+    moe.moe_rmsnorm(x, r, _dt(r), w, moe.MOE_DTYPE_BF16, 1e-6, T, H, r, y, 0, None, None, None)
+    assert torch.equal(r, apart[0]) and torch.equal(y, apart[1])
+    assert torch.equal(r[T - 1].cpu().double(),
+                       (x[T - 1].cpu().double() + _draw(T, H, seed=2, dtype=res)[T - 1].double())
+                       .to(torch.float32).to(res).double())

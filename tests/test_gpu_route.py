@@ -372,3 +372,30 @@ def test_sigmoid_gradient_of_large_logits(renorm):
     want = 1.5 * q * rest * (g - dot)
     assert torch.all((got - want).abs() <= W_TOL * 1.5 * q * rest * (g.abs() + size))
     assert torch.all(want[T // 2:].abs() < 1e-4)      # the rows of large logits are there
+
+
+@pytest.mark.parametrize("start,E", [(0, 256), (1, 256), (4, 128), (3, 17), (2, 60), (5, 300)])
+@pytest.mark.parametrize("f32", [True, False])
+@pytest.mark.parametrize("score,renorm", [(0, True), (0, False), (1, True), (1, False)])
+def test_route_gradient_of_pitches_and_offset_bases(start, E, f32, score, renorm):
+    """Rows of a wider table, from a base that vectors would not be aligned at; the
+    gradient's base likewise.  The bits are those of packed rows."""
+    moe = _moe()
+    T, k, pitch = 37, 4, 307
+    wide = _draw(T, pitch, f32, seed=17)
+    x = wide[:, start:start + E]
+    idx, _ = _route(x.contiguous(), k, score=score, renorm=renorm)
+    gw = torch.randn(T, k, generator=torch.Generator().manual_seed(9))
+    want = _grad(x.contiguous(), idx, gw, score, renorm, 2.0)
+    out = torch.full((T * E + 9,), 7.0, dtype=x.dtype, device="cuda")
+    view = out[start:start + T * E].view(T, E)
+    moe.moe_route_backward(wide.cuda()[:, start:start + E], moe.MOE_DTYPE_F32 if f32
+                           else moe.MOE_DTYPE_BF16, E, idx.cuda(), gw.cuda(), view, score=score,
+                           renorm=renorm, scale=2.0, logits_pitch=pitch)
+    torch.cuda.synchronize()
+    assert torch.equal(view.cpu(), want)
+    assert torch.all(out[:start] == 7) and torch.all(out[start + T * E:] == 7)
+    exact = ref.route_grad(x.double(), idx, gw.double(), score == 1, renorm, 2.0)
+    bound = W_TOL * 2.0 * gw.abs().amax(1, keepdim=True).double() * (1 + k ** 0.5)
+    bound = bound + (0 if f32 else 2.0 ** -8 * exact.abs())
+    assert torch.all((want.double() - exact).abs() <= bound)
