@@ -46,3 +46,48 @@ def build_rule(folder):
         assert len(ways) == len(calls)
         return ways
     return choose
+
+
+# One size at least of every way: (way, rows of the windows, capacity or 0 for packed
+# windows, N, K).  Windows of no rows, of one, of one to four row tiles of 16, of two tiles; N ends
+# inside a tile and K inside a stage, or is shorter than one.  With swiglu N is the
+# multiple of 16 below.
+_MIXED = [0, 1, 17, 33, 49, 64, 65, 129]
+_TALL = [0, 1, 64, 65, 127, 128, 129, 300]
+CASES = [
+    ("tile256", [257, 0, 1, 256, 1000, 65, 1120, 1400] * 2, 0, 1032, 1040),
+    ("tile256", [500, 0, 129, 1000], 1000, 2072, 144),
+    ("tile128", _TALL * 8, 0, 2072, 400),
+    ("tile128", _TALL * 3, 0, 4120, 144),
+    ("tile128", [0, 1, 65, 128, 130, 64] * 8, 130, 2072, 144),
+    ("wide", _MIXED * 3, 0, 1560, 1040),
+    ("wide", [3, 0, 64, 65] * 4, 0, 4120, 112),
+    ("wide", [0, 1, 17, 33, 49, 64] * 4, 64, 1560, 1040),
+    ("half", [0, 1, 17, 33, 49, 65], 0, 2072, 144),
+    ("half", [100], 0, 4120, 400),
+    ("half", [64, 0, 33], 64, 2072, 400),
+    ("half_two", [40, 0, 129, 100, 65, 150] * 2, 0, 1032, 400),
+    ("half_two", [64, 0, 65, 129, 80, 33, 90, 70] * 4, 0, 520, 1040),
+    ("half_two", [0, 5, 100, 64] * 3, 100, 1032, 400),
+    ("narrow", [1, 33, 65, 17], 0, 1032, 1040),
+    ("narrow", [64, 0, 49, 1], 64, 520, 2064),
+    ("few_rows", [1, 0, 15, 16, 17, 9], 0, 1032, 400),
+    ("few_rows", [12, 0, 3], 12, 2072, 400),
+    ("one_row", [1, 0, 16, 17], 0, 520, 1040),
+    ("one_row", [1], 0, 1560, 4112),
+    ("one_row", [8, 0, 3, 1], 8, 520, 1040),
+]
+
+
+def call_of(case, swiglu):
+    """The call that a case of CASES makes, as build_rule's function takes it."""
+    _, counts, cap, N, K = case
+    rows = len(counts) * cap if cap else sum(counts)
+    return rows, len(counts), N // 16 * 16 if swiglu else N, K, swiglu, 1
+
+
+# Calls whose weights, rows or outputs pass 2^32 bytes: (way, rows, E, N, K), packed windows.
+PAST_32_BITS = [("few_rows", 64, 34, 2048, 65536), ("wide", 16, 34, 2048, 65536),
+                ("tile128", 3400, 34, 2048, 65536), ("narrow", 70000, 1000, 8, 65536),
+                ("tile128", 70000, 1000, 264, 65536), ("wide", 70000, 1000, 32768, 64),
+                ("tile256", 70000, 300, 32768, 64)]

@@ -12,6 +12,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import layer_ref as ref  # noqa: E402
+import matmul_rule  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -282,3 +283,50 @@ def test_more_rows_than_one_launch_has_workgroups():
     for i in range(0, rows, step):
         want = (a[i:i + step].float() @ w[0].float().T.contiguous()) * sa[i:i + step, None] * sw
         assert bool(((y[i:i + step].float() - want).abs() <= BF16 * want.abs()).all()), i
+
+
+@pytest.mark.parametrize("case", matmul_rule.CASES, ids=lambda c: f"{c[0]}-{len(c[1])}-{c[3]}-{c[4]}")
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_every_way(case, swiglu):
+    """Each kernel and size of tile on packed or fixed windows."""
+    _, counts, cap, _, _ = case
+    rows, E, N, K, _, _ = matmul_rule.call_of(case, swiglu)
+    if cap:
+        offset, windows = [777 + e * cap for e in range(E + 1)], \
+            [(e * cap, n) for e, n in enumerate(counts)]
+    else:
+        offset, windows = _packed(counts)
+    t = _inputs(rows, E, N, K, seed=rows + N)
+    y = _run(*t, offset, counts, swiglu)
+    _check(y, *t, windows, swiglu)
+    if not cap and E > 1:
+        assert torch.equal(_run(*t, offset, None, swiglu), y)
+
+
+@pytest.mark.parametrize("way,rows,E,N,K", matmul_rule.PAST_32_BITS)
+def test_every_kernel_past_32_bits(way, rows, E, N, K):
+    """Weights, rows or outputs whose byte offsets pass 2^32: the last rows, and channels of
+    the last expert."""
+    moe = _moe()
+    n = min(rows, max(3, rows // E))
+    start = rows - n
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+
+    def int8(*shape):
+        return torch.randint(-128, 128, shape, generator=g, device="cuda", dtype=torch.int8)
+    a = torch.zeros(rows, K, dtype=torch.int8, device="cuda")
+    w = torch.zeros(E, N, K, dtype=torch.int8, device="cuda")
+    a[start:], w[-1, -8:] = int8(n, K), int8(8, K)
+    offset = torch.full((E + 1,), start, dtype=torch.int32, device="cuda")
+    offset[0], offset[E] = 0, rows
+    count = torch.zeros(E, dtype=torch.int32, device="cuda")
+    count[-1] = n
+    sa = torch.full((rows,), 1 / 73, device="cuda")
+    sw = torch.full((E, N), 1 / (73 * 256.0), device="cuda")
+    y = torch.zeros(rows, N, dtype=torch.bfloat16, device="cuda")
+    moe.moe_expert_matmul(a, sa, rows, w, sw, E, N, K, offset, count, moe.MOE_ACT_NONE, y)
+    want = (a[start:].double() @ w[-1, -8:].double().T.contiguous()) / (73 * 73 * 256.0)
+    got = y[start:, -8:].double()
+    assert torch.all((got - want).abs() <= BF16 * want.abs() + 1e-9)
+    assert not torch.any(y[:start]) and not torch.any(y[start:, :-8])

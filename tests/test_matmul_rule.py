@@ -45,3 +45,17 @@ def test_every_call_gets_a_way_that_can_be_launched(choose):
             assert tiles < 2 ** 31 - 512, (way, call)
         else:
             assert -(-tiles // 256) * 256 * 512 < 2 ** 32, (way, call)
+
+
+@pytest.mark.parametrize("swiglu", [0, 1])
+def test_the_sizes_of_the_gpu_tests_take_every_way(choose, swiglu):
+    got = choose([matmul_rule.call_of(c, swiglu) for c in matmul_rule.CASES])
+    assert got == [c[0] for c in matmul_rule.CASES]
+    assert set(got) == set(matmul_rule.WAYS)
+
+
+def test_the_sizes_past_32_bits_take_their_ways(choose):
+    calls = [(*c[1:], 0, 1) for c in matmul_rule.PAST_32_BITS]
+    assert choose(calls) == [c[0] for c in matmul_rule.PAST_32_BITS]
+    for rows, E, N, K, _, _ in calls:
+        assert max(rows * K, E * N * K, 2 * rows * N) > 2 ** 32
