@@ -409,3 +409,29 @@ def test_sum_over_the_residual_of_many_rows(T, H, res):
     assert torch.equal(r[T - 1].cpu().double(),
                        (x[T - 1].cpu().double() + _draw(T, H, seed=2, dtype=res)[T - 1].double())
                        .to(torch.float32).to(res).double())
+
+
+@pytest.mark.parametrize("rows,H", [((1 << 22) + 99, 128), ((1 << 20) + 77, 1152)])
+@pytest.mark.parametrize("fp8", [True, False])
+def test_quantize_more_rows_than_one_grid(rows, H, fp8):
+    """Workgroups go round again, over rows that are skipped and rows that are not: the last
+    rows as in a call of their own, and as the definition has them."""
+    moe = _moe()
+    d = moe.MOE_DTYPE_FP8_E4M3 if fp8 else moe.MOE_DTYPE_INT8
+    cols, tail = H // 128 if fp8 else 1, 3000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(H)
+    x = torch.randn(rows, H, generator=g, device="cuda", dtype=torch.bfloat16)
+    src = torch.arange(rows, dtype=torch.int32, device="cuda")
+    src[1::3] = -1
+    q = torch.full((rows, H), 77, dtype=torch.int8, device="cuda")
+    s = torch.full((rows, cols), -3.0, device="cuda")
+    moe.moe_quantize(x, rows, H, d, q, s, row_src=src)
+    part_q = torch.full((tail, H), 77, dtype=torch.int8, device="cuda")
+    part_s = torch.full((tail, cols), -3.0, device="cuda")
+    moe.moe_quantize(x[-tail:], tail, H, d, part_q, part_s, row_src=src[-tail:])
+    assert torch.equal(q[-tail:], part_q) and torch.equal(s[-tail:], part_s)
+    live = (src[-200:] >= 0).cpu()
+    _close_codes(q[-200:].cpu()[live], s[-200:].cpu()[live], x[-200:].cpu()[live].double(), fp8)
+    assert bool((q[src < 0] == 77).all()) and bool((s[src < 0] == -3.0).all())
+    assert bool((s[src >= 0] > 0).all())

@@ -399,3 +399,30 @@ def test_route_gradient_of_pitches_and_offset_bases(start, E, f32, score, renorm
     bound = W_TOL * 2.0 * gw.abs().amax(1, keepdim=True).double() * (1 + k ** 0.5)
     bound = bound + (0 if f32 else 2.0 ** -8 * exact.abs())
     assert torch.all((want.double() - exact).abs() <= bound)
+
+
+@pytest.mark.parametrize("E,k,opt", [(8, 2, {}), (16, 4, dict(groups=4, top_groups=2, group_top=2)),
+                                     (4, 1, dict(renorm=False)), (72, 4, {})])
+@pytest.mark.parametrize("score", [0, 1])
+def test_more_tokens_than_one_grid(E, k, opt, score):
+    """Workgroups go round again from 2^24 tokens on: the last ones route, and have gradients,
+    as in a call of their own (with 72 experts past 2^32 bytes)."""
+    moe = _moe()
+    T, tail = (1 << 24) + 1237, 5000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(E)
+    x = torch.randn(T, E, generator=g, device="cuda", dtype=torch.float32)
+    idx = torch.full((T, k), -9, dtype=torch.int32, device="cuda")
+    w = torch.full((T, k), -9.0, device="cuda")
+    moe.moe_route(x, moe.MOE_DTYPE_F32, E, None, None, idx, w, score=score, **opt)
+    part_idx, part_w = torch.empty_like(idx[-tail:]), torch.empty_like(w[-tail:])
+    moe.moe_route(x[-tail:], moe.MOE_DTYPE_F32, E, None, None, part_idx, part_w, score=score, **opt)
+    assert torch.equal(idx[-tail:], part_idx) and torch.equal(w[-tail:], part_w)
+    assert bool(((idx >= 0) & (idx < E)).all()) and bool((w > 0).all())
+    _check(x[-50:].cpu(), idx[-50:].cpu(), w[-50:].cpu(), k, score=score, **opt)
+    gw = torch.randn(T, k, generator=g, device="cuda")
+    grad, part = torch.full_like(x, 7.0), torch.empty_like(x[-tail:])
+    back = dict(score=score, renorm=opt.get("renorm", True))
+    moe.moe_route_backward(x, moe.MOE_DTYPE_F32, E, idx, gw, grad, **back)
+    moe.moe_route_backward(x[-tail:], moe.MOE_DTYPE_F32, E, part_idx, gw[-tail:], part, **back)
+    assert torch.equal(grad[-tail:], part) and not bool((grad == 7.0).any())
