@@ -541,8 +541,10 @@ int moe_expert_scale(const uint64_t* recv_x, const uint64_t* recv_scales, int sc
  * eligible experts is never kept), and the experts of the top_groups best
  * blocks, equal ones in the order of their index, take part.
  *
- * w = s (renorm 0), or s divided by the sum over the chosen (renorm 1; 0 if
- * that sum is 0), times scale.  A slot without an eligible expert, and every
+ * w = s (renorm 0), or s divided by the sum over the chosen (renorm 1), times
+ * scale.  A renormalised softmax is one over the chosen logits: its weights sum to
+ * scale also where every chosen score is too small for float32; sigmoid scores that all
+ * are 0 give weights of 0.  A slot without an eligible expert, and every
  * slot of a token whose token_mask byte is 0, gets topk_idx = -1 and weight 0,
  * which moe_layout takes as unused.
  *
@@ -591,7 +593,8 @@ int moe_route_backward(const void* logits, int dtype, int64_t logits_pitch, int6
  *      h = x + residual           sum_out = h
  *      rstd = 1 / sqrt(mean(h^2) + eps)
  *      v = h * rstd * weight      y = bf16(v), q = 8-bit codes of v
- * The norm reads the unrounded h.
+ * The norm reads the unrounded h.  Its squares are summed in float32: rows of values
+ * beyond about 2^63, or with eps 0 below 2^-63, are outside what it can norm.
  *
  * x         [T,H] bf16, rows x_pitch elements apart, 16-byte aligned rows.
  * residual  [T,H] of residual_dtype (BF16 or F32), rows residual_pitch apart, or
@@ -668,7 +671,8 @@ int moe_quantize(const uint16_t* x, int64_t x_pitch, int64_t rows, int H,
  * moe_expert_matmul -- the experts' products on 8-bit integers, scales for each
  * row and each channel:
  *      v[r,n] = (sum_k a[r,k] * w[e,n,k]) * a_scales[r] * w_scales[e,n]
- * for the rows r of expert e's window, summed exactly in int32.
+ * for the rows r of expert e's window, summed exactly in int32.  The two scales are
+ * multiplied first.
  *      MOE_ACT_NONE    y[r,n] = bf16(v[r,n])                    n < N
  *      MOE_ACT_SWIGLU  y[r,i] = bf16(silu(v[r,i]) * v[r,N/2+i])  i < N/2
  *
@@ -677,10 +681,10 @@ int moe_quantize(const uint16_t* x, int64_t x_pitch, int64_t rows, int H,
  * w         [E,N,K] int8, 16-byte aligned: channel by channel, the depth innermost.
  * w_scales  [E,N] float32.
  * expert_offset, expert_count: expert e's window is the expert_count[e] rows
- *           from expert_offset[e] - expert_offset[0], clipped to [0, rows).
- *           expert_count NULL: up to expert_offset[e+1].  Both as moe_layout or
- *           moe_layout_fixed leave them; a rank passes expert_offset + r*L and
- *           expert_count + r*L with its own region.  Windows may not overlap.
+ *           from expert_offset[e] - expert_offset[0], cut off at `rows`; one that
+ *           begins outside [0, rows) has none.  expert_count NULL: up to
+ *           expert_offset[e+1].  Both as moe_layout or moe_layout_fixed leave them; a
+ *           rank passes expert_offset + r*L and expert_count + r*L with its own region.  Windows may not overlap.
  *           expert_offset NULL (E = 1 only): one window of all rows, a plain
  *           matrix product.
  * y         [rows,N] or [rows,N/2] bf16, 16-byte aligned, row bytes % 16 == 0; rows of no

@@ -113,7 +113,7 @@ typedef __attribute__((address_space(3))) uint8_t lds_u8;
 
 // LDS rows are 128 bytes of the depth, as eight chunks of 16: chunk c of row r at
 // place c ^ (r & 7), so that eight lanes that read one chunk of eight rows
-// touch all banks.
+// touch all banks: no bank conflicts are counted.
 constexpr int kDepth = 128;
 
 // One load instruction of a wavefront: eight rows of 128 bytes from memory into
@@ -141,11 +141,13 @@ __device__ __forceinline__ void meet() {
 // A wavefront of 128 rows reads 12 fragments for 32 matrix instructions of 16 x 16 x
 // 64, half a stage ahead.  Tiles of 128 rows are for calls that make few of 256: a tile
 // alone waits for memory 1.6 us a stage with 256 rows and one stage ahead, 1.05 us with
-// 128 and two (4096 rows, 32 experts, 7168 x 4096 with swiglu 275 and 207 us; with one
-// stage ahead 128 rows took 259).
+// 128 and two (32 experts of 128 rows, 7168 x 4096 with swiglu 225 and 184 us; 2048 x 4096
+// x 4096 55 and 35).  With one stage ahead tiles of 128 rows took a quarter longer.
 //
-// Bound by the matrix instructions, which are busy about two thirds of the cycles
-// at the clock that the card's power leaves them (operands of zeros run 8% faster).
+// Bound by the matrix instructions and the clock that the card's power leaves them.  Of
+// four calls one after another the clock falls from 1.95 to 1.34 GHz and the matrix
+// instructions are busy 59 to 70% of the cycles (operands of zeros run 8% faster); between a
+// layer's other kernels 54% at 1.96 GHz.
 // 32768 rows, 16 experts, 7168 x 4096 with swiglu: 805 to 847 us by card, 2270 to
 // 2390 TOP/s; 16384 x 8192 x 8192: 807 to 842 us, 2610 to 2725 TOP/s; 32 experts of 980
 // to 1080 rows, 7168 x 4096: 835 us.  Beside it 32 x 32 x 32 instructions 1012 us (16 x

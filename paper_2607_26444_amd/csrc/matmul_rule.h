@@ -70,18 +70,27 @@ inline bool way_fits(const MatmulArgs& a, int n) {
 
 // Microseconds of a call: its rounds of workgroups, the last one counted for the
 // larger part also where it is not full, and the reading of the weights, which partly
-// hides behind them.  Measured where two ways are near each other, us:
-//   rows, experts, K x N                   256   128    64 x 128  64 x 64 (three, two stages)
-//   13483, 3, 5952 x 4752, swiglu          357   402    858       946   881
-//   2048, 1, 4096 x 4096                    58    37     76        94    66
-//   4096, 32, 7168 x 4096, swiglu          275   212    316       389   359
-//   4662, 96, 2064 x 1416                  105    88     84       100    95
-//   512, 1, 4096 x 4096                     46    35     24        26    19
-//   256, 1, 4096 x 4096                     42    29     23        15    17
-// and of few rows             64 x 128  64 x 64  64 x 32  16 x 32  16 x 16
-//   64, 1, 7168 x 4096               28       17       13       16       18
-//   64, 8, 2048 x 1024               11      8.6      7.3      5.6      6.2
-//   1, 1, 7168 x 4096                26       16        -       12        9
+// hides behind them.  The model is there to order the ways; its times are mostly long, by
+// up to a half where rounds and reading hide more of each other.  Measured / model, us,
+// rows drawn to the experts evenly:
+//   rows, experts, K x N               256      128      64 x 128  64 x 64 three, two stages
+//   512, 32, 7168 x 4096, swiglu     183/276  158/233  157/209  168/269  163/243
+//   2048, 32, the same               187/276  165/233  203/257  235/329  239/280
+//   4096, 32, the same               217/276  219/274  315/373  393/473  361/374
+//   4200, 32, the same               219/276  250/311  338/421  406/489  371/395
+//   8192, 32, the same               331/354  314/378  555/627  683/791  598/596
+//   8192, 32, 2048 x 7168            184/223  177/226  296/350  446/527  352/366
+//   13483, 3, 5952 x 4752, swiglu    345/401  379/442  854/909  946/1168 883/858
+//   2048, 1, 4096 x 4096              55/60    35/40    73/80    89/107   66/76
+//   4662, 96, 2064 x 1416             90/117   79/89    73/79    93/101   84/85
+//   512, 1, 4096 x 4096               47/60    34/40    23/26    25/27    20/19
+//   256, 1, 4096 x 4096               42/60    30/40    22/26    13/14    16/19
+// and of few rows                   64 x 128  64 x 64  64 x 32  16 x 32  16 x 16
+//   64, 1, 7168 x 4096                27/44    16/22    13/14    15/16    15/21
+//   64, 8, 2048 x 1024                10/15   6.2/9.0  6.0/6.8  4.1/6.7  4.9/6.2
+//   1, 1, 7168 x 4096                 25/44    14/22    11/14    10/14   5.2/11
+// The way chosen is the best of each line or within 6% of it, but for 64 rows over 8
+// experts (4.9 for 4.1).
 inline double way_time(const MatmulArgs& a, const Way& w) {
   const double groups = even_tiles(a, w.rows) * pieces_of(a, w);
   const double full = groups / w.resident;

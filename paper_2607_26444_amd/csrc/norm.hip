@@ -9,10 +9,10 @@
 // written once; every sum is float32.  h is rounded only where it is stored: the norm
 // and the 8-bit codes follow from the unrounded row.
 //
-// Bound by HBM.  16384 rows of 7168, bf16 residual, to fp8 (826 MB): 158 us, 5.2 TB/s.
-// Gradients of 32768 x 4096 bf16 (1074 MB): 200 us, 5.4 TB/s.  A workgroup that
+// Bound by HBM.  16384 rows of 7168, bf16 residual, to fp8 (826 MB): 159 us, 5.2 TB/s.
+// Gradients of 32768 x 4096 bf16 (1074 MB): 201 us, 5.4 TB/s.  A workgroup that
 // ends after its row reads nothing while it reduces, so workgroups stay and ask for
-// the next row first (227 -> 158 us and 222 -> 200).  Small batches are bound by the
+// the next row first (227 -> 159 us and 222 -> 201).  Small batches are bound by the
 // launch: 64 rows of 7168 6.1 us; the gradients take two launches, 777 x 2056 11 us.
 
 #include <math.h>

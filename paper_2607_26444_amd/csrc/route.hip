@@ -11,11 +11,12 @@
 // are a softmax over the k winners' logits.  All of it is float32, the sum in a
 // fixed order, so equal inputs give equal keys.
 //
-// A batch is read once and little is written, but neither bounds it: up to
-// about 4096 tokens a call takes 4 to 5 us, of which the launch is most, and beyond
-// that the instructions of a token do.  16384 tokens, 256 float32 logits, 8 slots (17.8
-// MB): 6.7 us; with sigmoid, bias and 4 of 8 groups 11.9 us.  The gradient of 32768 x
-// 128 bf16 softmax logits (18.9 MB): 7.3 us.
+// A batch is read once and little is written, but neither bounds it.  Up to about
+// 4096 tokens it is the launch and the chain of one token's steps: 3.5 to 5 us where
+// logits are the keys, 7 to 8.5 with scores, a bias and groups.  Beyond that the
+// instructions of a token: 16384 tokens, 256 float32 logits, 8 slots (17.8 MB) 6.5 us with
+// logits as keys, 9.7 with sigmoid scores and a bias, 11.8 with 4 of 8 groups
+// besides.  The gradient of 32768 x 128 bf16 softmax logits (18.9 MB): 7.3 us.
 
 #include <math.h>
 
@@ -202,9 +203,9 @@ __device__ __forceinline__ void keep_lane_groups(const RouteArgs& a, int sub, fl
 }
 
 // The same for any groups; `mine`: the keys in LDS.  Of a whole wavefront up to 16
-// lanes look over each group (7638 tokens, 512 experts in 4 groups 9.7 us, by one lane
-// 16.5; 16384, 512 in 8, 28.6 and 33.5), of 16 lanes one (16384 tokens, 160 experts in 8
-// 10.9 us, by two 14.0).
+// lanes look over each group (7638 tokens, 512 bf16 logits in 4 groups, one slot, 9.7 us,
+// by one lane 16.5; 16384, 512 scores with a bias in 8, 8 slots, 28.6 and 33.5), of 16 lanes
+// one (16384 tokens, 160 logits in 8 groups 11 us, by two 14.0).
 template <int LANES, int VPL>
 __device__ __forceinline__ void keep_groups(const RouteArgs& a, int sub, int tok, float* mine,
                                             float (&kf)[VPL]) {
@@ -379,7 +380,7 @@ enum Groups : int { kOneGroup = 0, kLaneGroups = 1, kAnyGroups = 2 };
 enum Keys : int { kLogits = 0, kSigmoidKeys = 1, kSoftmaxKeys = 2, kSoftmaxSum = 3 };
 
 // From eight experts to a lane on the threshold is the faster way (16384
-// tokens, 256 experts, 8 slots 9.0 -> 6.7 us; 32768 tokens, 128 experts 9.5 -> 8.2;
+// tokens, 256 experts, 8 slots 9.0 -> 6.6 us; 32768 tokens, 128 experts 9.5 -> 8.2;
 // four to a lane: equal).  Up to two slots are found in turn.
 constexpr bool by_threshold(int vpl) { return vpl >= 8; }
 

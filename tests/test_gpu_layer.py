@@ -220,3 +220,26 @@ def test_no_tokens():
         assert layer.forward(x, r, given).shape == (0, 256)
     torch.cuda.synchronize()
     assert int(layer.layout.status) == 0 and torch.all(layer.layout.expert_count == 0)
+
+
+def test_gate_on_a_stream_of_another_library():
+    """A stream that is known by its address alone."""
+    from paper_2607_26444_amd.layer import random_layer
+    T, H, E = 64, 256, 8
+    layer = random_layer(T, H, 64, E, 2)
+    gate = torch.randn(H, E, device="cuda").bfloat16() / 16
+    x, r, _ = _inputs(T, H, E, seed=10)
+    want = layer.forward(x, r, lambda normed: normed @ gate).clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+
+    class Foreign:
+        cuda_stream = s.cuda_stream
+    seen = []
+
+    def logits(normed):
+        seen.append(torch.cuda.current_stream().cuda_stream)
+        return normed @ gate
+    y = layer.forward(x, r, logits, stream=Foreign())
+    s.synchronize()
+    assert seen == [s.cuda_stream] and torch.equal(y, want)
