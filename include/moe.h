@@ -582,6 +582,58 @@ int moe_route_backward(const void* logits, int dtype, int64_t logits_pitch, int6
                        int E, int score, int renorm, float scale, const int32_t* topk_idx,
                        const float* grad_w, void* grad_logits, void* stream);
 
+/* Workspace of moe_balance (written to *out_bytes, a HOST pointer; may be 0). */
+int moe_balance_workspace_bytes(int64_t T, int E, int64_t seq_len, size_t* out_bytes);
+
+/*
+ * moe_balance -- how evenly the tokens of each sequence went to the experts: the
+ * slots of every expert and the balance loss that trains the router.
+ *
+ * The T tokens are S = T / seq_len sequences of seq_len tokens each (seq_len 0: one
+ * sequence of all T, S = 1).  Over a sequence's live tokens (token_mask not 0), n of them,
+ * with s the scores of score over the eligible experts (logit neither -inf nor NaN):
+ *      p_te = s_te / sum_i s_ti                   (softmax: the scores themselves)
+ *      mean_score[e] = sum_t p_te / n
+ *      expert_count[e] = slots of live tokens that name e
+ *      loss = sum_e f_e mean_score[e],  f_e = E expert_count[e] / sum_i expert_count[i]
+ * which is 1 for an even load or even scores.  A token without an eligible expert, or whose
+ * scores add up to less than float32's smallest normal number, has p = 0 and counts in n;
+ * a sequence without live tokens or slots has loss 0.
+ *
+ * logits, dtype, logits_pitch, score, token_mask: as for moe_route; topk_idx [T,k] as it
+ * left it (entries outside [0, E) are no slots).
+ * Out: expert_count [S,E] int32, live_tokens [S] int32, mean_score [S,E] float32 or NULL,
+ *      loss [S] float32 or NULL.
+ * workspace: 256-byte aligned, moe_balance_workspace_bytes; NULL where that is 0.  Every call
+ * rewrites it: calls that share one may not overlap in time.
+ * Tokens are summed in an order that depends on the sizes alone: equal calls give equal bits.
+ * Errors: MOE_EINVAL also for seq_len < 0 or T % seq_len.
+ */
+int moe_balance(const void* logits, int dtype, int64_t logits_pitch, int64_t T, int k, int E,
+                int score, int64_t seq_len, const int32_t* topk_idx, const uint8_t* token_mask,
+                int32_t* expert_count, int32_t* live_tokens, float* mean_score, float* loss,
+                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * moe_balance_backward -- gradient of the logits from that of moe_balance's losses (the
+ * counts, a choice, have none).  With g = grad_loss of the token's sequence:
+ *      softmax    dx_te = g / n p_te (f_e - sum_i f_i p_ti) + grad_sum
+ *      sigmoid    dx_te = g / n p_te (1 - s_te) (f_e - sum_i f_i p_ti) + grad_sum
+ * and grad_sum alone for experts and tokens without a share.
+ *
+ * expert_count [S,E], live_tokens [S]: as moe_balance left them.  f follows from
+ *     expert_count alone, so counts added up over ranks balance the load of all of them.
+ * grad_loss   [S] float32.
+ * grad_sum    [T,E] (packed, type of the logits) or NULL: another gradient of the same
+ *     logits, as moe_route_backward leaves it.
+ * grad_logits [T,E] (packed, type of the logits), written whole; may be grad_sum.
+ */
+int moe_balance_backward(const void* logits, int dtype, int64_t logits_pitch, int64_t T, int E,
+                         int score, int64_t seq_len, const uint8_t* token_mask,
+                         const int32_t* expert_count, const int32_t* live_tokens,
+                         const float* grad_loss, const void* grad_sum, void* grad_logits,
+                         void* stream);
+
 /* Widest row of moe_rmsnorm, moe_rmsnorm_backward and moe_quantize: a workgroup holds one
  * row in registers, so that it is read once. */
 #define MOE_MAX_ROW 16384
@@ -697,6 +749,66 @@ int moe_expert_matmul(const int8_t* a, const float* a_scales, int a_scale_pitch,
                       const int8_t* w, const float* w_scales, int E, int N, int K,
                       const int32_t* expert_offset, const int32_t* expert_count, int act,
                       uint16_t* y, void* stream);
+
+/*
+ * Microscaled 4-bit floats (OCP MXFP4): 32 neighbouring values of a row share a scale byte s,
+ * 2^(s - 127), 255 marking a block with infinity or NaN; a value is a sign and a
+ * magnitude of 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (codes 0 to 7, plus 8 for a negative one).
+ * A row of H values is H/2 bytes of codes, two to a byte, the first in the low half, and
+ * H/32 scale bytes, whose rows are whole words: packed ones lie (H/32 + 3) / 4 * 4 bytes apart.
+ */
+#define MOE_MX_BLOCK 32
+#define MOE_MAX_MX_PITCH 1048576 /* widest pitch of the rows of moe_expert_matmul_mx */
+
+/*
+ * moe_quantize_mx -- bf16 rows as microscaled 4-bit floats: rows for moe_expert_matmul_mx,
+ * or an expert's weights, channel by channel, once.
+ *
+ * With a = max |x| of a block the scale is the power of two that puts a into [3.5, 7) of its
+ * units (at least 2^-127; 1 if a = 0) and a code is x / scale rounded to nearest even, at
+ * most 6.  Signs are kept, also those of zeros.  Codes of a block marked 255 say nothing.
+ *
+ * x           [rows,H] bf16, rows x_pitch elements apart, 16-byte aligned rows.
+ * row_src     [rows] int32 or NULL: rows whose entry is negative are skipped, as in
+ *             moe_quantize.
+ * q           [rows,H/2], rows q_pitch BYTES apart (0 = packed), 16-byte aligned rows.
+ * q_scales    [rows,H/32], rows scale_pitch BYTES apart (0 = packed), 4-byte aligned
+ *             rows; the bytes that fill the last word are written as 0.
+ *             With q_scales = q + H/2 and one pitch P for both, a multiple of 16, a row is P
+ *             neighbouring bytes: moe_dispatch carries it as P/2 values of MOE_DTYPE_BF16.
+ * values      [rows,H] bf16 or NULL: the values that codes and scales stand for (exact; NaN
+ *             in blocks marked 255), to train through the rounding or to measure it.
+ * Errors: MOE_EALIGN for H % 32, misaligned pointers or pitches; MOE_EINVAL for H >
+ * MOE_MAX_DEPTH, a pitch below a row's bytes.
+ */
+int moe_quantize_mx(const uint16_t* x, int64_t x_pitch, int64_t rows, int H,
+                    const int32_t* row_src, uint8_t* q, int64_t q_pitch, uint8_t* q_scales,
+                    int64_t scale_pitch, uint16_t* values, void* stream);
+
+/*
+ * moe_expert_matmul_mx -- the experts' products on microscaled 4-bit floats:
+ *      v[r,n] = sum_k a[r,k] * w[e,n,k]
+ * over the values that codes and scales stand for, for the rows r of expert e's window;
+ * products are exact and added in float32.
+ *      MOE_ACT_NONE    y[r,n] = bf16(v[r,n])                    n < N
+ *      MOE_ACT_SWIGLU  y[r,i] = bf16(silu(v[r,i]) * v[r,N/2+i])  i < N/2
+ * A block marked 255 makes every v that it takes part in NaN.
+ *
+ * a         [rows,K/2] codes, rows a_pitch BYTES apart (0 = packed), 16-byte aligned rows.
+ * a_scales  [rows,K/32], rows a_scale_pitch BYTES apart (0 = packed), 4-byte aligned rows.
+ *           What fills the last word of a row takes no part.
+ * w         [E,N,K/2] codes, packed, 16-byte aligned: channel by channel, the depth
+ *           innermost, as moe_quantize_mx leaves E*N rows of K values.
+ * w_scales  [E,N,K/32], packed (rows of whole words).
+ * expert_offset, expert_count, act, y: as for moe_expert_matmul.
+ * Errors: MOE_EALIGN for K % 32, N % 8 (SWIGLU: N % 16), misaligned pointers or pitches;
+ * MOE_EINVAL for K > MOE_MAX_DEPTH, a pitch below a row's bytes or above
+ * MOE_MAX_MX_PITCH, rows > INT32_MAX, E > MOE_MAX_EXPERTS.
+ */
+int moe_expert_matmul_mx(const uint8_t* a, int a_pitch, const uint8_t* a_scales, int a_scale_pitch,
+                         int64_t rows, const uint8_t* w, const uint8_t* w_scales, int E, int N,
+                         int K, const int32_t* expert_offset, const int32_t* expert_count, int act,
+                         uint16_t* y, void* stream);
 
 #ifdef __cplusplus
 }

@@ -24,7 +24,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libmoe.so")
 PYCALL = os.path.join(HERE, "_moecall" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.hip", "layout.hip", "dispatch.hip", "combine.hip", "expert.hip", "dedup.hip",
-           "scratch.hip", "api_layer.hip", "route.hip", "norm.hip", "matmul.hip"]
+           "scratch.hip", "api_layer.hip", "route.hip", "balance.hip", "norm.hip", "mx.hip",
+           "matmul.hip", "matmul_mx.hip"]
 
 
 def hipcc() -> str:

@@ -22,6 +22,14 @@ int route_shape(int64_t T, int k, int E, int dtype, int64_t pitch, int score, fl
   return isfinite(scale) ? MOE_OK : MOE_EINVAL;
 }
 
+// Sequences of the balance loss: whole ones.
+int balance_sizes(int64_t T, int k, int E, int64_t seq_len) {
+  if (T < 0 || T > (int64_t)INT32_MAX / k || E < 1 || E > MOE_MAX_EXPERTS || seq_len < 0 ||
+      (seq_len > 0 && T % seq_len != 0))
+    return MOE_EINVAL;
+  return MOE_OK;
+}
+
 // Shape of 8-bit codes: their kind, and the scales of a row.  Of no rows codes and
 // scales may be null: that is the address of an empty tensor.
 int quant_shape(const void* q, const float* scales, int64_t rows, int dtype, int H, int& cols,
@@ -105,6 +113,87 @@ int moe_route_backward(const void* logits, int dtype, int64_t logits_pitch, int6
   a.grad_w = grad_w;
   a.grad_logits = grad_logits;
   return moe::hip_status(moe::launch_route_backward(a, as_stream(stream)));
+}
+
+int moe_balance_workspace_bytes(int64_t T, int E, int64_t seq_len, size_t* out_bytes) {
+  if (!out_bytes || balance_sizes(T, 1, E, seq_len)) return MOE_EINVAL;
+  *out_bytes = moe::balance_shape(T, E, seq_len).bytes;
+  return MOE_OK;
+}
+
+int moe_balance(const void* logits, int dtype, int64_t logits_pitch, int64_t T, int k, int E,
+                int score, int64_t seq_len, const int32_t* topk_idx, const uint8_t* token_mask,
+                int32_t* expert_count, int32_t* live_tokens, float* mean_score, float* loss,
+                void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = route_shape(T, k, E, dtype, logits_pitch, score, 1.0f);
+  if (!rc) rc = balance_sizes(T, k, E, seq_len);
+  if (rc) return rc;
+  const moe::BalanceShape s = moe::balance_shape(T, E, seq_len);
+  if (s.seqs == 0) return MOE_OK;
+  if ((T > 0 && (!logits || !topk_idx)) || !expert_count || !live_tokens) return MOE_EINVAL;
+  if (!aligned(logits, dtype == MOE_DTYPE_F32 ? 4 : 2) || !aligned(topk_idx, 4) ||
+      !aligned(expert_count, 4) || !aligned(live_tokens, 4) || !aligned(mean_score, 4) ||
+      !aligned(loss, 4))
+    return MOE_EALIGN;
+  if (s.bytes > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes))
+    return MOE_EWORKSPACE;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  moe::BalanceArgs a;
+  a.logits = logits;
+  a.pitch = logits_pitch ? logits_pitch : E;
+  a.seq = s.seq;
+  a.seqs = s.seqs;
+  a.per = s.per;
+  a.parts = s.parts;
+  a.f32 = dtype == MOE_DTYPE_F32;
+  a.k = k;
+  a.E = E;
+  a.sigmoid = score == MOE_SCORE_SIGMOID;
+  a.topk_idx = topk_idx;
+  a.token_mask = token_mask;
+  a.expert_count = expert_count;
+  a.live_tokens = live_tokens;
+  a.mean_score = mean_score;
+  a.loss = loss;
+  a.partial = reinterpret_cast<float*>(ws);
+  a.part_live = reinterpret_cast<int32_t*>(ws + s.live_at);
+  a.tickets = reinterpret_cast<uint32_t*>(ws + s.ticket_at);
+  a.pieces = reinterpret_cast<float*>(ws + s.piece_at);
+  return moe::hip_status(moe::launch_balance(a, s.blocks, as_stream(stream)));
+}
+
+int moe_balance_backward(const void* logits, int dtype, int64_t logits_pitch, int64_t T, int E,
+                         int score, int64_t seq_len, const uint8_t* token_mask,
+                         const int32_t* expert_count, const int32_t* live_tokens,
+                         const float* grad_loss, const void* grad_sum, void* grad_logits,
+                         void* stream) {
+  int rc = route_shape(T, 1, E, dtype, logits_pitch, score, 1.0f);
+  if (!rc) rc = balance_sizes(T, 1, E, seq_len);
+  if (rc) return rc;
+  if (T == 0) return MOE_OK;
+  if (!logits || !expert_count || !live_tokens || !grad_loss || !grad_logits) return MOE_EINVAL;
+  const uintptr_t size = dtype == MOE_DTYPE_F32 ? 4 : 2;
+  if (!aligned(logits, size) || !aligned(grad_sum, size) || !aligned(grad_logits, size) ||
+      !aligned(expert_count, 4) || !aligned(live_tokens, 4) || !aligned(grad_loss, 4))
+    return MOE_EALIGN;
+  const moe::BalanceShape s = moe::balance_shape(T, E, seq_len);
+  moe::BalanceGradArgs a;
+  a.logits = logits;
+  a.pitch = logits_pitch ? logits_pitch : E;
+  a.seq = s.seq;
+  a.seqs = s.seqs;
+  a.per = s.per;
+  a.parts = s.parts;
+  a.f32 = dtype == MOE_DTYPE_F32;
+  a.E = E;
+  a.sigmoid = score == MOE_SCORE_SIGMOID;
+  a.token_mask = token_mask;
+  a.expert_count = expert_count;
+  a.live_tokens = live_tokens;
+  a.grad_loss = grad_loss;
+  a.grad_sum = grad_sum;
+  a.grad_logits = grad_logits;
+  return moe::hip_status(moe::launch_balance_backward(a, as_stream(stream)));
 }
 
 int moe_rmsnorm(const uint16_t* x, int64_t x_pitch, const void* residual, int residual_dtype,
@@ -243,6 +332,75 @@ int moe_expert_matmul(const int8_t* a, const float* a_scales, int a_scale_pitch,
   m.swiglu = swiglu;
   m.y = y;
   return moe::hip_status(moe::launch_matmul(m, as_stream(stream)));
+}
+
+int moe_quantize_mx(const uint16_t* x, int64_t x_pitch, int64_t rows, int H,
+                    const int32_t* row_src, uint8_t* q, int64_t q_pitch, uint8_t* q_scales,
+                    int64_t scale_pitch, uint16_t* values, void* stream) {
+  if (rows < 0 || rows > INT32_MAX || H < 1 || H > MOE_MAX_DEPTH || (x_pitch != 0 && x_pitch < H) ||
+      x_pitch > INT32_MAX)
+    return MOE_EINVAL;
+  if (H % MOE_MX_BLOCK != 0) return MOE_EALIGN;
+  const int64_t packed = moe::mx_scale_bytes(H);
+  if ((q_pitch != 0 && q_pitch < H / 2) || q_pitch > INT32_MAX ||
+      (scale_pitch != 0 && scale_pitch < packed) || scale_pitch > INT32_MAX)
+    return MOE_EINVAL;
+  if (x_pitch % 8 != 0 || q_pitch % 16 != 0 || scale_pitch % 4 != 0 || !aligned(x, 16) ||
+      !aligned(row_src, 4) || !aligned(q, 16) || !aligned(q_scales, 4) || !aligned(values, 16))
+    return MOE_EALIGN;
+  if (rows == 0) return MOE_OK;
+  if (!x || !q || !q_scales) return MOE_EINVAL;
+  moe::MxQuantArgs a;
+  a.x = reinterpret_cast<const uint8_t*>(x);
+  a.x_pitch = 2 * (x_pitch ? x_pitch : H);
+  a.rows = rows;
+  a.H = H;
+  a.row_src = row_src;
+  a.q = q;
+  a.q_pitch = q_pitch ? q_pitch : H / 2;
+  a.scales = q_scales;
+  a.scale_pitch = scale_pitch ? scale_pitch : packed;
+  a.values = reinterpret_cast<uint8_t*>(values);
+  return moe::hip_status(moe::launch_quantize_mx(a, as_stream(stream)));
+}
+
+int moe_expert_matmul_mx(const uint8_t* a, int a_pitch, const uint8_t* a_scales, int a_scale_pitch,
+                         int64_t rows, const uint8_t* w, const uint8_t* w_scales, int E, int N,
+                         int K, const int32_t* expert_offset, const int32_t* expert_count, int act,
+                         uint16_t* y, void* stream) {
+  if (rows < 0 || rows > INT32_MAX || E < 1 || E > MOE_MAX_EXPERTS || N < 1 || K < 1 ||
+      K > MOE_MAX_DEPTH)
+    return MOE_EINVAL;
+  if (act != MOE_ACT_NONE && act != MOE_ACT_SWIGLU) return MOE_EINVAL;
+  if ((!expert_offset && (E != 1 || expert_count)) || !w || !w_scales) return MOE_EINVAL;
+  const bool swiglu = act == MOE_ACT_SWIGLU;
+  if (K % MOE_MX_BLOCK != 0) return MOE_EALIGN;
+  const int packed = moe::mx_scale_bytes(K);
+  if ((a_pitch != 0 && a_pitch < K / 2) || a_pitch > MOE_MAX_MX_PITCH ||
+      (a_scale_pitch != 0 && a_scale_pitch < packed) || a_scale_pitch > MOE_MAX_MX_PITCH)
+    return MOE_EINVAL;
+  if (N % (swiglu ? 16 : 8) != 0 || a_pitch % 16 != 0 || a_scale_pitch % 4 != 0 || !aligned(a, 16) ||
+      !aligned(w, 16) || !aligned(y, 16) || !aligned(a_scales, 4) || !aligned(w_scales, 4) ||
+      !aligned(expert_offset, 4) || !aligned(expert_count, 4))
+    return MOE_EALIGN;
+  if (rows == 0) return MOE_OK;
+  if (!a || !a_scales || !y) return MOE_EINVAL;
+  moe::MatmulMxArgs m;
+  m.rows = rows;
+  m.E = E;
+  m.N = N;
+  m.K = K / 2;
+  m.swiglu = swiglu;
+  m.offset = expert_offset;
+  m.count = expert_count;
+  m.a = a;
+  m.a_scales = a_scales;
+  m.a_pitch = a_pitch ? a_pitch : K / 2;
+  m.a_scale_pitch = a_scale_pitch ? a_scale_pitch : packed;
+  m.w = w;
+  m.w_scales = w_scales;
+  m.y = y;
+  return moe::hip_status(moe::launch_matmul_mx(m, as_stream(stream)));
 }
 
 }  // extern "C"

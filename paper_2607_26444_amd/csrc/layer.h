@@ -1,5 +1,6 @@
-// Launchers of the layer around the exchange: routing (route.hip), RMS norm
-// and quantisation (norm.hip), the experts' products (matmul.hip).
+// Launchers of the layer around the exchange: routing (route.hip), its balance loss
+// (balance.hip), RMS norm and quantisation (norm.hip), 4-bit quantisation (mx.hip), the
+// experts' products (matmul.hip, matmul_mx.hip).
 // api_layer.hip validates arguments and calls them.
 #pragma once
 
@@ -48,6 +49,58 @@ struct RouteGradArgs {
 
 hipError_t launch_route_backward(const RouteGradArgs& a, hipStream_t stream);
 
+// Sequences of the balance loss, cut into parts of `per` tokens, and its workspace.
+struct BalanceShape {
+  int64_t seq;          // tokens of a sequence
+  int64_t seqs;
+  int64_t per;
+  int32_t parts;        // of a sequence
+  int32_t blocks;       // of 32 experts
+  size_t live_at, ticket_at, piece_at, bytes;   // 0 bytes: one part
+};
+BalanceShape balance_shape(int64_t T, int E, int64_t seq);
+
+struct BalanceArgs {
+  const void* logits;
+  int64_t pitch;        // elements
+  int64_t seq, seqs, per;
+  int32_t parts;
+  int32_t f32;
+  int32_t k;
+  int32_t E;
+  int32_t sigmoid;
+  const int32_t* topk_idx;
+  const uint8_t* token_mask;   // or null
+  int32_t* expert_count;
+  int32_t* live_tokens;
+  float* mean_score;           // or null
+  float* loss;                 // or null
+  float* partial;              // [seqs][parts]: sums, slots (part_pitch words each)
+  int32_t* part_live;          // [seqs][parts]
+  uint32_t* tickets;           // [seqs]
+  float* pieces;               // [seqs][blocks]: slots, their share of the loss
+};
+
+hipError_t launch_balance(const BalanceArgs& a, int blocks, hipStream_t stream);
+
+struct BalanceGradArgs {
+  const void* logits;
+  int64_t pitch;
+  int64_t seq, seqs, per;
+  int32_t parts;
+  int32_t f32;
+  int32_t E;
+  int32_t sigmoid;
+  const uint8_t* token_mask;
+  const int32_t* expert_count;
+  const int32_t* live_tokens;
+  const float* grad_loss;
+  const void* grad_sum;        // or null
+  void* grad_logits;
+};
+
+hipError_t launch_balance_backward(const BalanceGradArgs& a, hipStream_t stream);
+
 // 8-bit output of a row kernel.
 enum QuantKind : int32_t { kQuantNone = 0, kQuantFp8 = 1, kQuantInt8 = 2 };
 
@@ -94,23 +147,61 @@ struct NormGradArgs {
 int norm_grad_parts(int64_t rows, int H);
 hipError_t launch_norm_backward(const NormGradArgs& a, hipStream_t stream);
 
-struct MatmulArgs {
+// Sizes and windows of the experts' products, whatever their codes are.
+struct MatmulShape {
+  int64_t rows;
+  int32_t E;
+  int32_t N;
+  int32_t K;                 // bytes of a row of codes
+  int32_t swiglu;
+  const int32_t* offset;     // null: one window of all rows
+  const int32_t* count;      // null: offset[e + 1] - offset[e]
+};
+
+struct MatmulArgs : MatmulShape {
   const uint8_t* a;
   const float* a_scales;
   int32_t a_scale_pitch;
-  int32_t E;
-  int64_t rows;
   const uint8_t* w;
   const float* w_scales;
-  int32_t N;
-  int32_t K;
-  const int32_t* offset;     // null: one window of all rows
-  const int32_t* count;      // null: offset[e + 1] - offset[e]
-  int32_t swiglu;
   uint16_t* y;
 };
 
 hipError_t launch_matmul(const MatmulArgs& a, hipStream_t stream);
+
+// Microscaled 4-bit floats: two codes to a byte, a scale byte for 32 of them.
+constexpr int kMxBlock = 32;
+// Bytes of a row of scales: whole fours.
+__host__ __device__ inline int mx_scale_bytes(int values) {
+  return (values / kMxBlock + 3) / 4 * 4;
+}
+
+struct MxQuantArgs {
+  const uint8_t* x;          // bf16
+  int64_t x_pitch;           // bytes
+  int64_t rows;
+  int32_t H;
+  const int32_t* row_src;    // rows with a negative entry are skipped; or null
+  uint8_t* q;
+  int64_t q_pitch;
+  uint8_t* scales;
+  int64_t scale_pitch;
+  uint8_t* values;           // bf16, packed; or null
+};
+
+hipError_t launch_quantize_mx(const MxQuantArgs& a, hipStream_t stream);
+
+struct MatmulMxArgs : MatmulShape {
+  const uint8_t* a;
+  const uint8_t* a_scales;
+  int32_t a_pitch;           // bytes
+  int32_t a_scale_pitch;     // bytes
+  const uint8_t* w;
+  const uint8_t* w_scales;   // rows of mx_scale_bytes
+  uint16_t* y;
+};
+
+hipError_t launch_matmul_mx(const MatmulMxArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------- device
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));

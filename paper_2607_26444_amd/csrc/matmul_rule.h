@@ -18,13 +18,13 @@ constexpr int64_t kMaxTiles = INT32_MAX - 512;
 
 // Row tiles of `size` that the windows can have: each window with rows adds at
 // most one that is not full.
-inline int64_t row_tiles(const MatmulArgs& a, int size) {
+inline int64_t row_tiles(const MatmulShape& a, int size) {
   if (!a.offset) return (a.rows + size - 1) / size;
   return a.rows / size + (a.rows < a.E ? a.rows : a.E);
 }
 
 // Row tiles of `size` if the rows are spread about evenly.
-inline double even_tiles(const MatmulArgs& a, int size) {
+inline double even_tiles(const MatmulShape& a, int size) {
   const double windows = (double)(a.rows < a.E ? a.rows : a.E), n = (double)a.rows / windows / size;
   return windows * (a.E == 1 ? __builtin_ceil(n) : n > 0.8 ? n + 0.5 : 1.0);
 }
@@ -51,20 +51,20 @@ constexpr Way kWay[kWays] = {
 };
 
 // Output channels of the call, those of a way's tile, and its tiles of all windows.
-inline int out_channels(const MatmulArgs& a) { return a.swiglu ? a.N / 2 : a.N; }
-inline int tile_channels(const MatmulArgs& a, const Way& w) {
+inline int out_channels(const MatmulShape& a) { return a.swiglu ? a.N / 2 : a.N; }
+inline int tile_channels(const MatmulShape& a, const Way& w) {
   return a.swiglu ? w.channels / 2 : w.channels;
 }
-inline int pieces_of(const MatmulArgs& a, const Way& w) {
+inline int pieces_of(const MatmulShape& a, const Way& w) {
   const int per = tile_channels(a, w);
   return (out_channels(a) + per - 1) / per;
 }
-inline int64_t tiles_of(const MatmulArgs& a, const Way& w) {
+inline int64_t tiles_of(const MatmulShape& a, const Way& w) {
   return row_tiles(a, w.rows) * pieces_of(a, w);
 }
 
 // Whether a way can be launched for the call.
-inline bool way_fits(const MatmulArgs& a, int n) {
+inline bool way_fits(const MatmulShape& a, int n) {
   return tiles_of(a, kWay[n]) <= (n == kTile256 || n == kTile128 ? kMaxTiles : kMaxGroups);
 }
 
@@ -91,7 +91,7 @@ inline bool way_fits(const MatmulArgs& a, int n) {
 //   1, 1, 7168 x 4096                 25/44    14/22    11/14    10/14   5.2/11
 // The way chosen is the best of each line or within 6% of it, but for 64 rows over 8
 // experts (4.9 for 4.1).
-inline double way_time(const MatmulArgs& a, const Way& w) {
+inline double way_time(const MatmulShape& a, const Way& w) {
   const double groups = even_tiles(a, w.rows) * pieces_of(a, w);
   const double full = groups / w.resident;
   const double rounds = full < 1.0 ? 1.0 : full + 0.75 * (__builtin_ceil(full) - full);
@@ -102,7 +102,7 @@ inline double way_time(const MatmulArgs& a, const Way& w) {
 }
 
 // The way that takes least of those that can be launched; kWays if none can be.
-inline int choose_way(const MatmulArgs& a) {
+inline int choose_way(const MatmulShape& a) {
   int best = kWays;
   double least = 0.0;
   for (int n = 0; n < kWays; ++n) {

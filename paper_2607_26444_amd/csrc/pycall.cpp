@@ -40,7 +40,8 @@ PyObject* g_get_stream;       // (index) -> address of its current stream
 // all the same, and that call raises.
 #define MOE_LAYER_CALLS(X)                                                       \
   X(moe_route) X(moe_route_backward) X(moe_rmsnorm) X(moe_rmsnorm_backward)      \
-  X(moe_quantize) X(moe_expert_matmul)
+  X(moe_quantize) X(moe_expert_matmul) X(moe_balance) X(moe_balance_backward)      \
+  X(moe_quantize_mx) X(moe_expert_matmul_mx)
 #define X(name) decltype(&name) f_##name;
 MOE_CALLS(X)
 MOE_LAYER_CALLS(X)
@@ -508,6 +509,97 @@ PyObject* expert_matmul(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+PyObject* balance(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_balance, "moe_balance")) return nullptr;
+  Args a(args, n);
+  a.expect(14);
+  const void* x = a.ptr<const void>();
+  const int dtype = a.i32(), E = a.i32();
+  int64_t T;
+  int k;
+  const int32_t* idx = a.table(T, k);
+  const uint8_t* mask = a.ptr<const uint8_t>();
+  int32_t* count = a.ptr<int32_t>();
+  int32_t* live = a.ptr<int32_t>();
+  float* mean = a.ptr<float>();
+  float* loss = a.ptr<float>();
+  size_t bytes;
+  void* ws = a.workspace(bytes, true);
+  const int score = a.i32();
+  const int64_t seq = a.i64();
+  void* stream = a.stream();
+  const int64_t pitch = a.i64();
+  return finish(a, [&] {
+    return f_moe_balance(x, dtype, pitch, T, k, E, score, seq, idx, mask, count, live, mean, loss, ws,
+                         bytes, stream);
+  });
+}
+
+PyObject* balance_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_balance_backward, "moe_balance_backward")) return nullptr;
+  Args a(args, n);
+  a.expect(14);
+  const void* x = a.ptr<const void>();
+  const int dtype = a.i32();
+  const int64_t T = a.i64();
+  const int E = a.i32();
+  const uint8_t* mask = a.ptr<const uint8_t>();
+  const int32_t* count = a.ptr<const int32_t>();
+  const int32_t* live = a.ptr<const int32_t>();
+  const float* gl = a.ptr<const float>();
+  const void* gs = a.ptr<const void>();
+  void* gx = a.ptr<void>();
+  const int score = a.i32();
+  const int64_t seq = a.i64();
+  void* stream = a.stream();
+  const int64_t pitch = a.i64();
+  return finish(a, [&] {
+    return f_moe_balance_backward(x, dtype, pitch, T, E, score, seq, mask, count, live, gl, gs, gx,
+                                  stream);
+  });
+}
+
+PyObject* quantize_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_quantize_mx, "moe_quantize_mx")) return nullptr;
+  Args a(args, n);
+  a.expect(11);
+  const uint16_t* x = a.ptr<const uint16_t>();
+  const int64_t rows = a.i64();
+  const int H = a.i32();
+  uint8_t* q = a.ptr<uint8_t>();
+  uint8_t* scales = a.ptr<uint8_t>();
+  uint16_t* values = a.ptr<uint16_t>();
+  const int32_t* src = a.ptr<const int32_t>();
+  const int64_t q_pitch = a.i64(), s_pitch = a.i64();
+  void* stream = a.stream();
+  const int64_t pitch = a.i64();
+  return finish(a, [&] {
+    return f_moe_quantize_mx(x, pitch, rows, H, src, q, q_pitch, scales, s_pitch, values, stream);
+  });
+}
+
+PyObject* expert_matmul_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!present(f_moe_expert_matmul_mx, "moe_expert_matmul_mx")) return nullptr;
+  Args a(args, n);
+  a.expect(15);
+  const uint8_t* x = a.ptr<const uint8_t>();
+  const uint8_t* xs = a.ptr<const uint8_t>();
+  const int64_t rows = a.i64();
+  const uint8_t* w = a.ptr<const uint8_t>();
+  const uint8_t* ws = a.ptr<const uint8_t>();
+  const int E = a.i32(), N = a.i32(), K = a.i32();
+  const int32_t* offset = a.ptr<const int32_t>();
+  const int32_t* count = a.ptr<const int32_t>();
+  const int act = a.i32();
+  uint16_t* y = a.ptr<uint16_t>();
+  void* stream = a.stream();
+  const int pitch = a.i32(), s_pitch = a.i32();
+  return finish(a, [&] {
+    return f_moe_expert_matmul_mx(x, pitch, xs, s_pitch, rows, w, ws, E, N, K, offset, count, act, y,
+                                  stream);
+  });
+}
+
 // init(lib_path, argument_error, c_int, get_device, get_stream): binds the
 // entry points of the libmoe.so that is already loaded.
 PyObject* init(PyObject*, PyObject* args) {
@@ -559,6 +651,10 @@ PyMethodDef methods[] = {
     FAST("rmsnorm_backward", rmsnorm_backward),
     FAST("quantize", quantize),
     FAST("expert_matmul", expert_matmul),
+    FAST("balance", balance),
+    FAST("balance_backward", balance_backward),
+    FAST("quantize_mx", quantize_mx),
+    FAST("expert_matmul_mx", expert_matmul_mx),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_moecall", nullptr, -1, methods,

@@ -1,19 +1,21 @@
-"""One MoE layer in 8-bit integers, made of the library's calls.
+"""One MoE layer in 8-bit integers or 4-bit floats, made of the library's calls.
 
-    residual addition + RMS norm (bf16 and int8 rows)   moe_rmsnorm
-    experts and weights of each token                   moe_route
-    placement                                           moe_layout
-    int8 rows and their scales to the experts' windows  moe_dispatch
-    gate and up products, SwiGLU                        moe_expert_matmul
-    int8 rows of the result                             moe_quantize
-    down product                                        moe_expert_matmul
-    weighted sum in token order                         moe_combine
+    int8 weights                                        4-bit weights
+    residual addition + RMS norm (bf16 and int8 rows)   (bf16 rows)           moe_rmsnorm
+    experts and weights of each token                                         moe_route
+    placement                                                                 moe_layout
+                                                        4-bit rows            moe_quantize_mx
+    int8 rows and their scales to the experts' windows  (4-bit rows)          moe_dispatch
+    gate and up products, SwiGLU: moe_expert_matmul                           moe_expert_matmul_mx
+    int8 rows of the result: moe_quantize               (4-bit rows)          moe_quantize_mx
+    down product: moe_expert_matmul                                           moe_expert_matmul_mx
+    weighted sum in token order                                               moe_combine
 
 `MoeLayer` keeps the weights and the buffers of one batch shape; `forward`
 enqueues the calls on a stream and allocates nothing, so that it can be
 captured in a graph.  One GPU holds all experts (one rank).
 
-python -m paper_2607_26444_amd.layer [--tokens N ...] runs it on random inputs.
+python -m paper_2607_26444_amd.layer [--tokens N ...] [--mx] runs it on random inputs.
 """
 from __future__ import annotations
 
@@ -34,18 +36,32 @@ class MoeLayer:
 
     norm_weight [H] (bf16 or float32); w13 [E, 2I, H] int8, gate channels before
     up channels, w13_scale [E, 2I] float32; w2 [E, H, I] int8, w2_scale [E, H].
+    Or 4-bit floats as moe_quantize_mx leaves them (H and I multiples of 32): w13
+    [E, 2I, H/2] uint8, w13_scale [E, 2I, mx_scale_bytes(H)] uint8, w2 [E, H, I/2],
+    w2_scale [E, H, mx_scale_bytes(I)]; the rows are then rounded to 4 bits as well.
     The routing's options are those of moe_route.
     """
 
     def __init__(self, T, H, I, E, k, norm_weight, w13, w13_scale, w2, w2_scale, bias=None,
                  eps=1e-6, score=moe.MOE_SCORE_SOFTMAX, groups=1, top_groups=1, group_top=1,
                  renorm=True, scale=1.0, device="cuda"):
-        if H % BLOCK or I % 16:
-            raise ValueError(f"H has to be a multiple of {BLOCK} and I of 16")
-        for name, t, shape, dtype in (("w13", w13, (E, 2 * I, H), torch.int8),
-                                      ("w13_scale", w13_scale, (E, 2 * I), torch.float32),
-                                      ("w2", w2, (E, H, I), torch.int8),
-                                      ("w2_scale", w2_scale, (E, H), torch.float32),
+        self.mx = w13.dtype == torch.uint8
+        if self.mx:
+            if H % moe.MOE_MX_BLOCK or I % moe.MOE_MX_BLOCK:
+                raise ValueError(f"H and I have to be multiples of {moe.MOE_MX_BLOCK}")
+            cols, inner_cols = moe.mx_scale_bytes(H), moe.mx_scale_bytes(I)
+            weights = (("w13", w13, (E, 2 * I, H // 2), torch.uint8),
+                       ("w13_scale", w13_scale, (E, 2 * I, cols), torch.uint8),
+                       ("w2", w2, (E, H, I // 2), torch.uint8),
+                       ("w2_scale", w2_scale, (E, H, inner_cols), torch.uint8))
+        else:
+            if H % BLOCK or I % 16:
+                raise ValueError(f"H has to be a multiple of {BLOCK} and I of 16")
+            weights = (("w13", w13, (E, 2 * I, H), torch.int8),
+                       ("w13_scale", w13_scale, (E, 2 * I), torch.float32),
+                       ("w2", w2, (E, H, I), torch.int8),
+                       ("w2_scale", w2_scale, (E, H), torch.float32))
+        for name, t, shape, dtype in (*weights,
                                       ("norm_weight", norm_weight, (H,), norm_weight.dtype),
                                       ("bias", bias, (E,), torch.float32)):
             if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or
@@ -57,22 +73,33 @@ class MoeLayer:
         self.bias = bias
         self.options = dict(score=score, groups=groups, top_groups=top_groups,
                             group_top=group_top, renorm=renorm, scale=scale)
-        rows, cols = max(1, T * k), H // BLOCK
+        rows = max(1, T * k)
 
         def buf(*shape, dtype=torch.bfloat16):
             return torch.empty(*shape, dtype=dtype, device=device)
         self.sum, self.normed = buf(T, H), buf(T, H)
-        self.q, self.q_scale = buf(T, H, dtype=torch.int8), buf(T, cols, dtype=torch.float32)
+        if self.mx:
+            # a row's scales behind its codes, so that dispatch carries both as one row
+            self.row_bytes = -(-(H // 2 + cols) // 16) * 16
+            self.q = buf(T, self.row_bytes, dtype=torch.uint8)
+            self.rows = buf(rows, self.row_bytes, dtype=torch.uint8)
+            self.q_scale, self.row_scale = self.q[:, H // 2:], self.rows[:, H // 2:]
+            self.act_q = buf(rows, I // 2, dtype=torch.uint8)
+            self.act_scale = buf(rows, inner_cols, dtype=torch.uint8)
+        else:
+            cols = H // BLOCK
+            self.q, self.q_scale = buf(T, H, dtype=torch.int8), buf(T, cols, dtype=torch.float32)
+            self.rows = buf(rows, H, dtype=torch.int8)
+            self.row_scale = buf(rows, cols, dtype=torch.float32)
+            self.act_q = buf(rows, I, dtype=torch.int8)
+            self.act_scale = buf(rows, dtype=torch.float32)
         self.topk_idx = buf(T, k, dtype=torch.int32)
         self.topk_w = buf(T, k, dtype=torch.float32)
         self.layout = moe.Layout(T, k, E, 1, device=device)
-        # one rank: its regions are the tensors themselves
-        self.rows = buf(rows, H, dtype=torch.int8)
-        self.row_scale = buf(rows, cols, dtype=torch.float32)
         self.act = buf(rows, I)
-        self.act_q, self.act_scale = buf(rows, I, dtype=torch.int8), buf(rows, dtype=torch.float32)
         self.out = buf(rows, H)
         self.y = buf(T, H)
+        # one rank: its regions are the tensors themselves
         tables = [t.data_ptr() for t in (self.rows, self.row_scale, self.out)]
         self.tables = torch.tensor(tables, dtype=torch.int64, device=device)
         self.row_table, self.scale_table, self.out_table = self.tables.split(1)
@@ -90,10 +117,16 @@ class MoeLayer:
             if tuple(t.shape) != (T, H) or t.dtype != torch.bfloat16 or not t.is_contiguous():
                 raise ValueError(f"{name}: a contiguous bfloat16 tensor of shape {(T, H)} is needed")
         lay, rows = self.layout, T * self.k
-        moe.moe_rmsnorm(x, residual, moe.MOE_DTYPE_BF16, self.norm_weight, self.weight_dtype,
-                        self.eps, T, H, self.sum, self.normed if callable(logits) else None,
-                        moe.MOE_DTYPE_INT8, self.q, self.q_scale, None, self.q_scale.shape[1],
-                        stream)
+        if self.mx:
+            moe.moe_rmsnorm(x, residual, moe.MOE_DTYPE_BF16, self.norm_weight, self.weight_dtype,
+                            self.eps, T, H, self.sum, self.normed, 0, None, None, None, 0, stream)
+            moe.moe_quantize_mx(self.normed, T, H, self.q, self.q_scale, q_pitch=self.row_bytes,
+                                scale_pitch=self.row_bytes, stream=stream)
+        else:
+            moe.moe_rmsnorm(x, residual, moe.MOE_DTYPE_BF16, self.norm_weight, self.weight_dtype,
+                            self.eps, T, H, self.sum, self.normed if callable(logits) else None,
+                            moe.MOE_DTYPE_INT8, self.q, self.q_scale, None, self.q_scale.shape[1],
+                            stream)
         if callable(logits):
             with _current(stream):
                 logits = logits(self.normed)
@@ -109,17 +142,31 @@ class MoeLayer:
         moe.moe_route(logits, _dtype(logits), E, self.bias, token_mask, self.topk_idx,
                       self.topk_w, stream=stream, logits_pitch=pitch, **self.options)
         lay.run(self.topk_idx, stream)
-        moe.moe_dispatch(self.q, self.q_scale, moe.MOE_DTYPE_FP8_E4M3, H, E, 1, self.topk_idx,
-                         lay.pos, lay.rank_offset, self.row_table, self.scale_table, self.cap,
-                         lay.workspace, lay.status, stream)
-        moe.moe_expert_matmul(self.rows, self.row_scale, rows, self.w13, self.w13_scale, E, 2 * I,
-                              H, lay.expert_offset, lay.expert_count, moe.MOE_ACT_SWIGLU, self.act,
-                              stream, self.row_scale.shape[1])
-        moe.moe_quantize(self.act, rows, I, moe.MOE_DTYPE_INT8, self.act_q, self.act_scale,
-                         lay.row_src, 1, stream)
-        moe.moe_expert_matmul(self.act_q, self.act_scale, rows, self.w2, self.w2_scale, E, H, I,
-                              lay.expert_offset, lay.expert_count, moe.MOE_ACT_NONE, self.out,
-                              stream)
+        if self.mx:
+            moe.moe_dispatch(self.q, None, moe.MOE_DTYPE_BF16, self.row_bytes // 2, E, 1,
+                             self.topk_idx, lay.pos, lay.rank_offset, self.row_table, None, self.cap,
+                             lay.workspace, lay.status, stream)
+            moe.moe_expert_matmul_mx(self.rows, self.row_scale, rows, self.w13, self.w13_scale, E,
+                                     2 * I, H, lay.expert_offset, lay.expert_count,
+                                     moe.MOE_ACT_SWIGLU, self.act, stream, self.row_bytes,
+                                     self.row_bytes)
+            moe.moe_quantize_mx(self.act, rows, I, self.act_q, self.act_scale, row_src=lay.row_src,
+                                stream=stream)
+            moe.moe_expert_matmul_mx(self.act_q, self.act_scale, rows, self.w2, self.w2_scale, E, H,
+                                     I, lay.expert_offset, lay.expert_count, moe.MOE_ACT_NONE,
+                                     self.out, stream)
+        else:
+            moe.moe_dispatch(self.q, self.q_scale, moe.MOE_DTYPE_FP8_E4M3, H, E, 1, self.topk_idx,
+                             lay.pos, lay.rank_offset, self.row_table, self.scale_table, self.cap,
+                             lay.workspace, lay.status, stream)
+            moe.moe_expert_matmul(self.rows, self.row_scale, rows, self.w13, self.w13_scale, E, 2 * I,
+                                  H, lay.expert_offset, lay.expert_count, moe.MOE_ACT_SWIGLU, self.act,
+                                  stream, self.row_scale.shape[1])
+            moe.moe_quantize(self.act, rows, I, moe.MOE_DTYPE_INT8, self.act_q, self.act_scale,
+                             lay.row_src, 1, stream)
+            moe.moe_expert_matmul(self.act_q, self.act_scale, rows, self.w2, self.w2_scale, E, H, I,
+                                  lay.expert_offset, lay.expert_count, moe.MOE_ACT_NONE, self.out,
+                                  stream)
         moe.moe_combine(self.out_table, self.topk_w, H, E, 1, self.topk_idx, lay.pos,
                         lay.rank_offset, self.cap, self.y, lay.workspace, lay.status, stream)
         return self.y
@@ -144,12 +191,19 @@ def _dtype(t):
     raise ValueError(f"bfloat16 or float32 is needed, not {t.dtype}")
 
 
-def random_layer(T, H, I, E, k, seed=0, **options):
-    """A layer with weights of about unit gain."""
+def random_layer(T, H, I, E, k, seed=0, mx=False, **options):
+    """A layer with weights of about unit gain; mx: in 4-bit floats."""
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
 
     def weights(n, depth):
+        if mx:
+            q = torch.empty(E, n, depth // 2, dtype=torch.uint8, device="cuda")
+            scales = torch.empty(E, n, moe.mx_scale_bytes(depth), dtype=torch.uint8, device="cuda")
+            for e in range(E):
+                w = torch.randn(n, depth, generator=g, device="cuda") / depth ** 0.5
+                moe.moe_quantize_mx(w.bfloat16(), n, depth, q[e], scales[e])
+            return q, scales
         w = torch.randint(-127, 128, (E, n, depth), generator=g, device="cuda", dtype=torch.int8)
         return w, (0.5 + torch.rand(E, n, generator=g, device="cuda")) / (73.0 * depth ** 0.5)
     norm = (1 + 0.2 * torch.randn(H, generator=g, device="cuda")).bfloat16()
@@ -164,8 +218,9 @@ def main(argv=None):
     ap.add_argument("--experts", type=int, default=32)
     ap.add_argument("--topk", type=int, default=8)
     ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--mx", action="store_true", help="4-bit floats instead of 8-bit integers")
     a = ap.parse_args(argv)
-    layer = random_layer(a.tokens, a.hidden, a.inner, a.experts, a.topk,
+    layer = random_layer(a.tokens, a.hidden, a.inner, a.experts, a.topk, mx=a.mx,
                          score=moe.MOE_SCORE_SIGMOID)
     g = torch.Generator(device="cuda")
     g.manual_seed(1)

@@ -54,6 +54,8 @@ MOE_ACT_SWIGLU = 1
 MOE_MAX_GROUPS = 64
 MOE_MAX_ROW = 16384
 MOE_MAX_DEPTH = 131056
+MOE_MX_BLOCK = 32
+MOE_MAX_MX_PITCH = 1048576
 
 # Entry points declared in include/moe.h.
 EXPORTS = ("moe_version", "moe_strerror", "moe_last_hip_error", "moe_wall_clock_khz",
@@ -63,7 +65,8 @@ EXPORTS = ("moe_version", "moe_strerror", "moe_last_hip_error", "moe_wall_clock_
            "moe_expand", "moe_combine_local", "moe_combine_dedup", "moe_layout_scratch",
            "moe_route", "moe_route_backward", "moe_rmsnorm",
            "moe_rmsnorm_backward_workspace_bytes", "moe_rmsnorm_backward", "moe_quantize",
-           "moe_expert_matmul")
+           "moe_expert_matmul", "moe_balance_workspace_bytes", "moe_balance",
+           "moe_balance_backward", "moe_quantize_mx", "moe_expert_matmul_mx")
 
 _lib = None
 P = ctypes.c_void_p
@@ -129,9 +132,15 @@ def lib() -> ctypes.CDLL:
         L.moe_rmsnorm_backward.argtypes = [P, P, I32, P, P, I32, P, I64, I32, P, P, P, SZ, P]
         L.moe_quantize.argtypes = [P, I64, I64, I32, P, I32, P, P, I32, P]
         L.moe_expert_matmul.argtypes = [P, P, I32, I64, P, P, I32, I32, I32, P, P, I32, P, P]
+        L.moe_balance_workspace_bytes.argtypes = [I64, I32, I64, ctypes.POINTER(SZ)]
+        L.moe_balance.argtypes = [P, I32, I64, I64, I32, I32, I32, I64, P, P, P, P, P, P, P, SZ, P]
+        L.moe_balance_backward.argtypes = [P, I32, I64, I64, I32, I32, I64, P, P, P, P, P, P, P]
+        L.moe_quantize_mx.argtypes = [P, I64, I64, I32, P, P, I64, P, I64, P, P]
+        L.moe_expert_matmul_mx.argtypes = [P, I32, P, I32, I64, P, P, I32, I32, I32, P, P, I32, P, P]
         for f in ("moe_route", "moe_route_backward", "moe_rmsnorm",
                   "moe_rmsnorm_backward_workspace_bytes", "moe_rmsnorm_backward",
-                  "moe_quantize", "moe_expert_matmul"):
+                  "moe_quantize", "moe_expert_matmul", "moe_balance_workspace_bytes", "moe_balance",
+                  "moe_balance_backward", "moe_quantize_mx", "moe_expert_matmul_mx"):
             getattr(L, f).restype = I32
         for f in ("moe_layout_scratch", "moe_layout_workspace_bytes", "moe_layout", "moe_layout_fixed", "moe_dispatch",
                   "moe_dispatch_ex", "moe_combine", "moe_combine_ex", "moe_expert_scale",
@@ -411,6 +420,57 @@ def moe_expert_matmul(a, a_scales, rows, w, w_scales, E, N, K, expert_offset, ex
         a_scale_pitch)
     if rc:
         _check("moe_expert_matmul", rc)
+
+
+def moe_balance_workspace_bytes(T: int, E: int, seq_len: int = 0) -> int:
+    out = SZ(0)
+    _check("moe_balance_workspace_bytes",
+           lib().moe_balance_workspace_bytes(T, E, seq_len, ctypes.byref(out)))
+    return out.value
+
+
+def moe_balance(logits, dtype, E, topk_idx, token_mask, expert_count, live_tokens, mean_score,
+                loss, workspace, score=MOE_SCORE_SOFTMAX, seq_len=0, stream=None,
+                logits_pitch=0):
+    """Slots of each expert, mean scores and balance loss of every sequence of
+    topk_idx [T,k] (which sets T and k)."""
+    rc = (_fast or _calls()).balance(
+        logits, dtype, E, topk_idx, token_mask, expert_count, live_tokens, mean_score, loss,
+        workspace, score, seq_len, stream, logits_pitch)
+    if rc:
+        _check("moe_balance", rc)
+
+
+def moe_balance_backward(logits, dtype, T, E, token_mask, expert_count, live_tokens, grad_loss,
+                         grad_sum, grad_logits, score=MOE_SCORE_SOFTMAX, seq_len=0, stream=None,
+                         logits_pitch=0):
+    rc = (_fast or _calls()).balance_backward(
+        logits, dtype, T, E, token_mask, expert_count, live_tokens, grad_loss, grad_sum,
+        grad_logits, score, seq_len, stream, logits_pitch)
+    if rc:
+        _check("moe_balance_backward", rc)
+
+
+def mx_scale_bytes(H: int) -> int:
+    """Bytes of a packed row of scales of H 4-bit values: whole words."""
+    return -(-H // (4 * MOE_MX_BLOCK)) * 4
+
+
+def moe_quantize_mx(x, rows, H, q, q_scales, values=None, row_src=None, q_pitch=0, scale_pitch=0,
+                    stream=None, x_pitch=0):
+    rc = (_fast or _calls()).quantize_mx(
+        x, rows, H, q, q_scales, values, row_src, q_pitch, scale_pitch, stream, x_pitch)
+    if rc:
+        _check("moe_quantize_mx", rc)
+
+
+def moe_expert_matmul_mx(a, a_scales, rows, w, w_scales, E, N, K, expert_offset, expert_count, act,
+                         y, stream=None, a_pitch=0, a_scale_pitch=0):
+    rc = (_fast or _calls()).expert_matmul_mx(
+        a, a_scales, rows, w, w_scales, E, N, K, expert_offset, expert_count, act, y, stream,
+        a_pitch, a_scale_pitch)
+    if rc:
+        _check("moe_expert_matmul_mx", rc)
 
 
 # ------------------------------------------------------------ buffer plumbing

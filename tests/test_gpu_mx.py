@@ -1,0 +1,488 @@
+"""Microscaled 4-bit floats: quantisation and the experts' products against 64 bits, and the
+MoE layer that runs them.
+
+Quantisation is exact arithmetic up to its one rounding: codes, scales and values have to
+be equal.  Products of values on a narrow grid have sums that float32 holds, so they have to be
+equal but for the rounding to bf16 (2^-8 of the value at most); others may be off by
+mx_ref.matmul's bound besides.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import layer_ref  # noqa: E402
+import mx_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+BF16 = 2.0 ** -8
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _moe():
+    from paper_2607_26444_amd import moe
+    return moe
+
+
+def _gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+# ------------------------------------------------------------ quantisation
+def _quantize(x, rows=None, src=None, x_pitch=0, q_pitch=0, scale_pitch=0, values=True, H=None):
+    moe = _moe()
+    rows, H = rows if rows is not None else x.shape[0], H or x.shape[1]
+    n = max(1, rows)
+    q = torch.full((n, q_pitch or H // 2), 0xA5, dtype=torch.uint8, device="cuda")
+    s = torch.full((n, scale_pitch or ref.scale_cols(H)), 0x5A, dtype=torch.uint8, device="cuda")
+    v = torch.full((n, H), 77.0, dtype=torch.bfloat16, device="cuda") if values else None
+    moe.moe_quantize_mx(x.cuda(), rows, H, q, s, values=v, q_pitch=q_pitch, scale_pitch=scale_pitch,
+                        x_pitch=x_pitch,
+                        row_src=None if src is None else torch.tensor(src, dtype=torch.int32).cuda())
+    torch.cuda.synchronize()
+    return q.cpu(), s.cpu(), None if v is None else v.cpu()
+
+
+def _check_quantized(got, x):
+    q, s, v = got
+    H = x.shape[1]
+    wq, ws, wv = ref.quantize(x)
+    assert torch.equal(s[:, :ws.shape[1]], ws)
+    ok = (ws[:, :H // 32] != 255).repeat_interleave(16, 1)       # codes of marked blocks say nothing
+    assert torch.equal(q[:, :H // 2][ok], wq[ok])
+    if v is not None:
+        wv = wv.bfloat16()                                       # exact
+        assert torch.equal(torch.isnan(v), torch.isnan(wv))
+        at = ~torch.isnan(wv)
+        assert torch.equal(v.view(torch.int16)[at], wv.view(torch.int16)[at])
+
+
+def _rows(rows, H, seed):
+    g = _gen(seed)
+    x = torch.randn(rows, H, generator=g) * torch.exp(4 * torch.randn(rows, 1, generator=g))
+    return x.bfloat16()
+
+
+@pytest.mark.parametrize("H", [32, 64, 96, 128, 160, 480, 512, 544, 1024, 1056, 2080, 7168])
+@pytest.mark.parametrize("rows", [1, 3, 130])
+def test_quantize(rows, H):
+    x = _rows(rows, H, seed=rows * H)
+    _check_quantized(_quantize(x), x)
+
+
+def test_quantize_every_bf16_pattern():
+    """Each pattern as the largest of a block, beside the ties of every step, values over a
+    border and under it, the smallest ones, both zeros."""
+    u = torch.arange(0x8000, dtype=torch.int32)
+    x = torch.zeros(0x8000, 32, dtype=torch.int32)
+    x[:, 0] = u
+    exponent = (u & 0x7F80).clamp(max=0x7F00)
+    below = [0.25, 0.5, 0.75, 1.0, 1.25, 1.5, 1.75, 2.0, 2.5, 3.0, 3.5]      # of 4 units
+    top = exponent.to(torch.int16).view(torch.bfloat16).float()
+    for n, b in enumerate(below):
+        for sign in (0, 1):
+            v = (top * (b / 4)).bfloat16().view(torch.int16).int() & 0x7FFF
+            x[:, 1 + 2 * n + sign] = torch.minimum(v, u) | sign << 15
+    x[:, 24], x[:, 25] = u.clamp(max=1), 0x8000
+    x[:, 26] = (u - 1).clamp(min=0)
+    x[:, 27] = (u - 1).clamp(min=0) | 0x8000
+    x[:, 31] = u | 0x8000
+    x = torch.where(x > 0x7FFF, x - 0x10000, x).to(torch.int16).view(torch.bfloat16)
+    _check_quantized(_quantize(x.reshape(0x8000 // 4, 128)), x.reshape(0x8000 // 4, 128))
+
+
+def test_quantize_special_blocks():
+    x = torch.ones(6, 96).bfloat16()
+    x[0, 40], x[1, 33], x[2, 95] = math.nan, math.inf, -math.inf
+    x[3, 32:64], x[4, :32] = 0.0, -0.0
+    x[5] = 2.0 ** -133
+    q, s, v = _quantize(x)
+    _check_quantized((q, s, v), x)
+    assert s[0].tolist() == [125, 255, 125, 0] and s[3].tolist() == [125, 127, 125, 0]
+    assert torch.all(torch.isnan(v[1, 32:64])) and torch.all(v[1, :32] == 1)
+    assert torch.all(q[4, :16] == 0x88)
+
+
+@pytest.mark.parametrize("H", [32, 160, 2080])
+def test_quantize_pitches_and_skipped_rows(H):
+    """Rows in wider ones; rows that are skipped and bytes between rows stay."""
+    rows, moe = 21, _moe()
+    x = _rows(rows, H, seed=H)
+    wide = torch.full((rows, H + 24), math.nan).bfloat16()
+    wide[:, :H] = x
+    src = [-1 if r % 4 == 2 else r for r in range(rows)]
+    qp, sp = H // 2 + 48, ref.scale_cols(H) + 8
+    q, s, v = _quantize(wide, src=src, x_pitch=H + 24, q_pitch=qp, scale_pitch=sp, H=H)
+    keep = torch.tensor(src) >= 0
+    _check_quantized((q[keep], s[keep], v[keep]), x[keep])
+    assert torch.all(q[~keep] == 0xA5) and torch.all(s[~keep] == 0x5A) and torch.all(v[~keep] == 77)
+    assert torch.all(q[:, H // 2:] == 0xA5) and torch.all(s[:, ref.scale_cols(H):] == 0x5A)
+    assert torch.equal(_quantize(wide, src=src, x_pitch=H + 24, q_pitch=qp, scale_pitch=sp, H=H,
+                                 values=False)[0], q)
+    moe.moe_quantize_mx(None, 0, H, None, None)
+
+
+def test_quantize_codes_and_scales_in_one_row():
+    """The form that moe_dispatch carries: scales behind the codes, one pitch."""
+    moe, H, rows = _moe(), 224, 50
+    pitch = -(-(H // 2 + ref.scale_cols(H)) // 16) * 16
+    x = _rows(rows, H, seed=3)
+    buf = torch.full((rows, pitch), 0xA5, dtype=torch.uint8, device="cuda")
+    moe.moe_quantize_mx(x.cuda(), rows, H, buf, buf[:, H // 2:], q_pitch=pitch, scale_pitch=pitch)
+    end = H // 2 + ref.scale_cols(H)
+    got = buf.cpu()
+    _check_quantized((got[:, :H // 2], got[:, H // 2:end], None), x)
+    assert torch.all(got[:, end:] == 0xA5)
+
+
+def test_quantize_more_rows_than_one_grid():
+    """More wavefronts' work than the largest grid has; offsets past 2^32 bytes."""
+    moe, H = _moe(), 512
+    rows = 4_400_000
+    x = torch.zeros(rows, H, dtype=torch.bfloat16, device="cuda")
+    x[-9:] = _rows(9, H, seed=1).cuda()
+    x[:5] = x[-5:]
+    q = torch.full((rows, H // 2), 0xA5, dtype=torch.uint8, device="cuda")
+    s = torch.zeros(rows, H // 32, dtype=torch.uint8, device="cuda")
+    moe.moe_quantize_mx(x, rows, H, q, s)
+    _check_quantized((q[-9:].cpu(), s[-9:].cpu(), None), x[-9:].cpu())
+    assert torch.equal(q[:5], q[-5:]) and not torch.any(q[5:-9]) and torch.all(s[5:-9] == 127)
+
+
+# ---------------------------------------------------------------- products
+def _codes(rows, K, g, lo=126, hi=128):
+    """Random codes and scale bytes of [lo, hi]; what fills the rows of scales is 255."""
+    q = torch.randint(0, 256, (rows, K // 2), generator=g, dtype=torch.uint8)
+    s = torch.full((rows, ref.scale_cols(K)), 255, dtype=torch.uint8)
+    s[:, :K // 32] = torch.randint(lo, hi + 1, (rows, K // 32), generator=g, dtype=torch.uint8)
+    return q, s
+
+
+def _inputs(rows, E, N, K, seed, lo=126, hi=128):
+    g = _gen(seed)
+    a, w = _codes(rows, K, g, lo, hi), _codes(E * N, K, g, lo, hi)
+    return a, tuple(t.view(E, N, -1) for t in w)
+
+
+def _run(a, w, offset, count, swiglu, rows=None):
+    moe = _moe()
+    E, N, half = w[0].shape
+    y = torch.full((max(1, a[0].shape[0]), N // 2 if swiglu else N), math.nan, dtype=torch.bfloat16,
+                   device="cuda")
+    dev = [None if t is None else torch.tensor(t, dtype=torch.int32, device="cuda")
+           for t in (offset, count)]
+    moe.moe_expert_matmul_mx(a[0].cuda(), a[1].cuda(), a[0].shape[0] if rows is None else rows,
+                             w[0].cuda(), w[1].cuda(), E, N, 2 * half, *dev,
+                             moe.MOE_ACT_SWIGLU if swiglu else moe.MOE_ACT_NONE, y)
+    torch.cuda.synchronize()
+    return y.cpu()[:a[0].shape[0]]
+
+
+def _check(y, a, w, windows, swiglu, exact=True):
+    K = 2 * w[0].shape[2]
+    want, tol = ref.matmul(ref.decode(*a, K), ref.decode(*w, K), windows, swiglu)
+    if exact and not swiglu:
+        tol.zero_()
+    y = y.double()
+    assert torch.equal(torch.isnan(y), torch.isnan(want))        # rows of no window are untouched
+    at = ~torch.isnan(want)
+    assert torch.all((y[at] - want[at]).abs() <= BF16 * (want[at].abs() + tol[at]) + tol[at])
+
+
+def _packed(counts):
+    offset = [0]
+    for n in counts:
+        offset.append(offset[-1] + n)
+    return offset, list(zip(offset, counts))
+
+
+# Values are multiples of a quarter at most 12 in size: sums of up to 4608 products are
+# multiples of 1/16 under 2^20 / 1.5, which float32 holds.
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 33, 64, 100, 129, 257, 300])
+@pytest.mark.parametrize("N,K", [(8, 32), (16, 64), (72, 96), (64, 128), (200, 288), (264, 1056)])
+def test_plain_product(rows, N, K):
+    a, w = _inputs(rows, 1, N, K, seed=rows + N + K)
+    _check(_run(a, w, None, None, False), a, w, [(0, rows)], False)
+
+
+@pytest.mark.parametrize("N,K", [(16, 32), (32, 64), (80, 288), (256, 128), (528, 416)])
+@pytest.mark.parametrize("rows", [1, 31, 140, 270])
+def test_swiglu(rows, N, K):
+    a, w = _inputs(rows, 1, N, K, seed=rows * N, lo=123, hi=125)
+    _check(_run(a, w, None, None, True), a, w, [(0, rows)], True)
+
+
+@pytest.mark.parametrize("rows,N,K", [(1, 264, 4128), (40, 72, 2080), (300, 264, 7168)])
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_scales_of_any_size(rows, N, K, swiglu):
+    N = N // 16 * 16 if swiglu else N
+    a, w = _inputs(rows, 1, N, K, seed=rows + K, lo=112, hi=124)
+    _check(_run(a, w, None, None, swiglu), a, w, [(0, rows)], swiglu, exact=False)
+
+
+def test_scales_at_the_ends():
+    """Scales of 2^-127 and 2^127 that meet, and products below float32's normal range beside
+    ordinary ones."""
+    q = torch.full((1, 64), 0x22, dtype=torch.uint8)             # ones
+    a = (q.repeat(4, 1), torch.tensor([[0, 254, 127, 0], [127] * 4, [254, 0, 127, 127], [0, 0, 127, 0]],
+                                      dtype=torch.uint8))
+    w = (q.repeat(8, 1).view(1, 8, 64), torch.tensor([[254, 0, 127, 0]] * 4 + [[127] * 4] * 4,
+                                                     dtype=torch.uint8).view(1, 8, 4))
+    y = _run(a, w, None, None, False).double()
+    want, _ = ref.matmul(ref.decode(*a, 128), ref.decode(*w, 128), [(0, 4)], False)
+    want = torch.where(want.abs() < 2.0 ** 128, want, math.inf)
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(y), fine)
+    assert torch.all((y[fine] - want[fine]).abs() <= (BF16 + 2.0 ** -20) * want[fine].abs())
+
+
+@pytest.mark.parametrize("counts", [[0, 0, 0], [0, 5, 0, 0, 1], [1] * 70, [40, 0, 300, 17, 0, 1, 64],
+                                    [0] * 63 + [3, 0, 9], [256, 512, 128], [2] * 130])
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_packed_windows(counts, swiglu):
+    E, N, K = len(counts), 96, 224
+    offset, windows = _packed(counts)
+    a, w = _inputs(offset[-1], E, N, K, seed=E)
+    for count in (counts, None):
+        if offset[-1] == 0 and count is None:
+            continue
+        _check(_run(a, w, offset, count, swiglu), a, w, windows, swiglu)
+
+
+@pytest.mark.parametrize("cap", [8, 40, 300])
+def test_fixed_windows_of_a_rank(cap):
+    counts = [3, 0, cap, 7, 1]
+    base = 12345
+    offset = [base + e * cap for e in range(6)]
+    a, w = _inputs(5 * cap, 5, 88, 160, seed=cap)
+    _check(_run(a, w, offset, counts, False), a, w, [(e * cap, n) for e, n in enumerate(counts)],
+           False)
+
+
+def test_windows_are_clipped_to_the_rows():
+    a, w = _inputs(50, 3, 16, 32, seed=1)
+    y = _run(a, w, [0, 30, 70, 90], [30, 40, 20], False)          # the region holds 50 rows
+    _check(y, a, w, [(0, 30), (30, 20), (50, 0)], False)
+    y = _run(a, w, [5, 0, 60, 70], [-4, 9, 9], False)             # no window lies in the rows
+    assert torch.all(torch.isnan(y.float()))
+
+
+@pytest.mark.parametrize("counts,N,K", [([700], 1416, 2080), ([790, 710], 512, 1024),
+                                        ([4100], 4112, 1056), ([8193], 2064, 32),
+                                        ([0, 1024, 700, 2300, 65], 4112, 416), ([1000, 1], 16400, 288),
+                                        ([65, 190, 3, 250] * 32 + [0, 700], 2064, 160),
+                                        ([129, 0, 64, 1, 127, 128, 65, 190] * 5, 1056, 544),
+                                        ([63, 64, 65, 1, 0, 129] * 4, 2064, 1056), ([30] * 50, 2064, 416),
+                                        ([512], 4112, 1568), ([65, 17, 98], 1040, 2080)])
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_many_tiles(counts, N, K, swiglu):
+    E, rows = len(counts), sum(counts)
+    N -= 0 if swiglu or N % 16 else 8                             # an odd number of eights
+    N = N // 16 * 16 if swiglu else N
+    offset, windows = _packed(counts)
+    a, w = _inputs(rows, E, N, K, seed=rows)
+    y = _run(a, w, offset, counts, swiglu) if E > 1 else _run(a, w, None, None, swiglu)
+    _check(y, a, w, windows, swiglu)
+    if E > 1:
+        assert torch.equal(_run(a, w, offset, None, swiglu), y)
+
+
+@pytest.mark.parametrize("rows,K", [(7, 160), (300, 1056)])
+def test_row_pitches(rows, K):
+    """Codes and scales in one row, as they come from dispatch."""
+    moe = _moe()
+    a, w = _inputs(rows, 1, 72, K, seed=rows)
+    pitch = -(-(K // 2 + ref.scale_cols(K)) // 16) * 16
+    buf = torch.full((rows, pitch), 255, dtype=torch.uint8)
+    buf[:, :K // 2], buf[:, K // 2:K // 2 + a[1].shape[1]] = a
+    buf = buf.cuda()
+    y = torch.empty(rows, 72, dtype=torch.bfloat16, device="cuda")
+    moe.moe_expert_matmul_mx(buf, buf[:, K // 2:], rows, w[0].cuda(), w[1].cuda(), 1, 72, K, None,
+                             None, moe.MOE_ACT_NONE, y, a_pitch=pitch, a_scale_pitch=pitch)
+    _check(y.cpu(), a, w, [(0, rows)], False)
+
+
+@pytest.mark.parametrize("rows", [5, 200])
+def test_marked_blocks_show(rows):
+    a, w = _inputs(rows, 1, 72, 288, seed=rows)
+    a[1][3, 8], w[1][0, 7, 0] = 255, 255
+    y = _run(a, w, None, None, False)
+    bad = torch.zeros(rows, 72, dtype=torch.bool)
+    bad[3], bad[:, 7] = True, True
+    assert torch.equal(torch.isnan(y), bad)
+    fine = a[1].clone(), w[1].clone()
+    fine[0][3, 8], fine[1][0, 7, 0] = 126, 126
+    whole = _run((a[0], fine[0]), (w[0], fine[1]), None, None, False)
+    assert torch.equal(y[~bad], whole[~bad])
+
+
+def test_quantized_rows_and_weights():
+    """The two operators as they are used: bf16 rows and weights, quantised, multiplied."""
+    moe = _moe()
+    rows, E, N, K = 190, 3, 200, 608
+    g = _gen(9)
+    x, w = torch.randn(rows, K, generator=g).bfloat16(), torch.randn(E * N, K, generator=g).bfloat16()
+    qa, sa, _ = _quantize(x)
+    qw, sw, _ = _quantize(w)
+    a, wt = (qa, sa), (qw.view(E, N, -1), sw.view(E, N, -1))
+    counts = [100, 0, 90]
+    offset, windows = _packed(counts)
+    for swiglu in (False, True):
+        n = N // 16 * 16 if swiglu else N
+        wn = tuple(t[:, :n].contiguous() for t in wt)
+        _check(_run(a, wn, offset, counts, swiglu), a, wn, windows, swiglu, exact=False)
+    assert moe.mx_scale_bytes(K) == sa.shape[1]
+
+
+def test_no_rows():
+    moe = _moe()
+    w = torch.zeros(1, 8, 16, dtype=torch.uint8, device="cuda")
+    moe.moe_expert_matmul_mx(None, None, 0, w, w, 1, 8, 32, None, None, moe.MOE_ACT_NONE, None)
+
+
+def test_other_streams():
+    a, w = _inputs(130, 1, 256, 512, seed=4)
+    s = torch.cuda.Stream()
+    moe = _moe()
+    with torch.cuda.stream(s):
+        dev = [t.cuda(non_blocking=True) for t in (*a, *w)]
+        y = torch.empty(130, 256, dtype=torch.bfloat16, device="cuda")
+        moe.moe_expert_matmul_mx(dev[0], dev[1], 130, dev[2], dev[3], 1, 256, 512, None, None,
+                                 moe.MOE_ACT_NONE, y)
+    s.synchronize()
+    _check(y.cpu(), a, w, [(0, 130)], False)
+
+
+# ------------------------------------------------------------------- layer
+def _layer_inputs(T, H, E, seed):
+    g = _gen(seed)
+    x, r = (torch.randn(T, H, generator=g).bfloat16() for _ in range(2))
+    return x.cuda(), r.cuda(), torch.randn(T, E, generator=g).cuda()
+
+
+def _check_layer(layer, x, r, logits, y):
+    """Every step against 64 bits from what the step before left."""
+    T, H, I, E, k = layer.T, layer.H, layer.I, layer.E, layer.k
+    c = [t.cpu().double() for t in (x, r, layer.norm_weight, logits)]
+    h, _, normed = layer_ref.rmsnorm(c[0], c[1], c[2], layer.eps)
+    assert torch.all((layer.sum.cpu().double() - h).abs() <= BF16 * h.abs())
+    got = layer.normed.cpu()
+    # float32 sum of squares and three products: far under 2^-18
+    assert torch.all((got.double() - normed).abs() <= (BF16 + 2.0 ** -18) * normed.abs())
+    q, s, rows = ref.quantize(got)
+    codes = layer.q.cpu()
+    assert torch.equal(codes[:, :H // 2], q)
+    assert torch.equal(codes[:, H // 2:H // 2 + s.shape[1]], s)
+    idx, pos = layer.topk_idx.cpu(), layer.layout.pos.cpu()[:T * k].view(T, k)
+    act, out = layer.act.cpu(), layer.out.cpu().double()
+    q2 = ref.quantize(act)[2]
+    want, size = torch.zeros(T, H, dtype=torch.float64), torch.zeros(T, H, dtype=torch.float64)
+    w = layer.topk_w.cpu().double()
+    for e in range(E):
+        tok, slot = torch.nonzero(idx == e, as_tuple=True)
+        n = len(tok)
+        if not n:
+            continue
+        at = pos[tok, slot].long()
+        up = ref.decode(layer.w13[e].cpu(), layer.w13_scale[e].cpu(), H)[None]
+        v, tol = ref.matmul(rows[tok], up, [(0, n)], True)
+        assert torch.all((act[at].double() - v).abs() <= BF16 * v.abs() + 1.01 * tol)
+        down = ref.decode(layer.w2[e].cpu(), layer.w2_scale[e].cpu(), I)[None]
+        v, tol = ref.matmul(q2[at], down, [(0, n)], False)
+        assert torch.all((out[at] - v).abs() <= BF16 * v.abs() + 1.01 * tol)
+        want.index_add_(0, tok, out[at] * w[tok, slot][:, None])
+        size.index_add_(0, tok, (out[at] * w[tok, slot][:, None]).abs())
+    assert torch.all((y.cpu().double() - want).abs() <= BF16 * want.abs() + 40 * 2.0 ** -24 * size)
+    assert int(layer.layout.status) == 0
+
+
+@pytest.mark.parametrize("T,H,I,E,k", [(1, 256, 64, 4, 2), (33, 416, 224, 8, 3), (300, 512, 256, 16, 4),
+                                       (700, 1056, 160, 4, 2)])
+@pytest.mark.parametrize("score", [0, 1])
+def test_layer(T, H, I, E, k, score):
+    from paper_2607_26444_amd.layer import random_layer
+    layer = random_layer(T, H, I, E, k, seed=T, mx=True, score=score, scale=1.5)
+    x, r, logits = _layer_inputs(T, H, E, seed=1)
+    y = layer.forward(x, r, logits)
+    torch.cuda.synchronize()
+    _check_layer(layer, x, r, logits, y)
+
+
+def test_layer_with_padding_and_a_gate():
+    from paper_2607_26444_amd.layer import random_layer
+    T, H, E = 64, 256, 8
+    layer = random_layer(T, H, 64, E, 4, mx=True)
+    x, r, logits = _layer_inputs(T, H, E, seed=2)
+    logits[5] = -math.inf
+    mask = torch.ones(T, dtype=torch.uint8, device="cuda")
+    mask[60:] = 0
+    y = layer.forward(x, r, logits, token_mask=mask)
+    torch.cuda.synchronize()
+    assert torch.all(layer.topk_idx[60:] == -1) and torch.all(y[60:] == 0) and torch.all(y[5] == 0)
+    _check_layer(layer, x, r, logits, y)
+    gate = torch.randn(H, E, device="cuda").bfloat16() / 16
+    seen = []
+
+    def logits_of(normed):
+        seen.append(normed @ gate)
+        return seen[-1]
+    y = layer.forward(x, r, logits_of)
+    assert torch.equal(layer.forward(x, r, seen[0]).clone(), y)
+
+
+def test_layer_graph_replays():
+    from paper_2607_26444_amd.layer import random_layer
+    T, H, E = 48, 512, 8
+    layer, eager = (random_layer(T, H, 128, E, 2, mx=True) for _ in range(2))
+    x, r, logits = (t.clone() for t in _layer_inputs(T, H, E, seed=0))
+    layer.forward(x, r, logits)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward(x, r, logits)
+    for seed in range(1, 5):
+        for t, new in zip((x, r, logits), _layer_inputs(T, H, E, seed)):
+            t.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = eager.forward(x, r, logits)
+        torch.cuda.synchronize()
+        assert torch.equal(layer.y, want) and torch.equal(layer.sum, eager.sum)
+
+
+def test_layer_streams_and_refusals():
+    from paper_2607_26444_amd import layer as mod
+    layer = mod.random_layer(100, 256, 64, 8, 2, mx=True)
+    x, r, logits = _layer_inputs(100, 256, 8, seed=4)
+    want = layer.forward(x, r, logits).clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    y = layer.forward(x, r, logits, stream=s)
+    s.synchronize()
+    assert torch.equal(y, want)
+    good = dict(norm_weight=layer.norm_weight, w13=layer.w13, w13_scale=layer.w13_scale,
+                w2=layer.w2, w2_scale=layer.w2_scale)
+    for change in (dict(w2=layer.w2.to(torch.int8)), dict(w13_scale=layer.w13_scale.float()),
+                   dict(w2_scale=layer.w2_scale[:, :, :2]), dict(w13=layer.w13[:, :, :64])):
+        with pytest.raises(ValueError):
+            mod.MoeLayer(100, 256, 64, 8, 2, **dict(good, **change))
+    with pytest.raises(ValueError, match="multiples"):
+        mod.MoeLayer(100, 264, 64, 8, 2, **good)
+
+
+def test_layer_of_no_tokens():
+    from paper_2607_26444_amd.layer import random_layer
+    layer = random_layer(0, 256, 64, 8, 2, mx=True)
+    x, r, logits = _layer_inputs(0, 256, 8, seed=0)
+    assert layer.forward(x, r, logits).shape == (0, 256)
+    torch.cuda.synchronize()
+    assert int(layer.layout.status) == 0
