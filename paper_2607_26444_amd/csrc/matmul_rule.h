@@ -101,19 +101,44 @@ inline double way_time(const MatmulShape& a, const Way& w) {
   return __builtin_sqrt(work * work + read * read);
 }
 
-// The way that takes least of those that can be launched; kWays if none can be.
-inline int choose_way(const MatmulShape& a) {
+// The way of a table that takes least of those that `fits` says can be launched; kWays if none
+// can be.
+template <typename Fits>
+inline int quickest_way(const MatmulShape& a, const Way* ways, Fits&& fits) {
   int best = kWays;
   double least = 0.0;
   for (int n = 0; n < kWays; ++n) {
-    if (!way_fits(a, n)) continue;
-    const double t = way_time(a, kWay[n]);
+    if (!fits(n)) continue;
+    const double t = way_time(a, ways[n]);
     if (best == kWays || t < least) {
       least = t;
       best = n;
     }
   }
   return best;
+}
+inline int choose_way(const MatmulShape& a) {
+  return quickest_way(a, kWay, [&](int n) { return way_fits(a, n); });
+}
+
+// The same for the products on 4-bit floats, depths in bytes of codes.
+constexpr Way kMxWay[kWays] = {
+    {256, 256, 128, 256, 9.0, 1.60, 1.60, 4.85e6},     // matmul_mx_tile_kernel<256>
+    {128, 256, 128, 256, 6.0, 1.05, 1.05, 4.85e6},     // matmul_mx_tile_kernel<128>
+    {64, 128, 128, 512, 3.0, 0.72, 1.15, 5.9e6},       // matmul_mx_stream_kernel<64, 8, 1, 3>
+    {64, 64, 256, 256, 3.0, 0.65, 0.65, 4.5e6},        // <64, 4, 2, 3>
+    {64, 64, 256, 512, 3.0, 0.95, 1.00, 4.5e6},        // <64, 4, 2, 2>
+    {64, 32, 512, 256, 3.0, 0.68, 0.68, 4.5e6},        // <64, 2, 4, 3>
+    {16, 32, 512, 512, 3.0, 0.65, 0.80, 4.5e6},        // <16, 2, 4, 3>
+    {16, 16, 1024, 512, 3.0, 0.80, 1.00, 4.5e6},       // <16, 1, 8, 2>
+};
+// Windows that tiles of 128 rows have room for beside three stages and their scales.
+constexpr int kMxTile128Experts = 512;
+
+inline int choose_mx_way(const MatmulShape& a) {
+  return quickest_way(a, kMxWay, [&](int n) {
+    return way_fits(a, n) && (n != kTile128 || a.E <= kMxTile128Experts);
+  });
 }
 
 }  // namespace moe
