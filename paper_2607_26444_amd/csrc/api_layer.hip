@@ -159,7 +159,7 @@ int moe_balance(const void* logits, int dtype, int64_t logits_pitch, int64_t T, 
   a.part_live = reinterpret_cast<int32_t*>(ws + s.live_at);
   a.tickets = reinterpret_cast<uint32_t*>(ws + s.ticket_at);
   a.pieces = reinterpret_cast<float*>(ws + s.piece_at);
-  return moe::hip_status(moe::launch_balance(a, s.blocks, as_stream(stream)));
+  return moe::hip_status(moe::launch_balance(a, s, as_stream(stream)));
 }
 
 int moe_balance_backward(const void* logits, int dtype, int64_t logits_pitch, int64_t T, int E,
@@ -176,16 +176,14 @@ int moe_balance_backward(const void* logits, int dtype, int64_t logits_pitch, in
   if (!aligned(logits, size) || !aligned(grad_sum, size) || !aligned(grad_logits, size) ||
       !aligned(expert_count, 4) || !aligned(live_tokens, 4) || !aligned(grad_loss, 4))
     return MOE_EALIGN;
-  const moe::BalanceShape s = moe::balance_shape(T, E, seq_len);
   moe::BalanceGradArgs a;
   a.logits = logits;
   a.pitch = logits_pitch ? logits_pitch : E;
-  a.seq = s.seq;
-  a.seqs = s.seqs;
-  a.per = s.per;
-  a.parts = s.parts;
+  a.seq = seq_len ? seq_len : T;
+  a.seqs = T / a.seq;
   a.f32 = dtype == MOE_DTYPE_F32;
   a.E = E;
+  moe::balance_grad_parts(a);
   a.sigmoid = score == MOE_SCORE_SIGMOID;
   a.token_mask = token_mask;
   a.expert_count = expert_count;

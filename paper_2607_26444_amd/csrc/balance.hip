@@ -11,41 +11,71 @@
 // over the part's tokens, the slots are counted in LDS.  A second launch adds the parts, 32
 // experts to a workgroup; the last workgroup of a sequence adds the loss.  Sequences of
 // one part need no second launch.
+//
+// The logits are read once, but a token's chain of loads, exponentials and sums over lanes
+// takes longer than that: 32768 x 256 float32 in 8 sequences 16.0 us (2.2 TB/s), the
+// gradient of 32768 x 128 bf16 with another added 10.4 (2.4 TB/s), of 32768 x 256 float32
+// 16.2 (4.1 TB/s).  Small batches are bound by the launches: 128 x 16 5.0 us.
 
 #include "logits.h"
 
 namespace moe {
 namespace {
 
+// Neighbouring logits that a lane has of a row: 16 bytes where it has as many.
+template <int VPL, bool F32>
+constexpr int run_of() {
+  return VPL < (F32 ? 4 : 8) ? VPL : F32 ? 4 : 8;
+}
+
+// Expert of a lane's i-th value: runs of neighbours, dealt to the lanes in turn.
+template <int LANES, int VPL, bool F32>
+__device__ __forceinline__ int expert_of(int sub, int i) {
+  constexpr int N = run_of<VPL, F32>();
+  return (i / N * LANES + sub) * N + i % N;
+}
+
 // A token's dealt logits; -inf where the token takes no part.
-template <int LANES, int VPL>
-__device__ __forceinline__ void load_token(const void* logits, bool f32, int64_t at, int sub, int E,
-                                           int vec, bool take, float (&x)[VPL]) {
+template <int LANES, int VPL, bool F32>
+__device__ __forceinline__ void load_token(const void* logits, int64_t at, int sub, int E, int vec,
+                                           bool take, float (&x)[VPL]) {
 #pragma unroll
   for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
   if (!take) return;
-  constexpr int N = VPL >= 4 ? 4 : VPL;
+  constexpr int N = run_of<VPL, F32>();
 #pragma unroll
   for (int g = 0; g < VPL / N; ++g) {
     float v[N];
-    load_logits<N>(logits, f32, at, dealt<LANES, VPL>(sub, g * N), E, vec, v);
+    load_logits<N>(logits, F32, at, expert_of<LANES, VPL, F32>(sub, g * N), E, vec, v);
 #pragma unroll
     for (int j = 0; j < N; ++j) x[g * N + j] = v[j];
   }
 }
 
+constexpr float kLog2E = 1.44269504f;
+
 // Scores in place of the logits, and the factor that makes shares of them: 0 where their sum
-// is none, or lies below float32's normal range (sigmoid scores of very low logits).
-template <int LANES, int VPL, bool SIGMOID>
-__device__ __forceinline__ float scores(float (&x)[VPL]) {
+// is none, or lies below float32's normal range (sigmoid scores of very low logits).  By the
+// hardware's exponential and reciprocal (1 unit in the last place each): the argument's
+// rounding adds |x| 2^-24, and a share is one of many terms of a mean.  REST: also 1 - s.
+template <int LANES, int VPL, bool SIGMOID, bool REST = false>
+__device__ __forceinline__ float scores(float (&x)[VPL], float (&rest)[REST ? VPL : 1]) {
   float local = 0.0f;
   if constexpr (SIGMOID) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) x[i] = x[i] > -INFINITY ? sigmoid(x[i]) : 0.0f;
+    for (int i = 0; i < VPL; ++i) {
+      const float e = __builtin_amdgcn_exp2f(x[i] * -kLog2E);
+      const float s = x[i] > -INFINITY ? __builtin_amdgcn_rcpf(1.0f + e) : 0.0f;
+      if constexpr (REST) rest[i] = e > 1.0f ? 1.0f - s : e * s;   // also where s rounds to 1
+      x[i] = s;
+    }
   } else {
     const float m = row_max<LANES, VPL>(x);
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) x[i] = exp_term(x[i], m);
+    for (int i = 0; i < VPL; ++i) {
+      const float e = x[i] == m ? 1.0f : __builtin_amdgcn_exp2f((x[i] - m) * kLog2E);
+      x[i] = x[i] > -INFINITY ? e : 0.0f;
+    }
   }
 #pragma unroll
   for (int i = 0; i < VPL; ++i) local += x[i];
@@ -67,52 +97,56 @@ __device__ __forceinline__ float block_sum(float x, float* s) {
 // Words of a part in the workspace: sums of the experts' shares, slots.
 __host__ __device__ inline int part_pitch(int E) { return (E + 31) / 32 * 32; }
 
-template <int LANES, int VPL, bool SIGMOID>
-__global__ __launch_bounds__(kBlock) void balance_kernel(BalanceArgs a, int vec) {
-  constexpr int kTokens = kWave / LANES, kStep = kWavesPerBlock * kTokens;
-  __shared__ float s_sum[kWavesPerBlock][LANES * VPL];
+constexpr int kMaxWaves = 16;
+
+// A workgroup of up to 16 wavefronts has 4 (16 lanes a token) or 1 tokens a wavefront at once.
+template <int LANES, int VPL, bool F32, bool SIGMOID>
+__global__ __launch_bounds__(kMaxWaves * kWave) void balance_kernel(BalanceArgs a, int vec) {
+  constexpr int kTokens = kWave / LANES;
+  __shared__ float s_sum[kMaxWaves][LANES * VPL];
   __shared__ int s_count[LANES * VPL];
-  __shared__ int s_live[kWavesPerBlock];
-  __shared__ float s_word[kWavesPerBlock];
+  __shared__ int s_live[kMaxWaves];
+  __shared__ float s_word[kMaxWaves];
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int sub = lane & (LANES - 1), tok = lane / LANES;
+  const int threads = blockDim.x, waves = threads / kWave, step = waves * kTokens;
   const int64_t units = a.seqs * a.parts;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int64_t seq = u / a.parts;
     const int part = (int)(u - seq * a.parts);
     const int64_t begin = seq * a.seq + part * a.per, last = seq * a.seq + a.seq;
     const int64_t end = begin + a.per < last ? begin + a.per : last;
-    for (int e = threadIdx.x; e < LANES * VPL; e += kBlock) s_count[e] = 0;
+    float x[VPL], next[VPL], none[1];
+    auto fetch = [&](int64_t t0) {
+      const int64_t t = t0 + tok;
+      const bool take = t < end && (!a.token_mask || a.token_mask[t]);
+      load_token<LANES, VPL, F32>(a.logits, t * a.pitch, sub, a.E, vec, take, next);
+    };
+    fetch(begin + wave * kTokens);
+    for (int e = threadIdx.x; e < LANES * VPL; e += threads) s_count[e] = 0;
     __syncthreads();
 
     // slots
     const int slots = (int)(end - begin) * a.k;
-    for (int i = threadIdx.x; i < slots; i += kBlock) {
+    for (int i = threadIdx.x; i < slots; i += threads) {
       const int e = (int)ld4(a.topk_idx + begin * a.k + i);
       const bool live = !a.token_mask || a.token_mask[begin + i / a.k];
       if (live && (uint32_t)e < (uint32_t)a.E) atomicAdd(&s_count[e], 1);
     }
     int live = 0;
     if (a.token_mask) {
-      for (int64_t t = begin + threadIdx.x; t - threadIdx.x < end; t += kBlock)
+      for (int64_t t = begin + threadIdx.x; t - threadIdx.x < end; t += threads)
         live += __builtin_popcountll(__ballot(t < end && a.token_mask[t]));
     }
     if (lane == 0) s_live[wave] = live;
 
     // shares
     float sum[VPL] = {};
-    float x[VPL], next[VPL];
-    auto fetch = [&](int64_t t0) {
-      const int64_t t = t0 + tok;
-      const bool take = t < end && (!a.token_mask || a.token_mask[t]);
-      load_token<LANES, VPL>(a.logits, a.f32, t * a.pitch, sub, a.E, vec, take, next);
-    };
-    fetch(begin + wave * kTokens);
-    for (int64_t t0 = begin + wave * kTokens; t0 < end; t0 += kStep) {
+    for (int64_t t0 = begin + wave * kTokens; t0 < end; t0 += step) {
 #pragma unroll
       for (int i = 0; i < VPL; ++i) x[i] = next[i];
-      if (t0 + kStep < end) fetch(t0 + kStep);
-      const float inv = scores<LANES, VPL, SIGMOID>(x);
+      if (t0 + step < end) fetch(t0 + step);
+      const float inv = scores<LANES, VPL, SIGMOID>(x, none);
 #pragma unroll
       for (int i = 0; i < VPL; ++i) sum[i] = __builtin_fmaf(x[i], inv, sum[i]);
     }
@@ -123,17 +157,26 @@ __global__ __launch_bounds__(kBlock) void balance_kernel(BalanceArgs a, int vec)
         b = across32(b, fadd_bits);
         sum[i] = __uint_as_float(across16(b, fadd_bits));
       }
-      if (tok == 0) s_sum[wave][dealt<LANES, VPL>(sub, i)] = sum[i];
+      if (tok == 0) s_sum[wave][expert_of<LANES, VPL, F32>(sub, i)] = sum[i];
     }
     __syncthreads();
-    live = a.token_mask ? s_live[0] + s_live[1] + s_live[2] + s_live[3] : (int)(end - begin);
+    live = (int)(end - begin);
+    if (a.token_mask) {
+      live = 0;
+      for (int w = 0; w < waves; ++w) live += s_live[w];
+    }
+    auto share_of = [&](int e) {
+      float t = s_sum[0][e];
+      for (int w = 1; w < waves; ++w) t += s_sum[w][e];
+      return t;
+    };
 
     if (a.parts > 1) {
       const int pitch = part_pitch(a.E);
       float* out = a.partial + u * 2 * pitch;
       int* counts = reinterpret_cast<int*>(out + pitch);
-      for (int e = threadIdx.x; e < pitch; e += kBlock) {
-        out[e] = e < a.E ? ((s_sum[0][e] + s_sum[1][e]) + s_sum[2][e]) + s_sum[3][e] : 0.0f;
+      for (int e = threadIdx.x; e < pitch; e += threads) {
+        out[e] = e < a.E ? share_of(e) : 0.0f;
         counts[e] = e < a.E ? s_count[e] : 0;
       }
       if (threadIdx.x == 0) {
@@ -143,13 +186,12 @@ __global__ __launch_bounds__(kBlock) void balance_kernel(BalanceArgs a, int vec)
     } else {
       float total = 0.0f, dot = 0.0f;
       const float n = (float)(live > 0 ? live : 1);
-      for (int e = threadIdx.x; e < a.E; e += kBlock) {
-        const float share = ((s_sum[0][e] + s_sum[1][e]) + s_sum[2][e]) + s_sum[3][e];
-        const float count = (float)s_count[e];
+      for (int e = threadIdx.x; e < a.E; e += threads) {
+        const float mean = share_of(e) / n, count = (float)s_count[e];
         a.expert_count[seq * a.E + e] = s_count[e];
-        if (a.mean_score) a.mean_score[seq * a.E + e] = share / n;
+        if (a.mean_score) a.mean_score[seq * a.E + e] = mean;
         total += count;
-        dot = __builtin_fmaf(count, share / n, dot);
+        dot = __builtin_fmaf(count, mean, dot);
       }
       total = block_sum(total, s_word);
       dot = block_sum(dot, s_word);
@@ -162,96 +204,92 @@ __global__ __launch_bounds__(kBlock) void balance_kernel(BalanceArgs a, int vec)
   }
 }
 
-// Sums over the parts of a sequence: 32 experts to a workgroup, 128 rows of parts at a
+// Sums over the parts of a sequence: 32 experts to a workgroup, 32 rows of parts at a
 // time in fours of neighbours.  Each leaves its part of the loss, and the last of them adds
 // those in their order.
-__global__ __launch_bounds__(1024) void balance_join_kernel(BalanceArgs a, int blocks) {
-  __shared__ float s_sum[128][33];
-  __shared__ int s_count[128][33];
-  __shared__ int s_live[16];
-  __shared__ uint32_t s_order;
+__global__ __launch_bounds__(kBlock) void balance_join_kernel(BalanceArgs a, int blocks) {
+  __shared__ float s_sum[kWavesPerBlock][32];
+  __shared__ int s_count[kWavesPerBlock][32];
+  __shared__ int s_live[kWavesPerBlock];
   const int64_t seq = blockIdx.x / blocks;
   const int block = blockIdx.x - (int)seq * blocks;
   const int pitch = part_pitch(a.E);
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int quad = threadIdx.x & 7, row = threadIdx.x / 8;
   const float* from = a.partial + seq * a.parts * 2 * pitch + block * 32 + quad * 4;
   float sum[4] = {};
   int count[4] = {}, live = 0;
-  for (int p = row; p < a.parts; p += 128) {
-    const u32x4 v = ld16(from + (int64_t)p * 2 * pitch);
-    const u32x4 c = ld16(from + (int64_t)p * 2 * pitch + pitch);
-    sum[0] += __uint_as_float(v.x);
-    sum[1] += __uint_as_float(v.y);
-    sum[2] += __uint_as_float(v.z);
-    sum[3] += __uint_as_float(v.w);
-    count[0] += (int)c.x;
-    count[1] += (int)c.y;
-    count[2] += (int)c.z;
-    count[3] += (int)c.w;
-  }
-  for (int p = threadIdx.x; p < a.parts; p += 1024) live += a.part_live[seq * a.parts + p];
+  for (int p = threadIdx.x; p < a.parts; p += kBlock) live += a.part_live[seq * a.parts + p];
+  for (int p0 = row; p0 < a.parts; p0 += 128) {        // four rows asked for together
+    u32x4 v[4], c[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    s_sum[row][quad * 4 + j] = sum[j];
-    s_count[row][quad * 4 + j] = count[j];
-  }
-  live = (int)reduce<64>((uint32_t)live, [](uint32_t x, uint32_t y) { return x + y; });
-  if ((threadIdx.x & 63) == 0) s_live[threadIdx.x / 64] = live;
-  __syncthreads();
-  live = 0;
-  for (int w = 0; w < 16; ++w) live += s_live[w];
-  const int c = threadIdx.x & 31, part = threadIdx.x / 32;   // 32 parts of four rows
-  float t = 0.0f;
-  int m = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    t += s_sum[part * 4 + j][c];
-    m += s_count[part * 4 + j][c];
-  }
-  __syncthreads();
-  s_sum[part][c] = t;
-  s_count[part][c] = m;
-  __syncthreads();
-  if (threadIdx.x < kWave) {                           // one wavefront from here on
-    const int e = block * 32 + c;
-    float total = 0.0f, dot = 0.0f;
-    if (threadIdx.x < 32 && e < a.E) {
-      t = 0.0f;
-      m = 0;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        t += s_sum[j][c];
-        m += s_count[j][c];
-      }
-      t /= (float)(live > 0 ? live : 1);
-      a.expert_count[seq * a.E + e] = m;
-      if (a.mean_score) a.mean_score[seq * a.E + e] = t;
-      total = (float)m;
-      dot = total * t;
+    for (int i = 0; i < 4; ++i) {
+      const int64_t p = p0 + i * 32;
+      v[i] = p < a.parts ? ld16(from + p * 2 * pitch) : u32x4{0, 0, 0, 0};
+      c[i] = p < a.parts ? ld16(from + p * 2 * pitch + pitch) : u32x4{0, 0, 0, 0};
     }
-    total = reduce_sum<64>(total);
-    dot = reduce_sum<64>(dot);
-    float* piece = a.pieces + (seq * blocks + block) * 2;
-    if (threadIdx.x == 0) {
-      if (block == 0) a.live_tokens[seq] = live;
-      __hip_atomic_store(piece, total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(piece + 1, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      s_order = __hip_atomic_fetch_add(a.tickets + seq, 1u, __ATOMIC_ACQ_REL,
-                                       __HIP_MEMORY_SCOPE_AGENT);
-    }
-    if (threadIdx.x == 0 && a.loss && s_order == (uint32_t)blocks - 1u) {
-      total = dot = 0.0f;
-      piece = a.pieces + seq * blocks * 2;
-      for (int b = 0; b < blocks; ++b) {
-        total += __hip_atomic_load(piece + 2 * b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        dot += __hip_atomic_load(piece + 2 * b + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
-      a.loss[seq] = total > 0.0f ? dot * ((float)a.E / total) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum[0] += __uint_as_float(v[i].x);
+      sum[1] += __uint_as_float(v[i].y);
+      sum[2] += __uint_as_float(v[i].z);
+      sum[3] += __uint_as_float(v[i].w);
+      count[0] += (int)c[i].x;
+      count[1] += (int)c[i].y;
+      count[2] += (int)c[i].z;
+      count[3] += (int)c[i].w;
     }
   }
+  const auto add = [](uint32_t x, uint32_t y) { return x + y; };
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {                        // over the wavefront's eight rows
+    uint32_t b = across16(across32(__float_as_uint(sum[j]), fadd_bits), fadd_bits);
+    b = fadd_bits(b, row_rotate<8>(b));
+    uint32_t n = across16(across32((uint32_t)count[j], add), add);
+    n += row_rotate<8>(n);
+    if (lane < 8) {
+      s_sum[wave][quad * 4 + j] = __uint_as_float(b);
+      s_count[wave][quad * 4 + j] = (int)n;
+    }
+  }
+  live = (int)reduce<64>((uint32_t)live, add);
+  if (lane == 0) s_live[wave] = live;
+  __syncthreads();
+  if (wave > 0) return;                                // one wavefront from here on
+  live = s_live[0] + s_live[1] + s_live[2] + s_live[3];
+  const int e = block * 32 + lane;
+  float total = 0.0f, dot = 0.0f;
+  if (lane < 32 && e < a.E) {
+    const float t = (((s_sum[0][lane] + s_sum[1][lane]) + s_sum[2][lane]) + s_sum[3][lane]) /
+                    (float)(live > 0 ? live : 1);
+    const int m = s_count[0][lane] + s_count[1][lane] + s_count[2][lane] + s_count[3][lane];
+    a.expert_count[seq * a.E + e] = m;
+    if (a.mean_score) a.mean_score[seq * a.E + e] = t;
+    total = (float)m;
+    dot = total * t;
+  }
+  total = reduce_sum<64>(total);
+  dot = reduce_sum<64>(dot);
+  if (lane != 0) return;
+  if (block == 0) a.live_tokens[seq] = live;
+  if (!a.loss) return;
+  float* pieces = a.pieces + seq * blocks * 2;
+  if (blocks > 1) {
+    __hip_atomic_store(pieces + 2 * block, total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(pieces + 2 * block + 1, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__hip_atomic_fetch_add(a.tickets + seq, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) !=
+        (uint32_t)blocks - 1u)
+      return;
+    total = dot = 0.0f;
+    for (int b = 0; b < blocks; ++b) {
+      total += __hip_atomic_load(pieces + 2 * b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      dot += __hip_atomic_load(pieces + 2 * b + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  a.loss[seq] = total > 0.0f ? dot * ((float)a.E / total) : 0.0f;
 }
 
-template <int LANES, int VPL, bool SIGMOID>
+template <int LANES, int VPL, bool F32, bool SIGMOID>
 __global__ __launch_bounds__(kBlock) void balance_backward_kernel(BalanceGradArgs a, int vec) {
   constexpr int kTokens = kWave / LANES, kStep = kWavesPerBlock * kTokens;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
@@ -265,7 +303,7 @@ __global__ __launch_bounds__(kBlock) void balance_backward_kernel(BalanceGradArg
     float load[VPL], total = 0.0f;                     // f of the lane's experts
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-      const int e = dealt<LANES, VPL>(sub, i);
+      const int e = expert_of<LANES, VPL, F32>(sub, i);
       load[i] = e < a.E ? (float)(int)ld4(a.expert_count + seq * a.E + e) : 0.0f;
       total += load[i];
     }
@@ -280,20 +318,17 @@ __global__ __launch_bounds__(kBlock) void balance_backward_kernel(BalanceGradArg
     auto fetch = [&](int64_t t0) {
       const int64_t t = t0 + tok;
       const bool take = t < end && (!a.token_mask || a.token_mask[t]);
-      load_token<LANES, VPL>(a.logits, a.f32, t * a.pitch, sub, a.E, vec, take, next);
+      load_token<LANES, VPL, F32>(a.logits, t * a.pitch, sub, a.E, vec, take, next);
     };
     fetch(begin + wave * kTokens);
     for (int64_t t0 = begin + wave * kTokens; t0 < end; t0 += kStep) {
       const int64_t t = t0 + tok;
-      float rest[VPL], add[VPL];
+      float rest[SIGMOID ? VPL : 1], add[VPL];
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) {
-        x[i] = next[i];
-        if (SIGMOID) rest[i] = sigmoid(-x[i]);         // 1 - s, also where s rounds to 1
-      }
+      for (int i = 0; i < VPL; ++i) x[i] = next[i];
       if (t0 + kStep < end) fetch(t0 + kStep);
-      load_token<LANES, VPL>(a.grad_sum, a.f32, t * a.E, sub, a.E, vec, a.grad_sum && t < end, add);
-      const float inv = scores<LANES, VPL, SIGMOID>(x);
+      load_token<LANES, VPL, F32>(a.grad_sum, t * a.E, sub, a.E, vec, a.grad_sum && t < end, add);
+      const float inv = scores<LANES, VPL, SIGMOID, SIGMOID>(x, rest);
       float dot = 0.0f;
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
@@ -304,30 +339,36 @@ __global__ __launch_bounds__(kBlock) void balance_backward_kernel(BalanceGradArg
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
         // an expert without a share has no gradient
-        const float d = x[i] > 0.0f ? c * x[i] * (load[i] - dot) * (SIGMOID ? rest[i] : 1.0f) : 0.0f;
+        const float d = x[i] > 0.0f ? c * x[i] * (load[i] - dot) * (SIGMOID ? rest[SIGMOID ? i : 0] : 1.0f) : 0.0f;
         x[i] = a.grad_sum ? add[i] + d : d;
       }
       if (t >= end) continue;
       if constexpr (VPL >= 4) if (vec) {
+        constexpr int N = run_of<VPL, F32>();
 #pragma unroll
-        for (int i = 0; i < VPL; i += 4) {
-          const int e = dealt<LANES, VPL>(sub, i);
+        for (int i = 0; i < VPL; i += N) {
+          const int e = expert_of<LANES, VPL, F32>(sub, i);
           if (e >= a.E) continue;
-          if (a.f32)
+          if constexpr (F32) {
             st16(static_cast<float*>(a.grad_logits) + t * a.E + e,
                  u32x4{__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]),
                        __float_as_uint(x[i + 3])});
-          else
-            st4x2(static_cast<uint16_t*>(a.grad_logits) + t * a.E + e, pack_bf16x2(x[i], x[i + 1]),
-                  pack_bf16x2(x[i + 2], x[i + 3]));
+          } else {
+            uint16_t* to = static_cast<uint16_t*>(a.grad_logits) + t * a.E + e;
+            if constexpr (N == 8)
+              st16(to, u32x4{pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3]),
+                             pack_bf16x2(x[i + 4], x[i + 5]), pack_bf16x2(x[i + 6], x[i + 7])});
+            else
+              st4x2(to, pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3]));
+          }
         }
         continue;
       }
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
-        const int e = dealt<LANES, VPL>(sub, i);
+        const int e = expert_of<LANES, VPL, F32>(sub, i);
         if (e >= a.E) {
-        } else if (a.f32) {
+        } else if (F32) {
           static_cast<float*>(a.grad_logits)[t * a.E + e] = x[i];
         } else {
           static_cast<uint16_t*>(a.grad_logits)[t * a.E + e] = (uint16_t)pack_bf16x2(x[i], 0.0f);
@@ -337,10 +378,15 @@ __global__ __launch_bounds__(kBlock) void balance_backward_kernel(BalanceGradArg
   }
 }
 
+// launch(lanes, values of a lane, whether float32, whether sigmoid)
 template <typename F>
-hipError_t by_score(bool sigmoid, F&& launch) {
-  return sigmoid ? launch(std::integral_constant<bool, true>())
-                 : launch(std::integral_constant<bool, false>());
+hipError_t by_form(int E, bool f32, bool sigmoid, F&& launch) {
+  constexpr std::integral_constant<bool, true> yes;
+  constexpr std::integral_constant<bool, false> no;
+  return by_width(E, 1, 1, [&](auto lanes, auto vpl) {
+    return f32 ? sigmoid ? launch(lanes, vpl, yes, yes) : launch(lanes, vpl, yes, no)
+               : sigmoid ? launch(lanes, vpl, no, yes) : launch(lanes, vpl, no, no);
+  });
 }
 
 unsigned unit_blocks(int64_t seqs, int parts) {
@@ -350,17 +396,26 @@ unsigned unit_blocks(int64_t seqs, int parts) {
 
 }  // namespace
 
+// Tokens that a workgroup of `waves` wavefronts has at once.
+static int64_t tokens_at_once(int E, int waves) { return waves * (E <= 256 ? 4 : 1); }
+
+// A workgroup of 16 wavefronts for each compute unit: 32768 x 256 15.5 us, with twice or half
+// as many 21.0 and 16.8; 16384 x 512 14.9, with twice as many 19.1.  Up to eight rounds of
+// tokens one workgroup is quicker than two launches (256 x 64: 7.2 and 8.5 us).
 BalanceShape balance_shape(int64_t T, int E, int64_t seq) {
   BalanceShape s;
   s.seq = seq ? seq : T;
   s.seqs = seq ? T / seq : 1;
-  const int64_t step = E <= 256 ? 16 : 4;              // tokens that a workgroup has at once
-  int64_t parts = (s.seq + 4 * step - 1) / (4 * step);
-  const int64_t most = 1024 / (s.seqs > 0 ? s.seqs : 1);
+  const int64_t step = tokens_at_once(E, kMaxWaves);
+  int64_t parts = (s.seq + step - 1) / step;
+  const int64_t most = 256 / (s.seqs > 0 ? s.seqs : 1);
   parts = parts < most ? parts : most;
-  parts = parts > 1 ? parts : 1;
+  if (s.seq <= 8 * step || parts < 1) parts = 1;
   s.per = ((s.seq + parts - 1) / parts + step - 1) / step * step;
   s.parts = s.seq > 0 ? (int)((s.seq + s.per - 1) / s.per) : 1;
+  const int64_t a_wave = step / kMaxWaves, longest = s.seq < s.per ? s.seq : s.per;
+  const int64_t waves = (longest + a_wave - 1) / a_wave;
+  s.waves = (int)(waves < 1 ? 1 : waves < kMaxWaves ? waves : kMaxWaves);
   s.blocks = (E + 31) / 32;
   s.live_at = s.parts > 1 ? (size_t)s.seqs * s.parts * 2 * part_pitch(E) * 4 : 0;
   s.ticket_at = s.live_at + (s.parts > 1 ? (size_t)s.seqs * s.parts * 4 : 0);
@@ -369,31 +424,40 @@ BalanceShape balance_shape(int64_t T, int E, int64_t seq) {
   return s;
 }
 
-hipError_t launch_balance(const BalanceArgs& a, int blocks, hipStream_t stream) {
-  const hipError_t err = by_width(a.E, 1, 1, [&](auto lanes, auto vpl) {
-    return by_score(a.sigmoid, [&](auto sigmoid) {
-      const int vec = vpl.value >= 4 && vector_rows(a.logits, nullptr, a.pitch, a.E, 4, a.f32);
-      hipLaunchKernelGGL((balance_kernel<lanes.value, vpl.value, sigmoid.value>),
-                         dim3(unit_blocks(a.seqs, a.parts)), dim3(kBlock), 0, stream, a, vec);
-      return hipGetLastError();
-    });
+// The gradient's parts leave nothing behind: about 768 workgroups of four wavefronts, each
+// with up to eight rounds of tokens (us with one, two, four, eight rounds: 32768 x 128 bf16 14.7,
+// 10.7, 10.4, 14.0; 16384 x 512 18.2, 16.1, 13.8, 14.6; 2048 x 384 5.1, 5.3, 6.6, 9.2).
+void balance_grad_parts(BalanceGradArgs& a) {
+  const int64_t step = tokens_at_once(a.E, kWavesPerBlock);
+  const int64_t all = a.seqs * ((a.seq + step - 1) / step), rounds = (all + 767) / 768;
+  a.per = step * (rounds < 8 ? rounds : 8);
+  a.parts = (int)((a.seq + a.per - 1) / a.per);
+}
+
+hipError_t launch_balance(const BalanceArgs& a, const BalanceShape& shape, hipStream_t stream) {
+  const hipError_t err = by_form(a.E, a.f32, a.sigmoid, [&](auto lanes, auto vpl, auto f32,
+                                                            auto sigmoid) {
+    constexpr int run = run_of<vpl.value, f32.value>();
+    const int vec = vector_rows(a.logits, nullptr, a.pitch, a.E, run, f32.value);
+    hipLaunchKernelGGL((balance_kernel<lanes.value, vpl.value, f32.value, sigmoid.value>),
+                       dim3(unit_blocks(a.seqs, a.parts)), dim3(shape.waves * kWave), 0, stream, a,
+                       vec);
+    return hipGetLastError();
   });
   if (err != hipSuccess || a.parts == 1) return err;
-  hipLaunchKernelGGL(balance_join_kernel, dim3((unsigned)(a.seqs * blocks)), dim3(1024), 0, stream, a,
-                     blocks);
+  hipLaunchKernelGGL(balance_join_kernel, dim3((unsigned)(a.seqs * shape.blocks)), dim3(kBlock), 0,
+                     stream, a, shape.blocks);
   return hipGetLastError();
 }
 
 hipError_t launch_balance_backward(const BalanceGradArgs& a, hipStream_t stream) {
-  return by_width(a.E, 1, 1, [&](auto lanes, auto vpl) {
-    return by_score(a.sigmoid, [&](auto sigmoid) {
-      const int vec = vpl.value >= 4 &&
-                      vector_rows(a.logits, a.grad_logits, a.pitch, a.E, 4, a.f32) &&
-                      vector_rows(a.grad_sum, nullptr, a.E, a.E, 4, a.f32);
-      hipLaunchKernelGGL((balance_backward_kernel<lanes.value, vpl.value, sigmoid.value>),
-                         dim3(unit_blocks(a.seqs, a.parts)), dim3(kBlock), 0, stream, a, vec);
-      return hipGetLastError();
-    });
+  return by_form(a.E, a.f32, a.sigmoid, [&](auto lanes, auto vpl, auto f32, auto sigmoid) {
+    constexpr int run = run_of<vpl.value, f32.value>();
+    const int vec = vector_rows(a.logits, a.grad_logits, a.pitch, a.E, run, f32.value) &&
+                    vector_rows(a.grad_sum, nullptr, a.E, a.E, run, f32.value);
+    hipLaunchKernelGGL((balance_backward_kernel<lanes.value, vpl.value, f32.value, sigmoid.value>),
+                       dim3(unit_blocks(a.seqs, a.parts)), dim3(kBlock), 0, stream, a, vec);
+    return hipGetLastError();
   });
 }
 

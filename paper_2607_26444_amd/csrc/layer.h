@@ -55,6 +55,7 @@ struct BalanceShape {
   int64_t seqs;
   int64_t per;
   int32_t parts;        // of a sequence
+  int32_t waves;        // of a part's workgroup
   int32_t blocks;       // of 32 experts
   size_t live_at, ticket_at, piece_at, bytes;   // 0 bytes: one part
 };
@@ -81,7 +82,7 @@ struct BalanceArgs {
   float* pieces;               // [seqs][blocks]: slots, their share of the loss
 };
 
-hipError_t launch_balance(const BalanceArgs& a, int blocks, hipStream_t stream);
+hipError_t launch_balance(const BalanceArgs& a, const BalanceShape& shape, hipStream_t stream);
 
 struct BalanceGradArgs {
   const void* logits;
@@ -99,6 +100,8 @@ struct BalanceGradArgs {
   void* grad_logits;
 };
 
+// Sets per and parts from the sizes.
+void balance_grad_parts(BalanceGradArgs& a);
 hipError_t launch_balance_backward(const BalanceGradArgs& a, hipStream_t stream);
 
 // 8-bit output of a row kernel.
