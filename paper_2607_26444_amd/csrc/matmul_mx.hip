@@ -333,26 +333,41 @@ void matmul_mx_tile_kernel(MatmulMxArgs a, int pieces, int group) {
 // stage is 128 WK bytes of the depth, STAGES - 1 stages are on their way while one is
 // multiplied.  A wavefront loads its own weights (8 + 8 channels: with swiglu
 // gate and up channels, so that a lane and its partner 32 further on hold both
-// halves) with their scales, and an eighth of the rows and of theirs.  The sums of the WK
-// wavefronts meet in LDS.
+// halves) and an eighth of the rows.  The sums of the WK wavefronts meet in LDS.
+//
+// Scales come as pieces of 16 bytes of a row, whose lines cost more than their bytes: 8 bytes of
+// each row a stage, word by word, took 22 of 100 us (512 rows, 32 experts, 7168 x 4096 with
+// swiglu).  A row's pieces hold the stage, with WK = 1 two stages.
+template <int ROWS, int WC, int WK, int STAGES>
+struct MxStreamLds {
+  static constexpr int kBatch = WK == 1 ? 2 : 1;       // stages whose scales come together
+  static constexpr int kRowScales = kBatch * WK * kStageScales, kPieces = kRowScales / 16;
+  static constexpr int kScaleRows = WC * 16 + ROWS;    // the channels, then the rows
+  static constexpr int kScaleBytes = kScaleRows * kRowScales;
+  static constexpr int kPerWave = kScaleRows * kPieces / 8;
+  static_assert(kPerWave * 8 == kScaleRows * kPieces && kPerWave <= kWave, "one instruction");
+  static constexpr int kRowBytes = ROWS * kDepth * WK;
+  static constexpr int kCodes = kRowBytes + 16 * 1024;
+  static constexpr int kStage = kCodes + (kBatch == 1 ? kScaleBytes : 0);
+  static constexpr int kBatchAt = STAGES * kStage;     // two batches, where they are no part of stages
+  // what a tail's scales are read past the last row's
+  static constexpr int kBytes = kBatchAt + (kBatch == 1 ? 0 : 2 * kScaleBytes) + 64;
+  static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
+};
+
 template <int ROWS, int WC, int WK, int STAGES>
 __global__ __launch_bounds__(kTileThreads)
 void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
+  using Lds = MxStreamLds<ROWS, WC, WK, STAGES>;
   static_assert(WC * WK == 8, "eight wavefronts");
   constexpr int MT = ROWS / 16;
-  constexpr int kRowBytes = ROWS * kDepth * WK;
+  constexpr int kRowBytes = Lds::kRowBytes, kStage = Lds::kStage;
   constexpr int kRowLoads = WK * ROWS / 64;            // of a wavefront and stage
   static_assert(kRowLoads * 64 == WK * ROWS, "whole load instructions");
-  // scales: a wavefront's words of the weights (32), behind them those of the rows, in one
-  // instruction where they fit it
-  constexpr int kWords = ROWS * WK / 4;                // of the rows
-  constexpr int kTogether = kWords <= 32;
-  constexpr int kRowsAt = kTogether ? 128 : 256;
-  constexpr int kWaveScales = kRowsAt * 2;
-  constexpr int kScaleAt = kRowBytes + 16 * 1024;
-  constexpr int kStage = kScaleAt + 8 * kWaveScales;
-  constexpr int kLoads = 2 + kRowLoads + (kTogether ? 1 : 2);
-  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[STAGES * kStage];
+  // a batch of two stages is asked for before the codes of its first one, so that no
+  // count of loads on their way has to know of it
+  constexpr int kLoads = 2 + kRowLoads + (Lds::kBatch == 1 ? 1 : 0);
+  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[Lds::kBytes];
   static_assert(STAGES * kStage >= 8 * MT * kWave * 16, "sums meet there");
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   // 32 neighbouring tiles (mostly one window's, which share rows) to an XCD
@@ -371,44 +386,53 @@ void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
   const Rsrc rw0 = buffer_of(wbase, c0 < out ? 8 * a.K : 0);
   const Rsrc rw1 = buffer_of(wbase + (int64_t)(a.swiglu ? half : 8) * a.K, c1 < out ? 8 * a.K : 0);
   const uint32_t wo = (uint32_t)lr * (uint32_t)a.K + wk * kDepth + chunk * 16;
-  // Scale words come by address, lane by lane: those of rows and channels that are not there
-  // are another's (their outputs are not stored), those past the depth the row's first (they
-  // are masked).
-  const int pitch = mx_scale_bytes(2 * a.K);
-  const uint8_t *ps, *ps_rows = nullptr;
-  int shift, shift_rows = 0;                           // of the stage's depth
+
+  // A lane's piece of the scales, by address: that of a row or channel that is not there
+  // is another's (its outputs are not stored).  A row's last piece ends with it: scales
+  // are read as much further on.  Rows of less than a piece come word by word.
+  const int scale_bytes = mx_scale_bytes(2 * a.K);
+  const bool words = scale_bytes < 16;
+  const int last_piece = words ? 0 : scale_bytes - 16;
+  const int piece = (wave * Lds::kPerWave + lane) % Lds::kPieces * 16;
+  const uint8_t* scales;
   {
-    auto weights = [&](int l) {
-      int c = c0 + (l / 2 & 7);
-      if (l & 16) c += a.swiglu ? 0 : 8;
+    const int n = (wave * Lds::kPerWave + lane) / Lds::kPieces;
+    if (n < WC * 16) {
+      int c = t.piece * WC * step + n / 16 * step + (n & 7) + ((n & 8) && !a.swiglu ? 8 : 0);
       c = c < out ? c : out - 1;
-      if ((l & 16) && a.swiglu) c += half;
-      return a.w_scales + ((int64_t)t.expert * a.N + c) * pitch;
-    };
-    auto rows = [&](int l) {
-      const int n = wave * kWords + l;                 // word of [WK][ROWS][2]
-      const int r = n / 2 % ROWS;
-      return a.a_scales + (t.row + (r < t.rows ? r : t.rows - 1)) * a.a_scale_pitch;
-    };
-    auto depth_of = [&](int l) { return (wave * kWords + l) / 2 / ROWS * kDepth + (l & 1) * 64; };
-    const int l = lane & 31;
-    if (kTogether) {
-      ps = lane < 32 ? weights(l) : rows(l % kWords);
-      shift = lane < 32 ? wk * kDepth + (l & 1) * 64 : depth_of(l % kWords);
+      if ((n & 8) && a.swiglu) c += half;
+      scales = a.w_scales + ((int64_t)t.expert * a.N + c) * scale_bytes;
     } else {
-      ps = weights(l);
-      shift = wk * kDepth + (l & 1) * 64;
-      ps_rows = rows(lane);
-      shift_rows = depth_of(lane);
+      const int r = n - WC * 16;
+      scales = a.a_scales + (t.row + (r < t.rows ? r : t.rows - 1)) * a.a_scale_pitch;
     }
   }
-  auto load_words = [&](const uint8_t* p, int k, uint8_t* to) {
-    const uint8_t* from = p + (k < a.K ? k / 16 : 0);
+  auto scales_at = [&](int k0, uint32_t at) -> uint32_t {   // of the stage at `at`
+    return Lds::kBatch == 1 ? at + Lds::kCodes
+                            : Lds::kBatchAt + (k0 / (2 * kDepth) & 1) * Lds::kScaleBytes;
+  };
+  if (words) {                                         // the only scales there are
+    if (lane < Lds::kPerWave) {
+      u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (piece + i * 4 < scale_bytes) v[i] = ld4(scales + piece + i * 4);
+      *reinterpret_cast<u32x4*>(s_mem + scales_at(0, 0) + (wave * Lds::kPerWave + lane) * 16) = v;
+    }
+    scales = a.w;                                      // later stages read 16 bytes of no use
+  }
+  auto load_scales = [&](int k0, uint32_t at) {
+    if (lane >= Lds::kPerWave || (words && k0 == 0)) return;
+    const int want = (Lds::kBatch == 1 ? k0 / 16 : k0 / (2 * kDepth) * 16) + piece;
+    const uint8_t* from = scales + (want < last_piece ? want : last_piece);
     __builtin_amdgcn_global_load_lds(
         (const __attribute__((address_space(1))) uint32_t*)(uintptr_t)from,
-        (__attribute__((address_space(3))) uint32_t*)(lds_u8*)to, 4, 0, 0);
+        (__attribute__((address_space(3))) uint32_t*)(lds_u8*)(s_mem + scales_at(k0, at) +
+                                                               wave * Lds::kPerWave * 16),
+        16, 0, 0);
   };
   auto load = [&](int k0, uint32_t at) {               // past the depth: zeros
+    if (Lds::kBatch == 1 || !(k0 & kDepth)) load_scales(k0, at);
     const uint32_t w = (uint32_t)k0 + wk * kDepth + chunk * 16 < (uint32_t)a.K ? wo + k0 : kOutside;
     uint8_t* to = s_mem + at + kRowBytes + wave * 2048;
     load_to_lds(rw0, w, (lds_u8*)to);
@@ -420,16 +444,13 @@ void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
       load_to_lds(ra, k < (uint32_t)a.K ? (uint32_t)r * (uint32_t)a.a_pitch + k : kOutside,
                   (lds_u8*)(s_mem + at + n * 1024));
     }
-    uint8_t* scales = s_mem + at + kScaleAt + wave * kWaveScales;
-    load_words(ps, k0 + shift, scales);
-    if (!kTogether) load_words(ps_rows, k0 + shift_rows, scales + kRowsAt);
   };
 #pragma unroll
   for (int s = 0; s + 1 < STAGES; ++s) load(s * kDepth * WK, s * kStage);
 
   const int row = lane & 15, quarter = lane / 16;
   const uint32_t place = row * kDepth + ((quarter ^ (row & 7)) * 16);
-  const uint32_t at_sw = kScaleAt + wave * kWaveScales + row * kStageScales + quarter * 2;
+  const uint32_t mine = row * Lds::kRowScales + quarter * 2;
   f32x4 acc[MT] = {};
   auto multiply = [&](auto row_tiles) {
     constexpr int M = row_tiles.value;
@@ -438,15 +459,18 @@ void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
       meet<(STAGES - 2) * kLoads>();                   // this stage is there, the last is read
       load(k0 + (STAGES - 1) * kDepth * WK, fill);
       i32x4 wv[2], av[2][M];
-      const uint32_t mask = depth_mask(k0 + wk * kDepth, quarter, a.K);
-      const int sw = (int)(two_scales(s_mem + at + at_sw) & mask);
+      const int k = k0 + wk * kDepth;                  // the wavefront's part of the stage
+      const uint32_t mask = depth_mask(k, quarter, a.K);
+      // its scales in their piece, and how far that lies before the place it was meant for
+      const int first = k / 256 * 16;
+      const int behind = words || first < last_piece ? 0 : first - last_piece;
+      const uint32_t ps = scales_at(k0, at) + (Lds::kBatch == 1 ? k / 16 - k0 / 16 : k / 16 - first) +
+                          (behind < 16 ? behind : 16) + mine;
+      const int sw = (int)(two_scales(s_mem + ps + wc * 16 * Lds::kRowScales) & mask);
       int sa[M];
 #pragma unroll
-      for (int i = 0; i < M; ++i) {
-        const int n = (wk * ROWS + i * 16 + row) * 2;  // word of [WK][ROWS][2]
-        const uint32_t p = kScaleAt + n / kWords * kWaveScales + kRowsAt + n % kWords * 4 + quarter * 2;
-        sa[i] = (int)(two_scales(s_mem + at + p) & mask);
-      }
+      for (int i = 0; i < M; ++i)
+        sa[i] = (int)(two_scales(s_mem + ps + (WC + i) * 16 * Lds::kRowScales) & mask);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t p = at + (place ^ (h * 64));
