@@ -202,6 +202,7 @@ struct MatmulMxArgs : MatmulShape {
   const uint8_t* w;
   const uint8_t* w_scales;   // rows of mx_scale_bytes
   uint16_t* y;
+  int32_t stream_w;          // set by the launch: the weights are read once
 };
 
 hipError_t launch_matmul_mx(const MatmulMxArgs& a, hipStream_t stream);

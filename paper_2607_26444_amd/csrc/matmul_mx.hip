@@ -10,9 +10,11 @@
 // Which of a row's blocks meet in one instruction is free as long as both operands agree: of a
 // stage's eight chunks of 16 bytes (a block of 32 codes each) lane quarter q takes the chunks 2 q
 // and 2 q + 1, one to an instruction, so that their two scales are neighbouring bytes which
-// a lane reads at once and the instructions select.  In LDS chunk 2 q + h of row r is at place
-// (q + 4 h) ^ (r & 7), which no two of the lanes that read together share (2 q + h ^ (r & 7):
-// 46 M cycles of bank conflicts beside 104 M of reads).
+// a lane reads at once and the instructions select.  In LDS chunk c of row r is at place
+// c' ^ (r & 7), c' its number with the two low bits exchanged: lanes that read together touch
+// all banks (with c itself 46 M cycles of conflicts beside 104 M of reads), lanes that
+// load together have half a line (an order that spread them over whole lines made twice the
+// requests).
 
 #include <type_traits>
 
@@ -23,10 +25,16 @@ namespace {
 
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 
-// The chunk of its row that a lane loads to its place.
+// The chunk of its row that a lane loads to its place: four neighbouring lanes have half a
+// line.
 __device__ __forceinline__ int chunk_of(int lane) {
   const int place = (lane & 7) ^ (lane / 8);
-  return (place & 3) * 2 + place / 4;
+  return (place & 4) | (place & 1) << 1 | (place >> 1 & 1);
+}
+
+// Place of a lane's first chunk in a row of LDS; its second one is two further, 32 bytes.
+__device__ __forceinline__ uint32_t place_of(int row, int quarter) {
+  return row * kDepth + (((quarter & 2) << 1 | (quarter & 1)) ^ (row & 7)) * 16;
 }
 
 constexpr int kStageScales = kDepth / 16;   // scale bytes of a row and stage
@@ -52,22 +60,52 @@ __device__ __forceinline__ uint32_t depth_mask(int k, int quarter, int K) {
   return (at < K ? 0x00FF00FFu : 0u) | (at + 16 < K ? 0xFF00FF00u : 0u);
 }
 
-__device__ __forceinline__ void load_scales_to_lds(Rsrc r, uint32_t offset, lds_u8* to) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 4, (int)offset, 0, 0, 0);
+// The same for weights that are read once.
+__device__ __forceinline__ void stream_to_lds(Rsrc r, uint32_t offset, lds_u8* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, (int)offset, 0, 0, kLoadNonTemporal);
 }
 
-// LDS of the kernel of tiles of HEIGHT rows: stages of rows, weights and their scales, and the
-// windows.
+// f(0) to f(N - 1), their arguments constants.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>());
+    each<N, I + 1>(f);
+  }
+}
+
+// Tiles of 256 or 128 rows x 256 channels through LDS: eight wavefronts, each half the rows x 64
+// channels; stages of 128 bytes of the depth go from memory into LDS by the loads themselves.
+//
+// Scales.  A lane needs two bytes of every row and stage; a request for any of a row's bytes moves
+// a whole line to the compute unit, so that taking them stage by stage made a third of all
+// requests.  With tiles of 256 rows they come for four stages at once (32 bytes of a row), half
+// of a wavefront's rows at a time; before every second stage each thread takes 16 bytes of its own
+// row from there and puts them, by quarter and tile, where a lane finds its words of four tiles
+// in one read.
+//
+// Bound by what the compute units' loads take from the L2 cache: 32768 rows, 16 experts, 7168 x
+// 4096 with swiglu 490 us (3.9 PFLOP/s), with the loads left out 370, without those of the
+// scales alone 445.  On the way there: scales word by word and stage by stage 527; 16 bytes every
+// second stage 495; stages of half the depth, four of them, 510; four wavefronts with 128 x 128
+// each 523; lines asked for earlier, to have them in the L2 cache, +4 to 8%.
+
+// Scales of a row and pair of stages.
+constexpr int kPairScales = 2 * kStageScales;
+
+// LDS of the kernel of tiles of HEIGHT rows: stages of rows and weights; the scales of two stages
+// in the order of the lanes, and as they came; the workgroup's next tiles.
 template <int HEIGHT>
 struct MxTileLds {
   static constexpr int kStages = HEIGHT == 256 ? 2 : 3;
   static constexpr int kRowBytes = HEIGHT * kDepth;
-  static constexpr int kRowScaleAt = kRowBytes + kTile * kDepth;
-  static constexpr int kScaleAt = kRowScaleAt + HEIGHT * kStageScales;   // of the weights
-  static constexpr int kStageBytes = kScaleAt + kTile * kStageScales;
-  static constexpr int kWindowAt = kStages * kStageBytes;
-  static constexpr int kWindows = HEIGHT == 256 ? MOE_MAX_EXPERTS : kMxTile128Experts;
-  static constexpr int kBytes = kWindowAt + 3 * kWindows * 4;
+  static constexpr int kStageBytes = kRowBytes + kTile * kDepth;
+  static constexpr int kScaleAt = kStages * kStageBytes;
+  static constexpr bool kFourStages = HEIGHT == 256;   // scales come for four stages, else for two
+  static constexpr int kRawAt = kScaleAt + kTileThreads * kPairScales;
+  static constexpr int kListAt = kRawAt + (kFourStages ? kTileThreads * 2 * kPairScales : 0);
+  static constexpr int kBytes = kListAt + kWave * 16;
+  static_assert(3 * MOE_MAX_EXPERTS * 4 <= kScaleAt, "the windows lie there before the stages");
   static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
 };
 
@@ -75,11 +113,17 @@ struct MxTileLds {
 template <int HEIGHT>
 struct MxTileLoads {
   using Lds = MxTileLds<HEIGHT>;
-  Rsrc ra, rw, rsa, rsw;
+  Rsrc ra, rw;
   uint32_t ao, wo;             // of instruction 0
-  uint32_t sao, swo;
   int a_step, w_step;          // from one instruction to the next
-  int K, chunk, wave, word;
+  const uint8_t* scales;       // of the thread's row or channel
+  // of the wavefront's 64 rows, in two sets of 32 (tiles of 16 in turn): the second `other` further
+  const uint8_t* set;
+  int64_t other;
+  int set_bytes, other_bytes;
+  uint32_t so;
+  int K, wave, scale_bytes, last_piece;
+  const uint8_t* spare;        // 16 bytes that may be read
   uint8_t* s_tile;
 
   __device__ __forceinline__ MxTileLoads(const MatmulMxArgs& a, const Tile& t, int tid, uint8_t* lds)
@@ -87,11 +131,10 @@ struct MxTileLoads {
     const int lane = tid & (kWave - 1);
     wave = uniform(tid / kWave);
     // instruction j of a wavefront fills LDS rows (j * 8 + wave) * 8 + lane / 8
-    const int lr = lane / 8, half = a.N / 2, c0 = t.piece * (a.swiglu ? kTile / 2 : kTile);
-    chunk = chunk_of(lane);
-    const int r = wave * 8 + lr;
-    ao = (uint32_t)r * (uint32_t)a.a_pitch + chunk * 16;
-    wo = (uint32_t)channel_of(r, a.swiglu) * (uint32_t)K + chunk * 16;
+    const int half = a.N / 2, c0 = t.piece * (a.swiglu ? kTile / 2 : kTile);
+    const int r = wave * 8 + lane / 8;
+    ao = (uint32_t)r * (uint32_t)a.a_pitch + chunk_of(lane) * 16;
+    wo = (uint32_t)channel_of(r, a.swiglu) * (uint32_t)K + chunk_of(lane) * 16;
     a_step = 64 * a.a_pitch;
     w_step = (a.swiglu ? 32 : 64) * K;
     const int channels = (a.swiglu ? half : a.N) - c0, most = a.swiglu ? kTile / 2 : kTile;
@@ -99,170 +142,277 @@ struct MxTileLoads {
     const int64_t first = (int64_t)t.expert * a.N + c0;
     ra = buffer_of(a.a + t.row * a.a_pitch, (t.rows - 1) * a.a_pitch + K);
     rw = buffer_of(a.w + (first + (a.swiglu && (wave & 2) ? half : 0)) * K, held * K);
-    // scales: two words of a row by two lanes.  Of the weights a wavefront has the rows of the
-    // LDS tiles wave & 1 and (wave & 1) + 2 of a block of 64, which with swiglu are all gate
-    // or all up channels.
-    const int pitch = mx_scale_bytes(2 * K);
-    word = (lane & 1) * 4;
-    const int n = wave / 2 * 64 + (lane / 32) * 32 + (wave & 1) * 16 + (lane / 2 & 15);
-    swo = (uint32_t)channel_of(n, a.swiglu) * (uint32_t)pitch + word;
-    sao = (uint32_t)(wave * (HEIGHT / 8) + lane / 2) * (uint32_t)a.a_scale_pitch + word;
-    rsa = buffer_of(a.a_scales + t.row * a.a_scale_pitch, (t.rows - 1) * a.a_scale_pitch + pitch);
-    rsw = buffer_of(a.w_scales + (first + (a.swiglu && (wave & 1) ? half : 0)) * pitch, held * pitch);
+
+    scale_bytes = mx_scale_bytes(2 * K);
+    last_piece = scale_bytes > kPairScales ? scale_bytes - kPairScales : 0;
+    spare = a.w;
+    const int in_set = (lane / 2 & 15) + (lane / 2 & 16) * 2;   // row of the set by two lanes
+    if (wave < HEIGHT / 64) {
+      const int64_t pitch = a.a_scale_pitch;
+      set = a.a_scales + t.row * pitch;
+      scales = set + (tid < t.rows ? tid : t.rows - 1) * pitch;
+      other = 16 * pitch;
+      set_bytes = (t.rows - 1) * a.a_scale_pitch + scale_bytes;
+      other_bytes = t.rows > 16 ? set_bytes - 16 * a.a_scale_pitch : 0;
+      so = (uint32_t)(wave * 64 + in_set) * (uint32_t)a.a_scale_pitch;
+    } else {                                           // tiles 1 and 3: up channels, or 4 further
+      const int n = tid - HEIGHT, c = channel_of(n, a.swiglu);
+      set = a.w_scales + first * scale_bytes;
+      scales = set + ((c < held ? c : held - 1) + (int64_t)(a.swiglu && (n & 16) ? half : 0)) *
+                         scale_bytes;
+      other = (int64_t)(a.swiglu ? half : 4) * scale_bytes;
+      set_bytes = held * scale_bytes;
+      other_bytes = a.swiglu ? set_bytes : set_bytes - 4 * scale_bytes;   // 8 are held at least
+      so = (uint32_t)channel_of((wave - HEIGHT / 64) * 64 + in_set, a.swiglu) * (uint32_t)scale_bytes;
+    }
+    if (scale_bytes < kPairScales) set_bytes = other_bytes = 0;
   }
 
-  // A stage into LDS; past the depth and past the tile's rows and channels:
-  // zeros.  ROW_LOADS: as many 64 rows as the tile multiplies.
-  template <int ROW_LOADS = HEIGHT / 64>
-  __device__ __forceinline__ void stage(int k0, uint32_t buf, int lane) const {
-    const bool in = k0 + chunk * 16 < K;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (j < ROW_LOADS)
-        load_to_lds(ra, in ? ao + (k0 + j * a_step) : kOutside,
-                    (lds_u8*)(s_tile + buf + (j * 8 + wave) * 1024));
-      load_to_lds(rw, in ? wo + (k0 + j * w_step) : kOutside,
+  // A stage behind the depth is out of every range: zeros.
+  __device__ __forceinline__ int depth_of(int k0) const { return k0 < K ? k0 : 0x70000000; }
+
+  // Load `n` of a stage: rows and weights in turn, ROW_LOADS + 4 in all (ROW_LOADS: as many 64
+  // rows as the tile multiplies).  Past the tile's rows and channels: zeros.  Past the depth:
+  // those or the next row's codes, whose scales are 0.
+  template <int ROW_LOADS>
+  __device__ __forceinline__ void part(int n, int k0, uint32_t buf) const {
+    const bool is_row = n < 2 * ROW_LOADS && n % 2 == 0;
+    const int j = n < 2 * ROW_LOADS ? n / 2 : n - ROW_LOADS;
+    if (is_row)
+      load_to_lds(ra, ao + (k0 + j * a_step), (lds_u8*)(s_tile + buf + (j * 8 + wave) * 1024));
+    else
+      load_to_lds(rw, wo + (k0 + j * w_step),
                   (lds_u8*)(s_tile + buf + Lds::kRowBytes + (j * 8 + wave) * 1024));
-    }
-    // a word of scales covers 64 bytes of codes
-    const bool some = k0 + word * 16 < K;
-    const uint32_t at = (uint32_t)k0 / 16;
-    if (HEIGHT == 256 || lane < HEIGHT / 4)
-      load_scales_to_lds(rsa, some ? sao + at : kOutside,
-                         (lds_u8*)(s_tile + buf + Lds::kRowScaleAt + wave * HEIGHT));
-    load_scales_to_lds(rsw, some ? swo + at : kOutside,
-                       (lds_u8*)(s_tile + buf + Lds::kScaleAt + wave * kTile));
+  }
+
+  // First byte of a pair's 16 of a row; the last ones end with the row.
+  __device__ __forceinline__ int piece_of(int pair) const {
+    const int at = pair * kPairScales;
+    return at < last_piece ? at : last_piece;
+  }
+  // The thread's scales of a pair.
+  __device__ __forceinline__ u32x4 fetch(int pair) const {
+    return ld16(scale_bytes < kPairScales ? spare : scales + piece_of(pair));
+  }
+  // Those of the first pair also where a row has less than 16 bytes.
+  __device__ __forceinline__ u32x4 fetch_first() const {
+    if (scale_bytes >= kPairScales) return ld16(scales);
+    u32x4 v = {ld4(scales), 0, 0, 0};
+    if (scale_bytes > 4) v.y = ld4(scales + 4);
+    if (scale_bytes > 8) v.z = ld4(scales + 8);
+    return v;
+  }
+  // The scales of a pair and the next one of a set of the wavefront's rows into LDS.
+  __device__ __forceinline__ void ask(int which, int pair, int lane) const {
+    const Rsrc r = buffer_of(set + (which ? other : 0), which ? other_bytes : set_bytes);
+    load_to_lds(r, so + (lane & 1 ? piece_of(pair + 1) : piece_of(pair)),
+                (lds_u8*)(s_tile + Lds::kRawAt + wave * 2048 + which * 1024));
+  }
+  // The thread's scales of a pair from there: set 0 was asked for at even pairs, set 1 at odd ones.
+  __device__ __forceinline__ u32x4 asked(int pair, int tid) const {
+    const int l = tid & 63;
+    const uint32_t at = tid / 64 * 2048 + (l & 16) * 64 + ((l & 15) + (l & 32) / 2) * 32 + (l & 16);
+    return *reinterpret_cast<const u32x4*>(s_tile + Lds::kRawAt + (at ^ (pair & 1) * 16));
+  }
+  // A pair's scales in their places in LDS: for each quarter the words (two scales of either stage)
+  // of four neighbouring tiles of 16.  What lies behind the depth is 0.
+  __device__ __forceinline__ void place(u32x4 v, int pair, int tid) const {
+    uint32_t d[4] = {v.x, v.y, v.z, v.w};
+    const int at = pair * kPairScales, ahead = at - last_piece;   // bytes before the first stage
+    d[0] = ahead < 4 ? d[0] : ahead < 8 ? d[1] : ahead < 12 ? d[2] : d[3];
+    d[1] = ahead < 4 ? d[1] : ahead < 8 ? d[2] : d[3];
+    d[2] = ahead < 4 ? d[2] : d[3];
+    int left = K / 16 - at;                            // scales there are
+    left = left < 0 ? 0 : left > 16 ? 16 : left;
+    const uint64_t low = left < 8 ? (1ull << left * 8) - 1 : ~0ull;
+    const uint64_t high = left < 8 ? 0ull : left < 16 ? (1ull << (left - 8) * 8) - 1 : ~0ull;
+    d[0] &= (uint32_t)low;
+    d[1] &= (uint32_t)(low >> 32);
+    d[2] &= (uint32_t)high;
+    d[3] &= (uint32_t)(high >> 32);
+    uint8_t* to = s_tile + Lds::kScaleAt + tid / 64 * 1024 + (tid & 15) * 16 + (tid / 16 & 3) * 4;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<uint32_t*>(to + q * 256) =
+          __builtin_amdgcn_perm(d[2 + q / 2], d[q / 2], q & 1 ? 0x07060302u : 0x05040100u);
   }
 };
 
+// A tile's first stages and scales.
+template <int HEIGHT>
+__device__ __forceinline__ void begin_tile(const MatmulMxArgs& a, const Tile& t, int tid,
+                                           uint8_t* s_tile) {
+  using Lds = MxTileLds<HEIGHT>;
+  const MxTileLoads<HEIGHT> loads(a, t, tid, s_tile);
+#pragma unroll
+  for (int s = 0; s < Lds::kStages; ++s)
+#pragma unroll
+    for (int n = 0; n < HEIGHT / 64 + 4; ++n)
+      loads.template part<HEIGHT / 64>(n, loads.depth_of(s * kDepth), s * Lds::kStageBytes);
+  if constexpr (Lds::kFourStages) {
+    loads.ask(0, 0, tid & (kWave - 1));
+    loads.ask(1, 1, tid & (kWave - 1));
+  }
+  loads.place(loads.fetch_first(), 0, tid);
+}
+
 // One tile whose wavefronts take MT x 16 rows each: 8 for a full tile, 4 or 2
 // for the last rows of a window.  Its first stages have been asked for; those of
-// `next` are before its own outputs are computed and stored.
+// `next` are before its own outputs are computed and stored.  stores: what the tile before
+// left on its way after them.
 template <int HEIGHT, int MT>
 __device__ __forceinline__ void multiply_mx_tile(const MatmulMxArgs& a, const Tile& t,
-                                                 const Tile& next, int tid, uint8_t* s_tile) {
+                                                 const Tile& next, int tid, uint8_t* s_tile,
+                                                 int stores) {
   using Lds = MxTileLds<HEIGHT>;
   constexpr int NT = 4;
-  constexpr int kLoads = MT / 2 + 4 + 2;               // of a wavefront and stage
+  constexpr int kLoads = MT / 2 + 4;                   // of a wavefront and stage
   const int lane = tid & (kWave - 1), wave = uniform(tid / kWave);
   const MxTileLoads<HEIGHT> loads(a, t, tid, s_tile);
 
   const int wm = wave / 4, wn = wave % 4;              // 2 x 4 wavefronts
   const int row = lane & 15, quarter = lane / 16;
-  const uint32_t place = row * kDepth + ((quarter ^ (row & 7)) * 16);
+  const uint32_t place = place_of(row, quarter);
   const uint32_t at_a = wm * (MT * 16 * kDepth) + place;
   const uint32_t at_w = Lds::kRowBytes + wn * (64 * kDepth) + place;
-  const uint32_t mine = row * kStageScales + quarter * 2;
-  const uint32_t at_sa = Lds::kRowScaleAt + wm * (MT * 16 * kStageScales) + mine;
-  const uint32_t at_sw = Lds::kScaleAt + wn * (64 * kStageScales) + mine;
+  const uint32_t mine = Lds::kScaleAt + quarter * 256 + row * 16;
+  const uint32_t at_sa = wm * MT / 4 * 1024 + (MT == 2 ? wm * 8 : 0) + mine;
+  const uint32_t at_sw = (HEIGHT / 64 + wn) * 1024 + mine;
   f32x4 acc[MT][NT] = {};
 
-  i32x4 av[2][MT], wv[2][NT];
-  auto read = [&](int h, uint32_t buf) {               // half a stage into registers
-    const uint8_t* pw = s_tile + (at_w ^ (h * 64)) + buf;
-    const uint8_t* pa = s_tile + (at_a ^ (h * 64)) + buf;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) wv[h][j] = *(const i32x4*)(pw + j * 16 * kDepth);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) av[h][i] = *(const i32x4*)(pa + i * 16 * kDepth);
+  // A stage is U units of 16 rows (the first halves of the chunks, then the second), NT
+  // instructions each.  Unit u asks for the rows of unit u + D; from unit B on all of the
+  // stage is in registers.
+  constexpr int U = 2 * MT, D = U == 16 ? 4 : U == 8 ? 3 : 2, B = U - D + 1, kLeft = U - B;
+  constexpr int R = U < 8 ? U : 8, kPlace = B / 2 + 1;
+  i32x4 av[R], wv[2][NT];
+  uint32_t sa[MT], sw[NT], sa_next[MT], sw_next[NT];   // scales of two stages
+  auto read_a = [&](int u, uint32_t buf) {
+    av[u % R] = *(const i32x4*)(s_tile + (at_a ^ (u / MT * 32)) + buf + u % MT * 16 * kDepth);
   };
-  uint32_t sa[MT / 2], sw[NT / 2];                     // two tiles' scales to a word
-  auto read_scales = [&](uint32_t buf) {
-    const uint8_t* pw = s_tile + at_sw + buf;
-    const uint8_t* pa = s_tile + at_sa + buf;
-    // tiles j and j + 2 lie in one wavefront's part
-#pragma unroll
-    for (int j = 0; j < NT / 2; ++j)
-      sw[j] = two_scales(pw + j * 32 * kStageScales) |
-              two_scales(pw + (j * 32 + 16) * kStageScales) << 16;
-#pragma unroll
-    for (int i = 0; i < MT / 2; ++i)
-      sa[i] = two_scales(pa + i * 32 * kStageScales) |
-              two_scales(pa + (i * 32 + 16) * kStageScales) << 16;
+  auto read_w = [&](int h, int j, uint32_t buf) {
+    wv[h][j] = *(const i32x4*)(s_tile + (at_w ^ (h * 32)) + buf + j * 16 * kDepth);
   };
-  auto multiply = [&](auto half, int i0, int i1) {
-    constexpr int h = half.value;
+  auto read_scales = [&](uint32_t (&a4)[MT], uint32_t (&w4)[NT]) {
+    const u32x4 w = *(const u32x4*)(s_tile + at_sw);
 #pragma unroll
-    for (int i = i0; i < i1; ++i) {
+    for (int j = 0; j < NT; ++j) w4[j] = w[j];
+    if constexpr (MT == 2) {
+      const u32x2 v = *(const u32x2*)(s_tile + at_sa);
+      a4[0] = v.x;
+      a4[1] = v.y;
+    } else {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int s = (int)sw[j & 1], r = (int)sa[i / 2];   // channel tiles j and j + 2 share a word
-        if (j < 2 && i % 2 == 0) acc[i][j] = multiply_mx<h, h>(wv[h][j], av[h][i], acc[i][j], s, r);
-        if (j < 2 && i % 2 == 1) acc[i][j] = multiply_mx<h, h + 2>(wv[h][j], av[h][i], acc[i][j], s, r);
-        if (j >= 2 && i % 2 == 0) acc[i][j] = multiply_mx<h + 2, h>(wv[h][j], av[h][i], acc[i][j], s, r);
-        if (j >= 2 && i % 2 == 1) acc[i][j] = multiply_mx<h + 2, h + 2>(wv[h][j], av[h][i], acc[i][j], s, r);
+      for (int c = 0; c < MT / 4; ++c) {
+        const u32x4 v = *(const u32x4*)(s_tile + at_sa + c * 1024);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a4[4 * c + i] = v[i];
       }
     }
   };
-  constexpr std::integral_constant<int, 0> kFirst;
-  constexpr std::integral_constant<int, 1> kSecond;
-
-  // Stage s is in LDS at s % kStages.  Within a turn the wavefronts meet once: by
-  // then each has read the last of stage s into registers, and its loads of
-  // stage s + 1, asked for kStages - 1 turns ago, have arrived.  Half of the matrix
-  // instructions of a register set stand on either side of the barrier.
-  meet<0>();                                           // the first stages are there
+  // The first stages are there; the stores after them may be on their way.
+  if (stores >= 16) meet<16>();
+  else if (stores >= 8) meet<8>();
+  else if (stores >= 4) meet<4>();
+  else if (stores >= 2) meet<2>();
+  else meet<0>();
   uint32_t buf = 0;
-  read(0, 0);
-  for (int k0 = 0; k0 < a.K; k0 += kDepth) {
-    read_scales(buf);
-    if (k0 + kDepth > a.K) {
-      const uint32_t mask = depth_mask(k0, quarter, a.K);
 #pragma unroll
-      for (int j = 0; j < NT / 2; ++j) sw[j] &= mask;
+  for (int u = 0; u < D; ++u) read_a(u, 0);
 #pragma unroll
-      for (int i = 0; i < MT / 2; ++i) sa[i] &= mask;
+  for (int j = 0; j < NT; ++j) read_w(0, j, 0);
+  read_scales(sa, sw);
+  u32x4 row_scales = {};
+  if constexpr (!Lds::kFourStages) row_scales = loads.fetch(1);
+  // Stage s is in LDS at s % kStages.  Within a turn the wavefronts meet once: by then each has
+  // asked for the last of stage s, and its loads of stage s + 1 have arrived.  The scales of the
+  // next two stages are placed before that in every second turn, and read behind it.
+  auto turn = [&](auto parity, int k0) {
+    constexpr int p = parity.value;
+    const int fill = loads.depth_of(k0 + Lds::kStages * kDepth);
+    uint32_t next_buf = buf + Lds::kStageBytes == Lds::kScaleAt ? 0 : buf + Lds::kStageBytes;
+    if constexpr (Lds::kStages == 2) next_buf = Lds::kStageBytes - buf;
+    __builtin_amdgcn_sched_barrier(0);
+    each<U>([&](auto unit) {
+      constexpr int u = unit.value, h = u / MT, i = u % MT, x = u - B;
+      if constexpr (u == B) meet<(Lds::kStages - 2) * kLoads>();
+      if constexpr (u + D < U) read_a(u + D, buf);
+      if constexpr (h == 0) {
+#pragma unroll
+        for (int j = i * NT / MT; j < (i + 1) * NT / MT; ++j) read_w(1, j, buf);
+      }
+      const int pair = k0 / (2 * kDepth);
+      if constexpr (p == 1 && u == kPlace - 1 && Lds::kFourStages)
+        row_scales = loads.asked(pair + 1, tid);
+      if constexpr (p == 1 && u == kPlace) loads.place(row_scales, pair + 1, tid);
+      if constexpr (p == 1 && u == B) {
+        if constexpr (Lds::kFourStages) loads.ask(pair & 1, pair + 2, lane);
+        else row_scales = loads.fetch(pair + 2);
+      }
+      if constexpr (u >= B) {
+#pragma unroll
+        for (int n = x * kLoads / kLeft; n < (x + 1) * kLoads / kLeft; ++n)
+          loads.template part<MT / 2>(n, fill, buf);
+#pragma unroll
+        for (int j = x * NT / kLeft; j < (x + 1) * NT / kLeft; ++j) read_w(0, j, next_buf);
+#pragma unroll
+        for (int v = x * D / kLeft; v < (x + 1) * D / kLeft; ++v) read_a(v, next_buf);
+        if constexpr (p == 1 && u == B) read_scales(sa_next, sw_next);
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        acc[i][j] = multiply_mx<h + 2 * p, h + 2 * p>(wv[h][j], av[u % R], acc[i][j], (int)sw[j],
+                                                      (int)sa[i]);
+    });
+    buf = next_buf;
+    if constexpr (p == 1) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) sa[i] = sa_next[i];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) sw[j] = sw_next[j];
     }
-    read(1, buf);
-    multiply(kFirst, 0, MT / 2);
-    interleave<kIssueLdsRead, MT + NT, 1>();
-    meet<(Lds::kStages - 2) * kLoads>();
-    loads.template stage<MT / 2>(k0 + Lds::kStages * kDepth, buf, lane);
-    multiply(kFirst, MT / 2, MT);
-    if constexpr (Lds::kStages == 2) buf = Lds::kStageBytes - buf;
-    else buf = buf + Lds::kStageBytes == Lds::kWindowAt ? 0 : buf + Lds::kStageBytes;
-    __builtin_amdgcn_sched_barrier(0);
-    read(0, buf);
-    multiply(kSecond, 0, MT);
-    interleave<kIssueLdsRead, MT + NT, MT / 4 + 1 < 2 ? 1 : 2>();
-    // the reads stay in this turn
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+  };
+  // No branch within two turns: one there cost as much as a tenth of the loop.
+  int k0 = 0;
+  for (; k0 + kDepth < a.K; k0 += 2 * kDepth) {
+    turn(std::integral_constant<int, 0>(), k0);
+    turn(std::integral_constant<int, 1>(), k0 + kDepth);
   }
+  if (k0 < a.K) turn(std::integral_constant<int, 0>(), k0);
   meet<0>();                                           // loads past the end have landed
 
-  if (next.rows) {
-    const MxTileLoads<HEIGHT> first(a, next, tid, s_tile);
-#pragma unroll
-    for (int n = 0; n < Lds::kStages; ++n) first.stage(n * kDepth, n * Lds::kStageBytes, lane);
-  }
+  if (next.rows) begin_tile<HEIGHT>(a, next, tid, s_tile);
 
+  // Rows and channels that are not there lie outside the range, so that every wavefront makes
+  // the same number of stores.
   const int out = a.swiglu ? a.N / 2 : a.N;
   const int c0 = t.piece * (a.swiglu ? kTile / 2 : kTile) +
                  (a.swiglu ? wn * 32 + quarter * 8 : wn * 64 + quarter * 16);
+  const Rsrc ry = buffer_of(reinterpret_cast<uint8_t*>(a.y + t.row * out), t.rows * out * 2);
+  const uint32_t to = (uint32_t)(wm * (MT * 16) + row) * (uint32_t)out * 2;
+  const uint32_t at0 = c0 < out ? to + c0 * 2 : kOutside;
+  const uint32_t at1 = c0 + 8 < out ? to + c0 * 2 + 16 : kOutside;
+  if (a.swiglu) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int r = wm * (MT * 16) + i * 16 + row;
-    if (r >= t.rows) continue;
-    uint16_t* y = a.y + (t.row + r) * out;
-    float v[8];
-    if (a.swiglu) {
-      if (c0 >= out) continue;
+    for (int i = 0; i < MT; ++i) {
+      float v[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         const int j = q / 4 * 2;
         v[q] = silu(acc[i][j][q & 3]) * acc[i][j + 1][q & 3];
       }
-      st16(y + c0, pack8(v));
-    } else {
+      __builtin_amdgcn_raw_buffer_store_b128(pack8(v), ry, (int)(at0 + i * 32 * out), 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (c0 + h * 8 >= out) continue;
+        float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = acc[i][h * 2 + q / 4][q & 3];
-        st16(y + c0 + h * 8, pack8(v));
+        __builtin_amdgcn_raw_buffer_store_b128(pack8(v), ry, (int)((h ? at1 : at0) + i * 32 * out), 0, 0);
       }
-    }
   }
 }
 
@@ -274,57 +424,79 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
 void matmul_mx_tile_kernel(MatmulMxArgs a, int pieces, int group) {
   using Lds = MxTileLds<HEIGHT>;
   __shared__ __attribute__((aligned(1024))) uint8_t s_tile[Lds::kBytes];
-  int* s_end = reinterpret_cast<int*>(s_tile + Lds::kWindowAt);  // row tiles to a window's end
-  int* s_start = s_end + Lds::kWindows;
-  int* s_rows = s_start + Lds::kWindows;
+  struct Entry {
+    int expert, row, rows, piece;
+  };
+  Entry* s_list = reinterpret_cast<Entry*>(s_tile + Lds::kListAt);
   const int lane = threadIdx.x & (kWave - 1);
-  if (threadIdx.x < kWave) {
-    const int first = a.offset ? uniform((int)ld4(a.offset)) : 0;
-    int before = 0;
-    for (int e0 = 0; e0 < a.E; e0 += kWave) {
-      int s = 0, m = (int)a.rows;
-      if (a.offset) window_of(a, e0 + lane < a.E ? e0 + lane : a.E - 1, first, s, m);
-      if (e0 + lane >= a.E) m = 0;
-      const int end = before + scan_add((m + HEIGHT - 1) / HEIGHT);
-      s_end[e0 + lane] = end;                          // E is at most kWindows, whole 64s
-      s_start[e0 + lane] = s;
-      s_rows[e0 + lane] = m;
-      before = __builtin_amdgcn_readlane(end, kWave - 1);
+  // The workgroup's next 64 tiles, one to a lane.  The windows' row tiles to their ends, first
+  // rows and rows lie where the stages will be.
+  auto list_tiles = [&](int first_tile) {
+    int* s_end = reinterpret_cast<int*>(s_tile);
+    int* s_start = s_end + MOE_MAX_EXPERTS;
+    int* s_rows = s_start + MOE_MAX_EXPERTS;
+    __syncthreads();
+    if (threadIdx.x < kWave) {
+      const int first = a.offset ? uniform((int)ld4(a.offset)) : 0;
+      int before = 0;
+      for (int e0 = 0; e0 < a.E; e0 += kWave) {
+        int s = 0, m = (int)a.rows;
+        if (a.offset) window_of(a, e0 + lane < a.E ? e0 + lane : a.E - 1, first, s, m);
+        if (e0 + lane >= a.E) m = 0;
+        const int end = before + scan_add((m + HEIGHT - 1) / HEIGHT);
+        s_end[e0 + lane] = end;                        // E is at most 16 times 64
+        s_start[e0 + lane] = s;
+        s_rows[e0 + lane] = m;
+        before = __builtin_amdgcn_readlane(end, kWave - 1);
+      }
+      const int64_t id = (int64_t)(first_tile + lane) * 256 + (blockIdx.x & 7) * 32 + blockIdx.x / 8;
+      Entry entry = {0, 0, 0, 0};
+      if ((int64_t)before * pieces > id) {
+        int low = 0, high = a.E - 1;                   // the first window that ends behind it
+        while (low < high) {
+          const int mid = (low + high) / 2;
+          if ((int64_t)s_end[mid] * pieces > id) high = mid;
+          else low = mid + 1;
+        }
+        const int64_t start = low ? (int64_t)s_end[low - 1] * pieces : 0;
+        const Tile t = tile_of(low, s_start[low], s_rows[low], (int)(id - start), HEIGHT, pieces,
+                               group);
+        entry = {t.expert, (int)t.row, t.rows, t.piece};
+      }
+      s_list[lane] = entry;
     }
-  }
-  __syncthreads();
+    __syncthreads();
+  };
   auto tile_at = [&](int n) -> Tile {
-    const int id = n * 256 + (blockIdx.x & 7) * 32 + blockIdx.x / 8;
-    for (int e0 = 0; e0 < a.E; e0 += kWave) {
-      const uint64_t hit = __ballot((int64_t)s_end[e0 + lane] * pieces > id);
-      if (!hit) continue;
-      const int e = e0 + __builtin_ctzll(hit);
-      const int before = e ? uniform(s_end[e - 1]) : 0;
-      return tile_of(e, uniform(s_start[e]), uniform(s_rows[e]), id - before * pieces, HEIGHT,
-                     pieces, group);
-    }
-    return {0, 0, 0, 0};
+    const Entry e = s_list[n];
+    return {uniform(e.expert), (int64_t)uniform(e.row), uniform(e.rows), uniform(e.piece)};
   };
 
-  Tile t = tile_at(0);
-  if (t.rows == 0) return;                             // the whole workgroup
   int tid = threadIdx.x;
-  {
-    const MxTileLoads<HEIGHT> first(a, t, tid, s_tile);
-#pragma unroll
-    for (int n = 0; n < Lds::kStages; ++n) first.stage(n * kDepth, n * Lds::kStageBytes, lane);
-  }
-  for (int n = 1;; ++n) {
-    const Tile next = tile_at(n);
-    // what follows from the thread's number is worked out anew for each tile:
-    // kept over the loop it would not fit the registers
-    asm volatile("" : "+v"(tid));
-    if (HEIGHT > 128 && t.rows > 128)
-      multiply_mx_tile<HEIGHT, HEIGHT / 32>(a, t, next, tid, s_tile);
-    else if (t.rows > 64) multiply_mx_tile<HEIGHT, 4>(a, t, next, tid, s_tile);
-    else multiply_mx_tile<HEIGHT, 2>(a, t, next, tid, s_tile);
-    if (next.rows == 0) return;
-    t = next;
+  for (int first_tile = 0;; first_tile += kWave) {
+    list_tiles(first_tile);
+    Tile t = tile_at(0);
+    if (t.rows == 0) return;                           // the whole workgroup
+    begin_tile<HEIGHT>(a, t, tid, s_tile);
+    int stores = 0;
+    for (int n = 1;; ++n) {
+      Tile next = {0, 0, 0, 0};
+      if (n < kWave) next = tile_at(n);
+      // what follows from the thread's number is worked out anew for each tile:
+      // kept over the loop it would not fit the registers
+      asm volatile("" : "+v"(tid));
+      const int mt = HEIGHT > 128 && t.rows > 128 ? HEIGHT / 32 : t.rows > 64 ? 4 : 2;
+      if (HEIGHT > 128 && mt == HEIGHT / 32)
+        multiply_mx_tile<HEIGHT, HEIGHT / 32>(a, t, next, tid, s_tile, stores);
+      else if (mt == 4) multiply_mx_tile<HEIGHT, 4>(a, t, next, tid, s_tile, stores);
+      else multiply_mx_tile<HEIGHT, 2>(a, t, next, tid, s_tile, stores);
+      if (next.rows == 0) {
+        if (n < kWave) return;
+        break;
+      }
+      stores = a.swiglu ? mt : 2 * mt;
+      t = next;
+    }
   }
 }
 
@@ -435,8 +607,13 @@ void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
     if (Lds::kBatch == 1 || !(k0 & kDepth)) load_scales(k0, at);
     const uint32_t w = (uint32_t)k0 + wk * kDepth + chunk * 16 < (uint32_t)a.K ? wo + k0 : kOutside;
     uint8_t* to = s_mem + at + kRowBytes + wave * 2048;
-    load_to_lds(rw0, w, (lds_u8*)to);
-    load_to_lds(rw1, w, (lds_u8*)(to + 1024));
+    if (a.stream_w) {
+      stream_to_lds(rw0, w, (lds_u8*)to);
+      stream_to_lds(rw1, w, (lds_u8*)(to + 1024));
+    } else {
+      load_to_lds(rw0, w, (lds_u8*)to);
+      load_to_lds(rw1, w, (lds_u8*)(to + 1024));
+    }
 #pragma unroll
     for (int g = 0; g < kRowLoads; ++g) {              // eight rows of a 128 of the depth
       const int n = g * 8 + wave, r = n % (ROWS / 8) * 8 + lr;
@@ -449,7 +626,7 @@ void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
   for (int s = 0; s + 1 < STAGES; ++s) load(s * kDepth * WK, s * kStage);
 
   const int row = lane & 15, quarter = lane / 16;
-  const uint32_t place = row * kDepth + ((quarter ^ (row & 7)) * 16);
+  const uint32_t place = place_of(row, quarter);
   const uint32_t mine = row * Lds::kRowScales + quarter * 2;
   f32x4 acc[MT] = {};
   auto multiply = [&](auto row_tiles) {
@@ -473,7 +650,7 @@ void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
         sa[i] = (int)(two_scales(s_mem + ps + (WC + i) * 16 * Lds::kRowScales) & mask);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t p = at + (place ^ (h * 64));
+        const uint32_t p = at + (place ^ (h * 32));
         wv[h] = *(const i32x4*)(s_mem + kRowBytes + wave * 2048 + p);
 #pragma unroll
         for (int i = 0; i < M; ++i)
@@ -534,8 +711,13 @@ hipError_t launch_stream(const MatmulMxArgs& a, hipStream_t stream) {
   static_assert(w.rows == ROWS && w.channels == 16 * WC && w.depth == kDepth * WK,
                 "the rule's tile");
   const int64_t groups = (tiles_of(a, w) + 255) / 256 * 256;
+  // Weights that one tile of a window reads and that the caches would not keep: 512 rows, 32
+  // experts, 7168 x 4096 89 -> 83 us; windows of several tiles read them again (4662 rows over 96
+  // experts 50 -> 63).
+  MatmulMxArgs m = a;
+  m.stream_w = a.rows <= 32 * (int64_t)a.E && (int64_t)a.E * a.N * a.K >= (int64_t)128 << 20;
   hipLaunchKernelGGL((matmul_mx_stream_kernel<ROWS, WC, WK, STAGES>), dim3((unsigned)groups),
-                     dim3(kTileThreads), 0, stream, a, pieces_of(a, w));
+                     dim3(kTileThreads), 0, stream, m, pieces_of(a, w));
   return hipGetLastError();
 }
 

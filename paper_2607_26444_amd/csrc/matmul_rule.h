@@ -132,12 +132,13 @@ constexpr Way kMxWay[kWays] = {
     {16, 32, 512, 512, 3.0, 0.65, 0.80, 4.5e6},        // <16, 2, 4, 3>
     {16, 16, 1024, 512, 3.0, 0.80, 1.00, 4.5e6},       // <16, 1, 8, 2>
 };
-// Windows that tiles of 128 rows have room for beside three stages and their scales.
-constexpr int kMxTile128Experts = 512;
+// Widest output whose tile of 256 rows a store reaches with a 32-bit offset.
+constexpr int kMxTileChannels = 1 << 21;
 
 inline int choose_mx_way(const MatmulShape& a) {
   return quickest_way(a, kMxWay, [&](int n) {
-    return way_fits(a, n) && (n != kTile128 || a.E <= kMxTile128Experts);
+    const bool tile = n == kTile256 || n == kTile128;
+    return way_fits(a, n) && (!tile || out_channels(a) <= kMxTileChannels);
   });
 }
 
