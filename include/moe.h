@@ -758,7 +758,8 @@ int moe_expert_matmul(const int8_t* a, const float* a_scales, int a_scale_pitch,
  * H/32 scale bytes, whose rows are whole words: packed ones lie (H/32 + 3) / 4 * 4 bytes apart.
  */
 #define MOE_MX_BLOCK 32
-#define MOE_MAX_MX_PITCH 1048576 /* widest pitch of the rows of moe_expert_matmul_mx */
+#define MOE_MAX_MX_PITCH 1048576     /* widest pitch of the rows of moe_expert_matmul_mx */
+#define MOE_MAX_MX_CHANNELS 2097152  /* most channels N of its weights */
 
 /*
  * moe_quantize_mx -- bf16 rows as microscaled 4-bit floats: rows for moe_expert_matmul_mx,
@@ -802,8 +803,8 @@ int moe_quantize_mx(const uint16_t* x, int64_t x_pitch, int64_t rows, int H,
  * w_scales  [E,N,K/32], packed (rows of whole words).
  * expert_offset, expert_count, act, y: as for moe_expert_matmul.
  * Errors: MOE_EALIGN for K % 32, N % 8 (SWIGLU: N % 16), misaligned pointers or pitches;
- * MOE_EINVAL for K > MOE_MAX_DEPTH, a pitch below a row's bytes or above
- * MOE_MAX_MX_PITCH, rows > INT32_MAX, E > MOE_MAX_EXPERTS.
+ * MOE_EINVAL for K > MOE_MAX_DEPTH, N > MOE_MAX_MX_CHANNELS, a pitch below a row's bytes
+ * or above MOE_MAX_MX_PITCH, rows > INT32_MAX, E > MOE_MAX_EXPERTS.
  */
 int moe_expert_matmul_mx(const uint8_t* a, int a_pitch, const uint8_t* a_scales, int a_scale_pitch,
                          int64_t rows, const uint8_t* w, const uint8_t* w_scales, int E, int N,

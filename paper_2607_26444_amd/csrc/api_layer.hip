@@ -366,8 +366,8 @@ int moe_expert_matmul_mx(const uint8_t* a, int a_pitch, const uint8_t* a_scales,
                          int64_t rows, const uint8_t* w, const uint8_t* w_scales, int E, int N,
                          int K, const int32_t* expert_offset, const int32_t* expert_count, int act,
                          uint16_t* y, void* stream) {
-  if (rows < 0 || rows > INT32_MAX || E < 1 || E > MOE_MAX_EXPERTS || N < 1 || K < 1 ||
-      K > MOE_MAX_DEPTH)
+  if (rows < 0 || rows > INT32_MAX || E < 1 || E > MOE_MAX_EXPERTS || N < 1 ||
+      N > MOE_MAX_MX_CHANNELS || K < 1 || K > MOE_MAX_DEPTH)
     return MOE_EINVAL;
   if (act != MOE_ACT_NONE && act != MOE_ACT_SWIGLU) return MOE_EINVAL;
   if ((!expert_offset && (E != 1 || expert_count)) || !w || !w_scales) return MOE_EINVAL;

@@ -101,14 +101,12 @@ inline double way_time(const MatmulShape& a, const Way& w) {
   return __builtin_sqrt(work * work + read * read);
 }
 
-// The way of a table that takes least of those that `fits` says can be launched; kWays if none
-// can be.
-template <typename Fits>
-inline int quickest_way(const MatmulShape& a, const Way* ways, Fits&& fits) {
+// The way of a table that takes least of those that can be launched; kWays if none can be.
+inline int quickest_way(const MatmulShape& a, const Way* ways) {
   int best = kWays;
   double least = 0.0;
   for (int n = 0; n < kWays; ++n) {
-    if (!fits(n)) continue;
+    if (!way_fits(a, n)) continue;
     const double t = way_time(a, ways[n]);
     if (best == kWays || t < least) {
       least = t;
@@ -117,29 +115,44 @@ inline int quickest_way(const MatmulShape& a, const Way* ways, Fits&& fits) {
   }
   return best;
 }
-inline int choose_way(const MatmulShape& a) {
-  return quickest_way(a, kWay, [&](int n) { return way_fits(a, n); });
-}
+inline int choose_way(const MatmulShape& a) { return quickest_way(a, kWay); }
 
-// The same for the products on 4-bit floats, depths in bytes of codes.
+// The same for the products on 4-bit floats, depths in bytes of codes.  The rates are those that
+// fit beside the rounds' times, not the memory's: most of the reading hides.  Measured / model, us,
+// rows drawn to the experts evenly:
+//   rows, experts, K x N               256      128      64 x 128  64 x 64 three, two stages
+//   512, 32, 7168 x 4096, swiglu     100/120   89/97     82/85   101/107   93/95
+//   512, 32, 2048 x 7168              63/88    59/65     49/54    72/84    56/62
+//   2048, 32, 7168 x 4096, swiglu    110/120   98/97    133/121  182/156  152/136
+//   4096, 32, the same               134/120  155/129   205/196  286/256  231/220
+//   8192, 32, the same               227/175  212/201   340/349  507/459  382/393
+//   8192, 32, 2048 x 7168            143/130  130/138   194/212  346/373  239/271
+//   16384, 32, the same              199/198  222/242   355/396  647/704  454/508
+//   13483, 3, 5952 x 4752, swiglu    237/237  265/270   523/534  727/713  601/606
+//   32768, 16, 7168 x 4096, swiglu   499/504  596/649  1136/1268 1878/1652 1350/1412
+//   2048, 1, 4096 x 4096              40/36    28/24     46/47    68/69    48/55
+//   4662, 96, 2080 x 1416             61/68    55/49     50/42    74/60    54/49
+//   512, 1, 4096 x 4096               37/36    26/24     16/14    20/17    15/14
+//   24000, 64, 1024 x 512             21/15    22/20     27/31    53/59    34/40
+// and of few rows                   64 x 128  64 x 64  64 x 32  16 x 32  16 x 16
+//   8, 32, 7168 x 4096, swiglu        22/24    24/27    33/36    22/23    32/33
+//   256, 1, 4096 x 4096               15/14   11.2/9.6  14/13    21/27    29/40
+//   64, 1, 7168 x 4096, swiglu        21/23    14/14    11/10    11/9.6   14/13
+//   64, 8, 2048 x 1024               7.3/8.7  5.8/6.4  5.6/5.5  4.5/4.4  4.7/4.4
+//   1, 1, 7168 x 4096                 16/23    10/14   8.2/10   7.5/7.7  5.9/5.9
+// The way chosen is the best of each line or within 3% of it, but for 8192 rows over 32
+// experts (227 for 212, 143 for 130).
 constexpr Way kMxWay[kWays] = {
-    {256, 256, 128, 256, 9.0, 1.60, 1.60, 4.85e6},     // matmul_mx_tile_kernel<256>
-    {128, 256, 128, 256, 6.0, 1.05, 1.05, 4.85e6},     // matmul_mx_tile_kernel<128>
-    {64, 128, 128, 512, 3.0, 0.72, 1.15, 5.9e6},       // matmul_mx_stream_kernel<64, 8, 1, 3>
-    {64, 64, 256, 256, 3.0, 0.65, 0.65, 4.5e6},        // <64, 4, 2, 3>
-    {64, 64, 256, 512, 3.0, 0.95, 1.00, 4.5e6},        // <64, 4, 2, 2>
-    {64, 32, 512, 256, 3.0, 0.68, 0.68, 4.5e6},        // <64, 2, 4, 3>
-    {16, 32, 512, 512, 3.0, 0.65, 0.80, 4.5e6},        // <16, 2, 4, 3>
-    {16, 16, 1024, 512, 3.0, 0.80, 1.00, 4.5e6},       // <16, 1, 8, 2>
+    {256, 256, 128, 256, 8.2, 1.73, 1.73, 11.5e6},     // matmul_mx_tile_kernel<256>
+    {128, 256, 128, 256, 5.7, 1.17, 1.17, 8.0e6},      // matmul_mx_tile_kernel<128>
+    {64, 128, 128, 512, 3.1, 0.70, 1.27, 13.5e6},      // matmul_mx_stream_kernel<64, 8, 1, 3>
+    {64, 64, 256, 256, 3.2, 0.80, 0.68, 14.0e6},       // <64, 4, 2, 3>
+    {64, 64, 256, 512, 3.2, 0.95, 1.32, 12.5e6},       // <64, 4, 2, 2>
+    {64, 32, 512, 256, 3.5, 0.92, 0.70, 10.0e6},       // <64, 2, 4, 3>
+    {16, 32, 512, 512, 2.9, 0.66, 0.94, 9.2e6},        // <16, 2, 4, 3>
+    {16, 16, 1024, 512, 3.4, 0.48, 0.77, 6.0e6},       // <16, 1, 8, 2>
 };
-// Widest output whose tile of 256 rows a store reaches with a 32-bit offset.
-constexpr int kMxTileChannels = 1 << 21;
-
-inline int choose_mx_way(const MatmulShape& a) {
-  return quickest_way(a, kMxWay, [&](int n) {
-    const bool tile = n == kTile256 || n == kTile128;
-    return way_fits(a, n) && (!tile || out_channels(a) <= kMxTileChannels);
-  });
-}
+static_assert(kTile * 2ll * MOE_MAX_MX_CHANNELS < 1ll << 31, "a tile's stores have 31-bit offsets");
+inline int choose_mx_way(const MatmulShape& a) { return quickest_way(a, kMxWay); }
 
 }  // namespace moe

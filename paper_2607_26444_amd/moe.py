@@ -56,6 +56,7 @@ MOE_MAX_ROW = 16384
 MOE_MAX_DEPTH = 131056
 MOE_MX_BLOCK = 32
 MOE_MAX_MX_PITCH = 1048576
+MOE_MAX_MX_CHANNELS = 2097152
 
 # Entry points declared in include/moe.h.
 EXPORTS = ("moe_version", "moe_strerror", "moe_last_hip_error", "moe_wall_clock_khz",

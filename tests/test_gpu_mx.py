@@ -13,6 +13,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import layer_ref  # noqa: E402
+import mx_rule  # noqa: E402
 import mx_ref as ref  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -294,6 +295,49 @@ def test_many_tiles(counts, N, K, swiglu):
     _check(y, a, w, windows, swiglu)
     if E > 1:
         assert torch.equal(_run(a, w, offset, None, swiglu), y)
+
+
+@pytest.mark.parametrize("case", mx_rule.CASES, ids=lambda c: f"{c[0]}-{len(c[1])}-{c[3]}-{c[4]}")
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_every_way(case, swiglu):
+    """Each kernel and size of tile on packed or fixed windows."""
+    _, counts, cap, _, _ = case
+    rows, E, N, K, _, _ = mx_rule.call_of(case, swiglu)
+    if cap:
+        offset, windows = [777 + e * cap for e in range(E + 1)], \
+            [(e * cap, n) for e, n in enumerate(counts)]
+    else:
+        offset, windows = _packed(counts)
+    a, w = _inputs(rows, E, N, K, seed=rows + N, lo=124 if swiglu else 126, hi=126 if swiglu else 128)
+    y = _run(a, w, offset, counts, swiglu)
+    _check(y, a, w, windows, swiglu, exact=K <= 4608)
+    if not cap and E > 1:
+        assert torch.equal(_run(a, w, offset, None, swiglu), y)
+
+
+@pytest.mark.parametrize("way,rows,E,N,K", mx_rule.PAST_32_BITS)
+def test_every_kernel_past_32_bits(way, rows, E, N, K):
+    """Weights, rows, outputs or scales whose byte offsets pass 2^32: the last rows, and channels
+    of the last expert.  Codes and scales of a row lie in one, as dispatch carries them."""
+    moe = _moe()
+    n = min(rows, max(3, rows // E))
+    start, half, cols = rows - n, K // 2, ref.scale_cols(K)
+    pitch = -(-(half + cols) // 16) * 16
+    (aq, asc), (wq, wsc) = _inputs(n, 1, 8, K, seed=rows)
+    a = torch.zeros(rows, pitch, dtype=torch.uint8, device="cuda")
+    w = torch.zeros(E, N, half, dtype=torch.uint8, device="cuda")
+    ws = torch.full((E, N, cols), 127, dtype=torch.uint8, device="cuda")
+    a[start:, :half], a[start:, half:half + cols] = aq.cuda(), asc.cuda()
+    w[-1, -8:], ws[-1, -8:] = wq[0].cuda(), wsc[0].cuda()
+    offset = torch.full((E + 1,), start, dtype=torch.int32, device="cuda")
+    offset[0], offset[E] = 0, rows
+    count = torch.zeros(E, dtype=torch.int32, device="cuda")
+    count[-1] = n
+    y = torch.zeros(rows, N, dtype=torch.bfloat16, device="cuda")
+    moe.moe_expert_matmul_mx(a, a[:, half:], rows, w, ws, E, N, K, offset, count, moe.MOE_ACT_NONE,
+                             y, a_pitch=pitch, a_scale_pitch=pitch)
+    _check(y[start:, -8:].cpu(), (aq, asc), (wq, wsc), [(0, n)], False, exact=K <= 4608)
+    assert not torch.any(y[:start]) and not torch.any(y[start:, :-8])
 
 
 @pytest.mark.parametrize("rows,K", [(7, 160), (300, 1056)])

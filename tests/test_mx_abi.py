@@ -80,6 +80,7 @@ def test_expert_matmul_mx_refusals():
     base._refuses("moe_expert_matmul_mx", good, [
         (dict(a=None), E), (dict(sa=None), E), (dict(w=None), E), (dict(sw=None), E), (dict(y=None), E),
         (dict(rows=-1), E), (dict(rows=2 ** 31), E), (dict(E=0), E), (dict(E=1025), E), (dict(N=0), E),
+        (dict(N=moe.MOE_MAX_MX_CHANNELS + 16), E),
         (dict(K=0), E), (dict(K=131072), E), (dict(act=2), E), (dict(off=None), E),
         (dict(off=None, E=1), E),                                # counts without offsets
         (dict(ap=128), E), (dict(ap=-16), E), (dict(sp=8), E), (dict(sp=-4), E),
