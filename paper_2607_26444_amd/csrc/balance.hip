@@ -8,12 +8,13 @@
 // follows from the sizes alone, slots in whole numbers.
 //
 // A sequence is cut into parts, a workgroup each: a lane keeps the sums of its experts
-// over the part's tokens, the slots are counted in LDS.  A second launch adds the parts, 32
-// experts to a workgroup; the last workgroup of a sequence adds the loss.  Sequences of
-// one part need no second launch.
+// over the part's tokens, the slots are counted in LDS.  A second launch adds the parts: one
+// workgroup a sequence, or where there is more to add 32 experts to a workgroup, the last of
+// which adds the loss.  Sequences of one part need no second launch.
 //
-// The logits are read once, but a token's chain of loads, exponentials and sums over lanes
-// takes longer than that: 32768 x 256 float32 in 8 sequences 16.0 us (2.2 TB/s), the
+// The logits are read once, but exponentials, reciprocals and sums over lanes take longer than
+// that, not the waiting for loads (two rounds of tokens asked for ahead instead of one, 32768 x
+// 256: 17.7 for 15.5 us): 32768 x 256 float32 in 8 sequences 14.3 us (2.4 TB/s), the
 // gradient of 32768 x 128 bf16 with another added 10.4 (2.4 TB/s), of 32768 x 256 float32
 // 16.2 (4.1 TB/s).  Small batches are bound by the launches: 128 x 16 5.0 us.
 
@@ -289,6 +290,87 @@ __global__ __launch_bounds__(kBlock) void balance_join_kernel(BalanceArgs a, int
   a.loss[seq] = total > 0.0f ? dot * ((float)a.E / total) : 0.0f;
 }
 
+// The same by one workgroup a sequence, for few sums: nothing to wait for between workgroups.
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void balance_join_one_kernel(BalanceArgs a) {
+  __shared__ __attribute__((aligned(16))) float s_sum[kJoinThreads * 4];
+  __shared__ __attribute__((aligned(16))) int s_count[kJoinThreads * 4];
+  __shared__ float s_word[kJoinThreads / kWave], s_dot[kJoinThreads / kWave];
+  __shared__ int s_live;
+  const int64_t seq = blockIdx.x;
+  const int pitch = part_pitch(a.E), quads = pitch / 4, rows = kJoinThreads / quads;
+  const int row = threadIdx.x / quads, quad = threadIdx.x - row * quads;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const float* from = a.partial + seq * a.parts * 2 * pitch + quad * 4;
+  float sum[4] = {};
+  int count[4] = {};
+  int live = 0;
+  if (wave == 0) {
+    for (int p = lane; p < a.parts; p += kWave) live += a.part_live[seq * a.parts + p];
+  }
+  for (int p0 = row; p0 < a.parts; p0 += 2 * rows) {
+    u32x4 v[2] = {}, c[2] = {};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t p = p0 + i * rows;
+      if (row < rows && p < a.parts) {
+        v[i] = ld16(from + p * 2 * pitch);
+        c[i] = ld16(from + p * 2 * pitch + pitch);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sum[j] += __uint_as_float(v[i][j]);
+        count[j] += (int)c[i][j];
+      }
+  }
+  if (row < rows) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      s_sum[threadIdx.x * 4 + j] = sum[j];
+      s_count[threadIdx.x * 4 + j] = count[j];
+    }
+  }
+  if (wave == 0) {
+    live = (int)reduce<64>((uint32_t)live, [](uint32_t x, uint32_t y) { return x + y; });
+    if (lane == 0) s_live = live;
+  }
+  __syncthreads();
+  live = s_live;
+  float total = 0.0f, dot = 0.0f;
+  const int e = threadIdx.x;
+  if (e < a.E) {
+    float t = 0.0f;
+    int m = 0;
+    for (int r = 0; r < rows; ++r) {
+      t += s_sum[r * pitch + e];
+      m += s_count[r * pitch + e];
+    }
+    t /= (float)(live > 0 ? live : 1);
+    a.expert_count[seq * a.E + e] = m;
+    if (a.mean_score) a.mean_score[seq * a.E + e] = t;
+    total = (float)m;
+    dot = total * t;
+  }
+  total = reduce_sum<64>(total);
+  dot = reduce_sum<64>(dot);
+  if (lane == 0) {
+    s_word[wave] = total;
+    s_dot[wave] = dot;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  a.live_tokens[seq] = live;
+  if (!a.loss) return;
+  for (int w = 1; w < (a.E + 63) / 64; ++w) {
+    total += s_word[w];
+    dot += s_dot[w];
+  }
+  a.loss[seq] = total > 0.0f ? dot * ((float)a.E / total) : 0.0f;
+}
+
 template <int LANES, int VPL, bool F32, bool SIGMOID>
 __global__ __launch_bounds__(kBlock) void balance_backward_kernel(BalanceGradArgs a, int vec) {
   constexpr int kTokens = kWave / LANES, kStep = kWavesPerBlock * kTokens;
@@ -445,6 +527,14 @@ hipError_t launch_balance(const BalanceArgs& a, const BalanceShape& shape, hipSt
     return hipGetLastError();
   });
   if (err != hipSuccess || a.parts == 1) return err;
+  // Up to 8192 sums a sequence one workgroup joins them sooner (us by one and by several: 16
+  // sequences of 16 parts of 256 experts 13.2 and 16.6, 8 of 32 14.3 and 16.0, one of 128 parts of
+  // 64 9.2 and 9.1, of 256 parts of 64 11.0 and 10.3).
+  if (a.parts * part_pitch(a.E) <= 8192) {
+    hipLaunchKernelGGL(balance_join_one_kernel, dim3((unsigned)a.seqs), dim3(kJoinThreads), 0,
+                       stream, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(balance_join_kernel, dim3((unsigned)(a.seqs * shape.blocks)), dim3(kBlock), 0,
                      stream, a, shape.blocks);
   return hipGetLastError();

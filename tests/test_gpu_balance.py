@@ -99,7 +99,8 @@ def _check_backward(got, x, count, live, mask, sigmoid, grad_loss, grad_sum=None
 CASES = [(1, 1, 1, 0), (1, 4, 2, 0), (5, 3, 2, 0), (64, 16, 2, 0), (65, 17, 3, 0), (128, 32, 4, 0),
          (300, 60, 6, 0), (1000, 64, 8, 0), (777, 60, 6, 111), (96, 96, 6, 32), (513, 128, 8, 0),
          (640, 160, 8, 64), (2000, 256, 8, 0), (2048, 256, 8, 256), (300, 257, 4, 0), (700, 384, 8, 350),
-         (130, 512, 8, 0), (90, 1000, 32, 45), (40, 1024, 8, 0), (12, 8, 8, 1), (5000, 8, 2, 0)]
+         (130, 512, 8, 0), (90, 1000, 32, 45), (40, 1024, 8, 0), (12, 8, 8, 1), (5000, 8, 2, 0),
+         (280, 890, 8, 140), (390, 1000, 8, 130), (9000, 60, 4, 0), (4200, 200, 8, 2100)]
 
 
 @pytest.mark.parametrize("T,E,k,seq", CASES)
