@@ -49,7 +49,7 @@ __device__ __forceinline__ void window_of(const MatmulShape& a, int e, int first
 // neighbouring tiles share rows or weights.
 __device__ __forceinline__ Tile tile_of(int expert, int start, int n, int at, int size, int pieces,
                                         int group) {
-  const int tiles = (n + size - 1) / size;
+  const int tiles = n / size + (n % size > 0);
   if (at >= tiles * pieces) return {0, 0, 0, 0};
   if (group > 1) {                                     // groups as even as they can be
     const int groups = (tiles + group - 1) / group;

@@ -79,8 +79,10 @@ class MoeLayer:
             return torch.empty(*shape, dtype=dtype, device=device)
         self.sum, self.normed = buf(T, H), buf(T, H)
         if self.mx:
-            # a row's scales behind its codes, so that dispatch carries both as one row
-            self.row_bytes = -(-(H // 2 + cols) // 16) * 16
+            # a row's scales behind its codes, so that dispatch carries both as one row; whole
+            # lines of 128 bytes where they are an eighth more at most
+            used, line = H // 2 + cols, -(-(H // 2 + cols) // 128) * 128
+            self.row_bytes = line if 8 * line <= 9 * used else -(-used // 16) * 16
             self.q = buf(T, self.row_bytes, dtype=torch.uint8)
             self.rows = buf(rows, self.row_bytes, dtype=torch.uint8)
             self.q_scale, self.row_scale = self.q[:, H // 2:], self.rows[:, H // 2:]
