@@ -798,6 +798,7 @@ int moe_quantize_mx(const uint16_t* x, int64_t x_pitch, int64_t rows, int H,
  * a         [rows,K/2] codes, rows a_pitch BYTES apart (0 = packed), 16-byte aligned rows.
  * a_scales  [rows,K/32], rows a_scale_pitch BYTES apart (0 = packed), 4-byte aligned rows.
  *           What fills the last word of a row takes no part.
+ *           Rows of codes that begin with a line of 128 bytes are read soonest.
  * w         [E,N,K/2] codes, packed, 16-byte aligned: channel by channel, the depth
  *           innermost, as moe_quantize_mx leaves E*N rows of K values.
  * w_scales  [E,N,K/32], packed (rows of whole words).
