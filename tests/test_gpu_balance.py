@@ -266,6 +266,55 @@ def test_many_tokens(T, seq):
     assert torch.all((grad - want).abs() <= REL * size)
 
 
+@pytest.mark.parametrize("T,E,seq", [(2000, 250, 0), (9000, 60, 0), (1400, 384, 700)])
+def test_graphs_that_share_a_workspace(T, E, seq):
+    """Sequences of several parts, both ways of joining them: two captured calls on one
+    workspace that held other bytes, replayed in turn with eager work between."""
+    moe = _moe()
+    S = T // seq if seq else 1
+    n = moe.moe_balance_workspace_bytes(T, E, seq)
+    assert n > 0
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+
+    class Call:
+        def __init__(self):
+            self.x = torch.empty(T, E, device="cuda")
+            self.idx = torch.zeros(T, 4, dtype=torch.int32, device="cuda")
+            self.out = [torch.empty(S, E, dtype=torch.int32, device="cuda"),
+                        torch.empty(S, dtype=torch.int32, device="cuda"),
+                        torch.empty(S, E, device="cuda"), torch.empty(S, device="cuda")]
+
+        def fill(self):
+            self.x.normal_()
+            self.idx.copy_(self.x.topk(4).indices)
+
+        def run(self):
+            moe.moe_balance(self.x, moe.MOE_DTYPE_F32, E, self.idx, None, *self.out, ws, seq_len=seq)
+
+    a, b, eager = Call(), Call(), Call()
+    graphs = []
+    for c in (a, b):
+        c.fill()
+        c.run()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            c.run()
+    for _ in range(4):
+        a.fill(), b.fill()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for c in (a, b):
+            eager.x.copy_(c.x), eager.idx.copy_(c.idx)
+            eager.run()
+            torch.cuda.synchronize()
+            for got, want in zip(c.out, eager.out):
+                assert torch.equal(got, want)
+        count, live, mean, loss = (t.cpu() for t in a.out)
+        _check_forward((count, live, mean, loss), a.x.cpu(), a.idx.cpu(), None, False, seq)
+
+
 def test_router_training_step_in_a_graph():
     """Routing, its loss and both gradients as a training step makes them, captured and replayed
     on new logits with eager work between, against 64 bits and the eager step."""

@@ -80,6 +80,12 @@ def test_quantize(rows, H):
     _check_quantized(_quantize(x), x)
 
 
+@pytest.mark.parametrize("H", [16416, 131040])
+def test_quantize_wide_rows(H):
+    x = _rows(3, H, seed=H)
+    _check_quantized(_quantize(x), x)
+
+
 def test_quantize_every_bf16_pattern():
     """Each pattern as the largest of a block, beside the ties of every step, values over a
     border and under it, the smallest ones, both zeros."""
@@ -222,7 +228,8 @@ def test_swiglu(rows, N, K):
     _check(_run(a, w, None, None, True), a, w, [(0, rows)], True)
 
 
-@pytest.mark.parametrize("rows,N,K", [(1, 264, 4128), (40, 72, 2080), (300, 264, 7168)])
+@pytest.mark.parametrize("rows,N,K", [(1, 264, 4128), (40, 72, 2080), (300, 264, 7168), (5, 24, 131040),
+                                      (100, 136, 131040), (700, 264, 65568)])
 @pytest.mark.parametrize("swiglu", [False, True])
 def test_scales_of_any_size(rows, N, K, swiglu):
     N = N // 16 * 16 if swiglu else N
@@ -450,7 +457,8 @@ def _check_layer(layer, x, r, logits, y):
 
 
 @pytest.mark.parametrize("T,H,I,E,k", [(1, 256, 64, 4, 2), (33, 416, 224, 8, 3), (300, 512, 256, 16, 4),
-                                       (700, 1056, 160, 4, 2)])
+                                       (700, 1056, 160, 4, 2), (70, 2048, 96, 8, 2),
+                                       (300, 2080, 128, 4, 2)])
 @pytest.mark.parametrize("score", [0, 1])
 def test_layer(T, H, I, E, k, score):
     from paper_2607_26444_amd.layer import random_layer
