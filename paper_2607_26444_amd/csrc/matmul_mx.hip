@@ -447,7 +447,7 @@ void matmul_mx_tile_kernel(MatmulMxArgs a, int pieces, int group) {
         int s = 0, m = (int)a.rows;
         if (a.offset) window_of(a, e0 + lane < a.E ? e0 + lane : a.E - 1, first, s, m);
         if (e0 + lane >= a.E) m = 0;
-        const int end = before + scan_add((m + HEIGHT - 1) / HEIGHT);
+        const int end = before + scan_add(m / HEIGHT + (m % HEIGHT > 0));
         s_end[e0 + lane] = end;                        // E is at most 16 times 64
         s_start[e0 + lane] = s;
         s_rows[e0 + lane] = m;
@@ -675,18 +675,10 @@ void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
   else multiply(std::integral_constant<int, MT>());
   meet<0>();                                           // loads past the end have landed
 
-  f32x4* s_acc = reinterpret_cast<f32x4*>(s_mem);      // [wavefront][row tile][lane]
-#pragma unroll
-  for (int i = 0; i < MT; ++i) s_acc[(wave * MT + i) * kWave + lane] = acc[i];
-  __syncthreads();
   // tile (w, i): channels of wavefront column w, rows 16 i..; a lane's four
   // sums are channels quarter * 4 .. + 3 of row `row`
-  for (int n = wave; n < WC * mt; n += 8) {
-    const int w = n % WC, i = n / WC;
+  auto store = [&](int w, int i, f32x4 sum) {
     const int r = i * 16 + row;
-    f32x4 sum = s_acc[(w * MT + i) * kWave + lane];
-#pragma unroll
-    for (int g = 1; g < WK; ++g) sum += s_acc[((g * WC + w) * MT + i) * kWave + lane];
     const int lc = w * step + (quarter * 4) % step, c = t.piece * WC * step + lc;
     const bool in = r < t.rows && c < out;
     float v[4];
@@ -697,6 +689,23 @@ void matmul_mx_stream_kernel(MatmulMxArgs a, int pieces) {
     }
     if (in && !(a.swiglu && quarter > 1))
       st4x2(a.y + (t.row + r) * out + c, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  };
+  if constexpr (WK == 1) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+      if (i < mt) store(wc, i, acc[i]);
+  } else {
+    f32x4* s_acc = reinterpret_cast<f32x4*>(s_mem);    // [wavefront][row tile][lane]
+#pragma unroll
+    for (int i = 0; i < MT; ++i) s_acc[(wave * MT + i) * kWave + lane] = acc[i];
+    __syncthreads();
+    for (int n = wave; n < WC * mt; n += 8) {
+      const int w = n % WC, i = n / WC;
+      f32x4 sum = s_acc[(w * MT + i) * kWave + lane];
+#pragma unroll
+      for (int g = 1; g < WK; ++g) sum += s_acc[((g * WC + w) * MT + i) * kWave + lane];
+      store(w, i, sum);
+    }
   }
 }
 

@@ -347,6 +347,28 @@ def test_every_kernel_past_32_bits(way, rows, E, N, K):
     assert not torch.any(y[:start]) and not torch.any(y[start:, :-8])
 
 
+def test_as_many_rows_as_there_can_be():
+    """Row tiles whose count and last row come near 2^31; the rows' ends and some between."""
+    moe = _moe()
+    rows, N, K = 2 ** 31 - 1, 8, 32
+    if torch.cuda.mem_get_info()[0] < 100e9:
+        pytest.skip("not enough memory free")
+    (aq, asc), (wq, wsc) = _inputs(300, 1, N, K, seed=11)
+    a = torch.zeros(rows, K // 2, dtype=torch.uint8, device="cuda")
+    s = torch.full((rows, 4), 127, dtype=torch.uint8, device="cuda")
+    y = torch.full((rows, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    starts = (0, 2 ** 30 - 100, rows - 300)
+    for at in starts:
+        a[at:at + 300], s[at:at + 300] = aq.cuda(), asc.cuda()
+    moe.moe_expert_matmul_mx(a, s, rows, wq.cuda(), wsc.cuda(), 1, N, K, None, None, moe.MOE_ACT_NONE, y)
+    for at in starts:
+        _check(y[at:at + 300].cpu(), (aq, asc), (wq, wsc), [(0, 300)], False)
+    between = [(300, 2 ** 30 - 100), (2 ** 30 + 200, rows - 300)]
+    for start, end in between:
+        for i in range(start, end, 1 << 26):
+            assert not torch.any(y[i:min(end, i + (1 << 26))])
+
+
 @pytest.mark.parametrize("rows,K", [(7, 160), (300, 1056)])
 def test_row_pitches(rows, K):
     """Codes and scales in one row, as they come from dispatch."""
