@@ -60,7 +60,7 @@ __device__ __forceinline__ uint32_t depth_mask(int k, int quarter, int K) {
   return (at < K ? 0x00FF00FFu : 0u) | (at + 16 < K ? 0xFF00FF00u : 0u);
 }
 
-// The same for weights that are read once.
+// load_to_lds past the caches, for weights that are read once.
 __device__ __forceinline__ void stream_to_lds(Rsrc r, uint32_t offset, lds_u8* to) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, (int)offset, 0, 0, kLoadNonTemporal);
 }
