@@ -87,8 +87,8 @@ __device__ __forceinline__ void each(F&& f) {
 // Bound by what the compute units' loads take from the L2 cache: 32768 rows, 16 experts, 7168 x
 // 4096 with swiglu 490 us (3.9 PFLOP/s), with the loads left out 370, without those of the
 // scales alone 445; with all codes 0 442, the rest is the clock that the power leaves.  Shallow
-// products also by their stores, which the next tile's loads wait behind (32 experts, 2048 x 7168
-// 356 us, without stores 274).  On the way there: scales word by word and stage by stage 527; 16
+// products also by their stores, which take the same path (32 experts, 2048 x 7168 356 us, without
+// stores 274; not waiting for them in the next tile's first stage changes nothing).  On the way there: scales word by word and stage by stage 527; 16
 // bytes every second stage 495; stages of half the depth, four of them, 510; four wavefronts with
 // 128 x 128 each 523; lines asked for earlier, to have them in the L2 cache, +4 to 8%; the windows'
 // short last tiles behind all others +1 to 15%; outputs in whole 64 bytes to a store, stores past
