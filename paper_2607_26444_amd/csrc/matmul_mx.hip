@@ -84,15 +84,18 @@ __device__ __forceinline__ void each(F&& f) {
 // row from there and puts them, by quarter and tile, where a lane finds its words of four tiles
 // in one read.
 //
-// Bound by what the compute units' loads take from the L2 cache: 32768 rows, 16 experts, 7168 x
-// 4096 with swiglu 490 us (3.9 PFLOP/s), with the loads left out 370, without those of the
-// scales alone 445; with all codes 0 442, the rest is the clock that the power leaves.  Shallow
-// products also by their stores, which take the same path (32 experts, 2048 x 7168 356 us, without
-// stores 274; not waiting for them in the next tile's first stage changes nothing).  On the way there: scales word by word and stage by stage 527; 16
-// bytes every second stage 495; stages of half the depth, four of them, 510; four wavefronts with
-// 128 x 128 each 523; lines asked for earlier, to have them in the L2 cache, +4 to 8%; the windows'
-// short last tiles behind all others +1 to 15%; outputs in whole 64 bytes to a store, stores past
-// the caches, workgroups that start at four different times, wavefronts of raised priority 0 to +2%.
+// 32768 rows, 16 experts, 7168 x 4096 with swiglu 477 us (4.0 PFLOP/s), and no unit is full: the
+// matrix units are busy half of the cycles, at 2.05 GHz (with all codes 0 7% less time), reads of
+// LDS take a quarter, and the loads would come in a third of a stage (a loop of them reaches 110
+// to 130 bytes a ns and compute unit, 70 from rows that lie across lines).  Two wavefronts a SIMD
+// that meet once a stage do not cover each other's waits: with the loads left out 370, without
+// those of the scales alone 445.  Shallow products also have their stores (32 experts, 2048 x 7168
+// 351 us, without stores 274; not waiting for them in the next tile's first stage changes nothing).
+// On the way there: scales word by word and stage by stage 527; 16 bytes every second stage 495;
+// stages of half the depth, four of them, 510; four wavefronts with 128 x 128 each 523; lines asked
+// for earlier, to have them in the L2 cache, +4 to 8%; the windows' short last tiles behind all
+// others +1 to 15%; outputs in whole 64 bytes to a store, stores past the caches, workgroups that
+// start at four different times, wavefronts of raised priority 0 to +2%.
 
 // Scales of a row and pair of stages.
 constexpr int kPairScales = 2 * kStageScales;
@@ -106,6 +109,9 @@ struct MxTileLds {
   static constexpr int kStageBytes = kRowBytes + kTile * kDepth;
   static constexpr int kScaleAt = kStages * kStageBytes;
   static constexpr bool kFourStages = HEIGHT == 256;   // scales come for four stages, else for two
+  // Loads of a full tile's stage that are asked for during the first units of the stage before it,
+  // and not as soon as their place is free: 0 486 us, 4 482, 6 477, 8 484 at the size above.
+  static constexpr int kLate = HEIGHT == 256 ? 6 : 0;
   static constexpr int kRawAt = kScaleAt + kTileThreads * kPairScales;
   static constexpr int kListAt = kRawAt + (kFourStages ? kTileThreads * 2 * kPairScales : 0);
   static constexpr int kBytes = kListAt + kWave * 16;
@@ -248,11 +254,14 @@ __device__ __forceinline__ void begin_tile(const MatmulMxArgs& a, const Tile& t,
                                            uint8_t* s_tile) {
   using Lds = MxTileLds<HEIGHT>;
   const MxTileLoads<HEIGHT> loads(a, t, tid, s_tile);
+  constexpr int kLoads = HEIGHT / 64 + 4;
+  const int second = t.rows > HEIGHT / 2 ? kLoads - Lds::kLate : kLoads;
 #pragma unroll
   for (int s = 0; s < Lds::kStages; ++s)
 #pragma unroll
-    for (int n = 0; n < HEIGHT / 64 + 4; ++n)
-      loads.template part<HEIGHT / 64>(n, loads.depth_of(s * kDepth), s * Lds::kStageBytes);
+    for (int n = 0; n < kLoads; ++n)
+      if (s != 1 || n < second)
+        loads.template part<HEIGHT / 64>(n, loads.depth_of(s * kDepth), s * Lds::kStageBytes);
   if constexpr (Lds::kFourStages) {
     loads.ask(0, 0, tid & (kWave - 1));
     loads.ask(1, 1, tid & (kWave - 1));
@@ -271,6 +280,7 @@ __device__ __forceinline__ void multiply_mx_tile(const MatmulMxArgs& a, const Ti
   using Lds = MxTileLds<HEIGHT>;
   constexpr int NT = 4;
   constexpr int kLoads = MT / 2 + 4;                   // of a wavefront and stage
+  constexpr int kLate = MT * 32 == HEIGHT ? Lds::kLate : 0, kEarly = kLoads - kLate;
   const int lane = tid & (kWave - 1), wave = uniform(tid / kWave);
   const MxTileLoads<HEIGHT> loads(a, t, tid, s_tile);
 
@@ -329,7 +339,8 @@ __device__ __forceinline__ void multiply_mx_tile(const MatmulMxArgs& a, const Ti
   u32x4 row_scales = {};
   if constexpr (!Lds::kFourStages) row_scales = loads.fetch(1);
   // Stage s is in LDS at s % kStages.  Within a turn the wavefronts meet once: by then each has
-  // asked for the last of stage s, and its loads of stage s + 1 have arrived.  The scales of the
+  // asked for the last of stage s, and its loads of stage s + 1 have arrived; those of stage s + 2
+  // follow then and, of full tiles, in the next turn.  The scales of the
   // next two stages are placed before that in every second turn, and read behind it.
   auto turn = [&](auto parity, int k0) {
     constexpr int p = parity.value;
@@ -341,6 +352,8 @@ __device__ __forceinline__ void multiply_mx_tile(const MatmulMxArgs& a, const Ti
       constexpr int u = unit.value, h = u / MT, i = u % MT, x = u - B;
       if constexpr (u == B) meet<(Lds::kStages - 2) * kLoads>();
       if constexpr (u + D < U) read_a(u + D, buf);
+      if constexpr (u < kLate)
+        loads.template part<MT / 2>(kEarly + u, loads.depth_of(k0 + kDepth), next_buf);
       if constexpr (h == 0) {
 #pragma unroll
         for (int j = i * NT / MT; j < (i + 1) * NT / MT; ++j) read_w(1, j, buf);
@@ -355,7 +368,7 @@ __device__ __forceinline__ void multiply_mx_tile(const MatmulMxArgs& a, const Ti
       }
       if constexpr (u >= B) {
 #pragma unroll
-        for (int n = x * kLoads / kLeft; n < (x + 1) * kLoads / kLeft; ++n)
+        for (int n = x * kEarly / kLeft; n < (x + 1) * kEarly / kLeft; ++n)
           loads.template part<MT / 2>(n, fill, buf);
 #pragma unroll
         for (int j = x * NT / kLeft; j < (x + 1) * NT / kLeft; ++j) read_w(0, j, next_buf);

@@ -125,15 +125,15 @@ inline int choose_way(const MatmulShape& a) { return quickest_way(a, kWay); }
 //   512, 32, 2048 x 7168              63/88    59/65     49/54    72/84    56/62
 //   2048, 32, 7168 x 4096, swiglu    110/120   98/97    133/121  182/156  152/136
 //   4096, 32, the same               134/120  155/129   205/196  286/256  231/220
-//   8192, 32, the same               227/175  212/201   340/349  507/459  382/393
-//   8192, 32, 2048 x 7168            143/130  130/138   194/212  346/373  239/271
-//   16384, 32, the same              199/198  222/242   355/396  647/704  454/508
-//   13483, 3, 5952 x 4752, swiglu    237/237  265/270   523/534  727/713  601/606
-//   32768, 16, 7168 x 4096, swiglu   499/504  596/649  1136/1268 1878/1652 1350/1412
+//   8192, 32, the same               230/175  212/201   340/349  507/459  382/393
+//   8192, 32, 2048 x 7168            137/130  130/138   194/212  346/373  239/271
+//   16384, 32, the same              191/198  222/242   355/396  647/704  454/508
+//   13483, 3, 5952 x 4752, swiglu    225/237  265/270   523/534  727/713  601/606
+//   32768, 16, 7168 x 4096, swiglu   477/504  596/649  1136/1268 1878/1652 1350/1412
 //   2048, 1, 4096 x 4096              40/36    28/24     46/47    68/69    48/55
 //   4662, 96, 2080 x 1416             61/68    55/49     50/42    74/60    54/49
 //   512, 1, 4096 x 4096               37/36    26/24     16/14    20/17    15/14
-//   24000, 64, 1024 x 512             21/15    22/20     27/31    53/59    34/40
+//   24000, 64, 1024 x 512             19/15    22/20     27/31    53/59    34/40
 // and of few rows                   64 x 128  64 x 64  64 x 32  16 x 32  16 x 16
 //   8, 32, 7168 x 4096, swiglu        22/24    24/27    33/36    22/23    32/33
 //   256, 1, 4096 x 4096               15/14   11.2/9.6  14/13    21/27    29/40
@@ -141,7 +141,7 @@ inline int choose_way(const MatmulShape& a) { return quickest_way(a, kWay); }
 //   64, 8, 2048 x 1024               7.3/8.7  5.8/6.4  5.6/5.5  4.5/4.4  4.7/4.4
 //   1, 1, 7168 x 4096                 16/23    10/14   8.2/10   7.5/7.7  5.9/5.9
 // The way chosen is the best of each line or within 3% of it, but for 8192 rows over 32
-// experts (227 for 212, 143 for 130).
+// experts (230 for 212, 137 for 130).
 constexpr Way kMxWay[kWays] = {
     {256, 256, 128, 256, 8.2, 1.73, 1.73, 11.5e6},     // matmul_mx_tile_kernel<256>
     {128, 256, 128, 256, 5.7, 1.17, 1.17, 8.0e6},      // matmul_mx_tile_kernel<128>
