@@ -85,12 +85,13 @@ __device__ __forceinline__ void each(F&& f) {
 // in one read.
 //
 // 32768 rows, 16 experts, 7168 x 4096 with swiglu 477 us (4.0 PFLOP/s), and no unit is full: the
-// matrix units are busy half of the cycles, at 2.05 GHz (with all codes 0 7% less time), reads of
-// LDS take a quarter, and the loads would come in a third of a stage (a loop of them reaches 110
-// to 130 bytes a ns and compute unit, 70 from rows that lie across lines).  Two wavefronts a SIMD
-// that meet once a stage do not cover each other's waits: with the loads left out 370, without
-// those of the scales alone 445.  Shallow products also have their stores (32 experts, 2048 x 7168
-// 351 us, without stores 274; not waiting for them in the next tile's first stage changes nothing).
+// matrix units are busy 44% of the cycles within a layer, at 2.0 GHz (with all codes 0 7% less
+// time), reads of LDS a fifth, and the loads would come in a third of a stage (a loop of them
+// reaches 110 to 130 bytes a ns and compute unit, 70 from rows that lie across lines).  Two
+// wavefronts a SIMD that meet once a stage do not cover each other's waits: with the loads left out
+// 370, without those of the scales alone 445.  Shallow products also have their stores (32 experts,
+// 2048 x 7168 351 us, without stores 274; not waiting for them in the next tile's first stage
+// changes nothing).
 // On the way there: scales word by word and stage by stage 527; 16 bytes every second stage 495;
 // stages of half the depth, four of them, 510; four wavefronts with 128 x 128 each 523; lines asked
 // for earlier, to have them in the L2 cache, +4 to 8%; the windows' short last tiles behind all
