@@ -1,0 +1,85 @@
+"""Shares of logits that lie far apart or far down, against 64 bits.
+
+Logits are multiples of 1/64 below 64 in size, whose differences float32 holds.  In units u of
+2^-24, relative: an exponential 3 (its argument's rounding is made good, the hardware's result 2,
+one rounding), 1 + e and its reciprocal 1 each, so that a softmax's term has 3 and a sigmoid score
+5; with up to 16 terms in a lane and 64 lanes their sum adds 15 + 6, the quotient 2.  So a share is
+off by 3 + 3 + 21 + 2 = 29 or 5 + 5 + 21 + 2 = 33 at most; 40 leaves room for the terms of second
+order.  The mean of sequences of one token is the share itself.  A gradient's terms: a share 33,
+1 - s 9, loads and g / n 4, the sum of f p 33 + 24, four products: 110 of the terms' size.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import mx_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+SHARE, GRAD = 40 * U, 110 * U
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _balance(x, idx, sigmoid, seq):
+    """Slots, live tokens and mean scores, and the gradient of ones."""
+    from paper_2607_26444_amd import moe
+    T, E = x.shape
+    S = T // seq
+    count = torch.empty(S, E, dtype=torch.int32, device="cuda")
+    live = torch.empty(S, dtype=torch.int32, device="cuda")
+    mean, loss = torch.empty(S, E, device="cuda"), torch.empty(S, device="cuda")
+    need = moe.moe_balance_workspace_bytes(T, E, seq)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    dtype = moe.MOE_DTYPE_F32 if x.dtype == torch.float32 else moe.MOE_DTYPE_BF16
+    dx = x.cuda()
+    moe.moe_balance(dx, dtype, E, idx.int().cuda(), None, count, live, mean, loss, ws,
+                    score=int(sigmoid), seq_len=seq)
+    grad = torch.empty_like(dx)
+    moe.moe_balance_backward(dx, dtype, T, E, None, count, live, torch.ones(S, device="cuda"), None,
+                             grad, score=int(sigmoid), seq_len=seq)
+    torch.cuda.synchronize()
+    return count.cpu(), live.cpu(), mean.cpu().double(), loss.cpu().double(), grad.cpu().double()
+
+
+def _logits(T, E, lo, hi, seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    x = torch.randint(64 * lo, 64 * hi + 1, (T, E), generator=g).float() / 64
+    return x, torch.randint(0, E, (T, min(4, E)), generator=g)
+
+
+# down to where a share of float32 has its lowest normal numbers, and where 1 - s has lost s
+@pytest.mark.parametrize("E", [2, 16, 60, 256, 890])
+@pytest.mark.parametrize("sigmoid,lo,hi", [(False, -40, 40), (True, -40, 40), (True, -62, -2),
+                                           (False, -62, 0), (True, 2, 30)])
+def test_shares_of_far_logits(E, sigmoid, lo, hi):
+    T = 150
+    x, idx = _logits(T, E, lo, hi, E)
+    _, _, mean, loss, _ = _balance(x, idx, sigmoid, 1)
+    want = ref.shares(x.double(), None, sigmoid)
+    assert torch.all((mean - want).abs() <= SHARE * want)
+    count, live, _, wl = ref.balance(x.double(), idx, None, sigmoid, 1)
+    assert torch.all((loss - wl).abs() <= (SHARE + 20 * U) * wl)
+
+
+@pytest.mark.parametrize("E", [2, 60, 890])
+@pytest.mark.parametrize("sigmoid,lo,hi", [(False, -40, 40), (True, -40, 40), (True, -62, -2)])
+def test_gradients_of_far_logits(E, sigmoid, lo, hi):
+    T, seq = 120, 4
+    x, idx = _logits(T, E, lo, hi, E + 1)
+    count, live, _, _, grad = _balance(x, idx, sigmoid, seq)
+    # by the formula: automatic differentiation takes 1 - s from s, which loses it near 1
+    rest = torch.sigmoid(-x.double()) if sigmoid else torch.ones(T, E, dtype=torch.float64)
+    p = ref.shares(x.double(), None, sigmoid).view(-1, seq, E)
+    f = (count.double() * E / count.sum(1, keepdim=True))[:, None]
+    dot, part = (f * p).sum(2, keepdim=True), p * rest.view(p.shape) / seq
+    want, size = (part * (f - dot)).view(T, E), (part * (f + dot)).view(T, E)
+    assert torch.all((grad - want).abs() <= GRAD * size + 2.0 ** -126)
