@@ -598,7 +598,7 @@ int moe_balance_workspace_bytes(int64_t T, int E, int64_t seq_len, size_t* out_b
  *      loss = sum_e f_e mean_score[e],  f_e = E expert_count[e] / sum_i expert_count[i]
  * which is 1 for an even load or even scores.  A token without an eligible expert, or whose
  * scores add up to less than float32's smallest normal number, has p = 0 and counts in n;
- * a sequence without live tokens or slots has loss 0.
+ * a sequence without live tokens or slots has loss 0.  A p below 2^-80 may come out as 0.
  *
  * logits, dtype, logits_pitch, score, token_mask: as for moe_route; topk_idx [T,k] as it
  * left it (entries outside [0, E) are no slots).

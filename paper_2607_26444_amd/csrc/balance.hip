@@ -65,23 +65,45 @@ __device__ __forceinline__ float exp_near(float x) {
 }
 
 // Scores in place of the logits, and the factor that makes shares of them: 0 where their sum
-// is none, or lies below float32's normal range (sigmoid scores of very low logits).  They are as
-// near as the routing's (expf and an exactly rounded reciprocal) in fewer instructions: arguments
-// are clamped to where nothing overflows.  A rounded argument and the bare reciprocal instead
-// take 0.4 us (softmax) and 1.2 us (sigmoid) of 32768 x 256 logits, and cost up to 44 units of a
-// share.  REST: also 1 - s.
+// is none, or lies below float32's normal range (sigmoid scores of very low logits).  Sigmoid
+// scores of a token whose logits all lie below -27 are exp(x) to 2^-40 of them; such come divided
+// by the largest, so that they are there also where each is below float32's range.
+// Exponentials and reciprocals are as near as the routing's (expf, exactly rounded) in fewer
+// instructions: their arguments are clamped to where nothing overflows.  A rounded argument and
+// the bare reciprocal would save 0.4 us (softmax) and 1.2 us (sigmoid) of 32768 x 256 logits and
+// cost up to 44 units of a share.  REST: also 1 - s.
 template <int LANES, int VPL, bool SIGMOID, bool REST = false>
 __device__ __forceinline__ float scores(float (&x)[VPL], float (&rest)[REST ? VPL : 1]) {
-  float local = 0.0f;
   if constexpr (SIGMOID) {
+    float v[VPL], local = 0.0f;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
       const float e = exp_near(__builtin_amdgcn_fmed3f(-x[i], -87.0f, 87.0f)), d = 1.0f + e;
       const float r = __builtin_amdgcn_rcpf(d);
-      const float s = x[i] >= -87.0f ? __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r) : 0.0f;
-      if constexpr (REST) rest[i] = e > 1.0f ? 1.0f - s : e * s;   // also where s rounds to 1
-      x[i] = s;
+      v[i] = x[i] >= -87.0f ? __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r) : 0.0f;
+      if constexpr (REST) rest[i] = e > 1.0f ? 1.0f - v[i] : e * v[i];   // also where s rounds to 1
+      local += v[i];
     }
+    float total = reduce_sum<LANES>(local);
+    if (total < 0x1p-40f) {                            // the token's lanes together
+      const float m = row_max<LANES, VPL>(x);
+      if (m > -INFINITY) {
+        local = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+          v[i] = exp_near(__builtin_amdgcn_fmed3f(x[i] - m, -150.0f, 0.0f));
+          if constexpr (REST) rest[i] = 1.0f;
+          local += v[i];
+        }
+        total = reduce_sum<LANES>(local);
+        // the sum of the scores, e^64 times as large, against 2^-126
+        if (exp_near(__builtin_amdgcn_fmed3f(m + 64.0f, -150.0f, 88.0f)) * total < 7.32938e-11f)
+          total = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) x[i] = v[i];
+    return total > 0.0f ? 1.0f / total : 0.0f;
   } else {
     float m = row_max<LANES, VPL>(x);
     if (m == INFINITY) {                               // infinite ones share alike
@@ -92,11 +114,12 @@ __device__ __forceinline__ float scores(float (&x)[VPL], float (&rest)[REST ? VP
     // -inf, NaN and what lies far below the largest come to the lower end, which gives 0
 #pragma unroll
     for (int i = 0; i < VPL; ++i) x[i] = exp_near(__builtin_amdgcn_fmed3f(x[i] - m, -150.0f, 0.0f));
-  }
+    float local = 0.0f;
 #pragma unroll
-  for (int i = 0; i < VPL; ++i) local += x[i];
-  const float total = reduce_sum<LANES>(local);
-  return total >= 0x1p-126f ? 1.0f / total : 0.0f;
+    for (int i = 0; i < VPL; ++i) local += x[i];
+    const float total = reduce_sum<LANES>(local);
+    return total > 0.0f ? 1.0f / total : 0.0f;         // 1 at least
+  }
 }
 
 // Sum over the workgroup's threads, each thread's the same; `s`: a word a wavefront.

@@ -83,3 +83,32 @@ def test_gradients_of_far_logits(E, sigmoid, lo, hi):
     dot, part = (f * p).sum(2, keepdim=True), p * rest.view(p.shape) / seq
     want, size = (part * (f - dot)).view(T, E), (part * (f + dot)).view(T, E)
     assert torch.all((grad - want).abs() <= GRAD * size + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("E", [3, 60, 256, 890])
+@pytest.mark.parametrize("lo,hi", [(-90, -90), (-100, -88), (-91, -86), (-50, -28), (-140, -60)])
+def test_sigmoid_scores_that_are_very_small(E, lo, hi):
+    """Scores below float32's normal range whose sum is not give shares all the same, beside tokens
+    of ordinary logits; only where the sum is below as well there are none."""
+    T, seq = 130, 2
+    x, idx = _logits(T, E, lo, hi, E - lo)
+    x[::5] = _logits(T, E, -4, 4, 1)[0][::5]
+    x[7, E // 2], x[9, 0] = -math.inf, math.nan
+    x[11:14] = -math.inf
+    total = torch.sigmoid(x.double()).masked_fill(~(x > -math.inf), 0.0).sum(1)
+    least = 2.0 ** -126
+    clear = ((total - least).abs() > 1e-4 * least).view(-1, seq).all(1)   # of the border
+    p = ref.shares(x.double(), None, True) * (total >= least)[:, None]
+    count, live, mean, loss, grad = _balance(x, idx, True, seq)
+    want = p.view(-1, seq, E).mean(1)
+    # two terms and a division more; a share below 2^-100 may be lost
+    tol = (SHARE + 2 * U) * want + 2.0 ** -100
+    assert torch.all(((mean - want).abs() <= tol)[clear])
+    f = count.double() * E / count.sum(1, keepdim=True)
+    wl = (f * want).sum(1)
+    assert torch.all(((loss - wl).abs() <= (SHARE + 20 * U) * wl)[clear])
+    p, f = p.view(-1, seq, E), f[:, None]
+    dot, part = (f * p).sum(2, keepdim=True), p * torch.sigmoid(-x.double()).nan_to_num(1.0).view(p.shape) / seq
+    want, size = (part * (f - dot)), part * (f + dot)
+    off = (grad.view(-1, seq, E) - want).abs() <= GRAD * size + E * 2.0 ** -100
+    assert torch.all(off[clear])
