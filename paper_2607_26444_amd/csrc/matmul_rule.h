@@ -63,9 +63,9 @@ inline int64_t tiles_of(const MatmulShape& a, const Way& w) {
   return row_tiles(a, w.rows) * pieces_of(a, w);
 }
 
-// Whether a way can be launched for the call.
-inline bool way_fits(const MatmulShape& a, int n) {
-  return tiles_of(a, kWay[n]) <= (n == kTile256 || n == kTile128 ? kMaxTiles : kMaxGroups);
+// Whether way `n`, with the sizes that its table has, can be launched for the call.
+inline bool way_fits(const MatmulShape& a, const Way* ways, int n) {
+  return tiles_of(a, ways[n]) <= (n == kTile256 || n == kTile128 ? kMaxTiles : kMaxGroups);
 }
 
 // Microseconds of a call: its rounds of workgroups, the last one counted for the
@@ -106,7 +106,7 @@ inline int quickest_way(const MatmulShape& a, const Way* ways) {
   int best = kWays;
   double least = 0.0;
   for (int n = 0; n < kWays; ++n) {
-    if (!way_fits(a, n)) continue;
+    if (!way_fits(a, ways, n)) continue;
     const double t = way_time(a, ways[n]);
     if (best == kWays || t < least) {
       least = t;
