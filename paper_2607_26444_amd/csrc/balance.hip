@@ -245,7 +245,8 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void balance_kernel(BalanceArgs 
 
 // Sums over the parts of a sequence: 32 experts to a workgroup, 32 rows of parts at a
 // time in fours of neighbours.  Each leaves its part of the loss, and the last of them adds
-// those in their order.
+// those in their order.  There are two workgroups at least: up to 32 experts the 256 parts that
+// a sequence can have are few sums, for the kernel below.
 __global__ __launch_bounds__(kBlock) void balance_join_kernel(BalanceArgs a, int blocks) {
   __shared__ float s_sum[kWavesPerBlock][32];
   __shared__ int s_count[kWavesPerBlock][32];
@@ -313,17 +314,15 @@ __global__ __launch_bounds__(kBlock) void balance_join_kernel(BalanceArgs a, int
   if (block == 0) a.live_tokens[seq] = live;
   if (!a.loss) return;
   float* pieces = a.pieces + seq * blocks * 2;
-  if (blocks > 1) {
-    __hip_atomic_store(pieces + 2 * block, total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(pieces + 2 * block + 1, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (__hip_atomic_fetch_add(a.tickets + seq, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) !=
-        (uint32_t)blocks - 1u)
-      return;
-    total = dot = 0.0f;
-    for (int b = 0; b < blocks; ++b) {
-      total += __hip_atomic_load(pieces + 2 * b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      dot += __hip_atomic_load(pieces + 2 * b + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+  __hip_atomic_store(pieces + 2 * block, total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(pieces + 2 * block + 1, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (__hip_atomic_fetch_add(a.tickets + seq, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) !=
+      (uint32_t)blocks - 1u)
+    return;
+  total = dot = 0.0f;
+  for (int b = 0; b < blocks; ++b) {
+    total += __hip_atomic_load(pieces + 2 * b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    dot += __hip_atomic_load(pieces + 2 * b + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   a.loss[seq] = total > 0.0f ? dot * ((float)a.E / total) : 0.0f;
 }
