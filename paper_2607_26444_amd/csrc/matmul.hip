@@ -231,7 +231,7 @@ void matmul_tile_kernel(MatmulArgs a, int pieces, int group) {
       int s = 0, m = (int)a.rows;
       if (a.offset) window_of(a, e0 + lane < a.E ? e0 + lane : a.E - 1, first, s, m);
       if (e0 + lane >= a.E) m = 0;
-      const int end = before + scan_add((m + HEIGHT - 1) / HEIGHT);
+      const int end = before + scan_add(m / HEIGHT + (m % HEIGHT > 0));   // m may be 2^31 - 1
       s_end[e0 + lane] = end;                          // E is at most 16 times 64
       s_start[e0 + lane] = s;
       s_rows[e0 + lane] = m;

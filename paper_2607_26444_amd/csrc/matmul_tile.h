@@ -73,7 +73,7 @@ __device__ __forceinline__ Tile find_tile(const MatmulShape& a, int id, int size
     int s, m;
     window_of(a, e0 + lane < a.E ? e0 + lane : a.E - 1, first, s, m);
     if (e0 + lane >= a.E) m = 0;
-    const int tiles = (m + size - 1) / size;
+    const int tiles = m / size + (m % size > 0);
     const int sum = before + scan_add(tiles);          // inclusive over the lanes
     const uint64_t hit = __ballot((int64_t)sum * pieces > id);
     if (hit) {
