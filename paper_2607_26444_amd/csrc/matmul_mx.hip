@@ -738,13 +738,8 @@ hipError_t launch_stream(const MatmulMxArgs& a, hipStream_t stream) {
   static_assert(w.rows == ROWS && w.channels == 16 * WC && w.depth == kDepth * WK,
                 "the rule's tile");
   const int64_t groups = (tiles_of(a, w) + 255) / 256 * 256;
-  // Weights that one tile of a window reads and that the caches would not keep: 512 rows, 32
-  // experts, 7168 x 4096 89 -> 83 us.  Windows of several tiles read them again (4662 rows over 96
-  // experts 50 -> 63, 2048 rows 31 -> 33), and rows that are no whole lines share lines between
-  // stages (512 rows, 32 experts, 7136 x 4096 108 -> 122).
   MatmulMxArgs m = a;
-  m.stream_w = a.rows <= 16 * (int64_t)a.E && a.K % kDepth == 0 &&
-               (int64_t)a.E * a.N * a.K >= (int64_t)128 << 20;
+  m.stream_w = weights_read_once(a);
   hipLaunchKernelGGL((matmul_mx_stream_kernel<ROWS, WC, WK, STAGES>), dim3((unsigned)groups),
                      dim3(kTileThreads), 0, stream, m, pieces_of(a, w));
   return hipGetLastError();
