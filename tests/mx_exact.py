@@ -100,6 +100,16 @@ def packed(counts):
     return offset, list(zip(offset, counts))
 
 
+# (way, rows of the windows, N, K) with and without swiglu.
+DEEP = [("one_row", [12], 48, 131040), ("one_row", [1], 2064, 131040),
+        ("few_rows", [33, 0, 16, 60, 1, 17, 3, 50], 1040, 131040), ("narrow", [2000], 144, 131040),
+        ("narrow", [100, 0, 65, 165], 1040, 8224), ("half", [1300], 2064, 131040),
+        ("half", [200, 300, 0, 200], 2064, 131040), ("half_two", [129, 321, 0, 250], 2064, 65568),
+        ("wide", [0, 64, 65, 128, 129, 1, 63, 250] * 2, 2064, 16416),
+        ("tile128", [1400, 0, 2471, 129], 1040, 131040), ("tile256", [1500, 0, 2300, 200], 2064, 131040),
+        ("tile256", [4000], 2064, 65568)]
+
+
 def _ragged(E, rows, longest):
     """Windows of `rows` rows together: every third empty, one of them the longest."""
     counts = [0 if e % 3 == 1 else 1 + (7 * e) % 23 for e in range(E)]

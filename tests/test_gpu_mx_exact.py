@@ -1,5 +1,5 @@
-"""The experts' products on 4-bit floats where every sum is exact, with weights that are
-read past the caches.  Plain outputs have to be equal."""
+"""The experts' products on 4-bit floats where every sum is exact: as deep as a call may be, with
+weights that are read past the caches, and past 2^32 bytes.  Plain outputs have to be equal."""
 import math
 
 import pytest
@@ -7,6 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import mx_exact  # noqa: E402
+import mx_rule  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -38,7 +39,7 @@ def _ids(c):
     return f"{c[0]}-{sum(c[1])}-{len(c[1])}-{c[2]}-{c[3]}"
 
 
-@pytest.mark.parametrize("case", mx_exact.READ_ONCE, ids=_ids)
+@pytest.mark.parametrize("case", mx_exact.DEEP + mx_exact.READ_ONCE, ids=_ids)
 @pytest.mark.parametrize("swiglu", [False, True])
 def test_exact_sums(case, swiglu):
     _, counts, N, K = case
@@ -55,3 +56,28 @@ def test_on_either_side_of_the_rule_for_weights_read_once(rows, E, N, K):
     offset, windows = mx_exact.packed(counts)
     a, w = mx_exact.inputs(rows, E, N, K, rows + N, False)
     mx_exact.check(_run(a, w, offset, counts, False, K), a, w, windows, False, K)
+
+
+@pytest.mark.parametrize("way,rows,E,N,K", mx_rule.PAST_32_BITS)
+def test_exact_sums_past_32_bits(way, rows, E, N, K):
+    """Weights, rows, outputs or scales whose byte offsets pass 2^32: the last rows, with every channel
+    of the last expert.  Codes and scales of a row lie in one, as dispatch carries them."""
+    from paper_2607_26444_amd import moe
+    n = min(rows, max(3, rows // E))
+    start, half, cols = rows - n, K // 2, mx_exact.scale_cols(K)
+    pitch = -(-(half + cols) // 16) * 16
+    (aq, asc), (wq, wsc) = mx_exact.inputs(n, 1, N, K, rows, False)
+    a = torch.zeros(rows, pitch, dtype=torch.uint8, device="cuda")
+    w = torch.zeros(E, N, half, dtype=torch.uint8, device="cuda")
+    ws = torch.full((E, N, cols), 127, dtype=torch.uint8, device="cuda")
+    a[start:, :half], a[start:, half:half + cols] = aq, asc
+    w[-1], ws[-1] = wq[0], wsc[0]
+    offset = torch.full((E + 1,), start, dtype=torch.int32, device="cuda")
+    offset[0], offset[E] = 0, rows
+    count = torch.zeros(E, dtype=torch.int32, device="cuda")
+    count[-1] = n
+    y = torch.zeros(rows, N, dtype=torch.bfloat16, device="cuda")
+    moe.moe_expert_matmul_mx(a, a[:, half:], rows, w, ws, E, N, K, offset, count, moe.MOE_ACT_NONE,
+                             y, a_pitch=pitch, a_scale_pitch=pitch)
+    mx_exact.check(y[start:], (aq, asc), (wq, wsc), [(0, n)], False, K)
+    assert not torch.any(y[:start])

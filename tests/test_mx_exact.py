@@ -1,6 +1,6 @@
-"""The exact products' inputs, sizes and check, on the CPU: each streaming
-way of the launch rule has calls that read their weights past the caches, and the check notices a
-mistake of one block."""
+"""The exact products' inputs, sizes and check, on the CPU: each way of the launch rule has deep
+calls and calls that read their weights past the caches, and the check notices a mistake of one
+block."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -15,6 +15,12 @@ def choose(tmp_path_factory):
 
 def _calls(cases, swiglu):
     return [(sum(counts), len(counts), N, K, swiglu) for _, counts, N, K in cases]
+
+
+@pytest.mark.parametrize("swiglu", [0, 1])
+def test_deep_sizes_take_every_way(choose, swiglu):
+    ways = [way for way, _ in choose(_calls(mx_exact.DEEP, swiglu))]
+    assert ways == [c[0] for c in mx_exact.DEEP] and len(set(ways)) == 8
 
 
 @pytest.mark.parametrize("swiglu", [0, 1])
