@@ -78,7 +78,7 @@ __device__ __forceinline__ float scores(float (&x)[VPL], float (&rest)[REST ? VP
     float v[VPL], local = 0.0f;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-      const float e = exp_near(__builtin_amdgcn_fmed3f(-x[i], -87.0f, 87.0f)), d = 1.0f + e;
+      const float e = exp_near(__builtin_amdgcn_fmed3f(-x[i], -150.0f, 87.0f)), d = 1.0f + e;
       const float r = __builtin_amdgcn_rcpf(d);
       v[i] = x[i] >= -87.0f ? __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r) : 0.0f;
       if constexpr (REST) rest[i] = e > 1.0f ? 1.0f - v[i] : e * v[i];   // also where s rounds to 1

@@ -112,3 +112,28 @@ def test_sigmoid_scores_that_are_very_small(E, lo, hi):
     want, size = (part * (f - dot)), part * (f + dot)
     off = (grad.view(-1, seq, E) - want).abs() <= GRAD * size + E * 2.0 ** -100
     assert torch.all(off[clear])
+
+
+@pytest.mark.parametrize("E", [3, 60, 890])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_infinite_logits(E, sigmoid):
+    """Infinite ones share alike under softmax, also beside float32's largest number, and have no
+    gradient under sigmoid, nor have logits whose 1 - s is no float32 number."""
+    T = 6
+    x, idx = _logits(T, E, -4, 4, E)
+    x[0, 1], x[1, :2], x[2, 2] = math.inf, math.inf, 3.4028234663852886e38
+    x[3, 1], x[3, 2] = math.inf, 3.4028234663852886e38
+    x[4, 0] = 200.0
+    _, _, mean, loss, grad = _balance(x, idx, sigmoid, 1)
+    assert torch.all(torch.isfinite(grad)) and torch.all(torch.isfinite(loss))
+    if not sigmoid:
+        for t, at in ((0, [1]), (1, [0, 1]), (2, [2]), (3, [1]), (4, [0])):
+            want = torch.zeros(E, dtype=torch.float64)
+            want[at] = 1.0 / len(at)
+            assert torch.equal(mean[t], want), t
+        return
+    want = ref.shares(x.double(), None, True)
+    want[3] = torch.sigmoid(x[3].double()) / torch.sigmoid(x[3].double()).sum()
+    ok = ~torch.isnan(want)
+    assert torch.all(((mean - want).abs() <= SHARE * want)[ok])
+    assert not grad[x >= 150].any()
