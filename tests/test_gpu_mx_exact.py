@@ -81,3 +81,27 @@ def test_exact_sums_past_32_bits(way, rows, E, N, K):
                              y, a_pitch=pitch, a_scale_pitch=pitch)
     mx_exact.check(y[start:], (aq, asc), (wq, wsc), [(0, n)], False, K)
     assert not torch.any(y[:start])
+
+
+@pytest.mark.parametrize("spread", [0, 12, 24, 40])
+@pytest.mark.parametrize("keep", [0.03, 0.3, 1.0])
+def test_what_an_instruction_loses(spread, keep):
+    """Two instructions (and the sum of two wavefronts or none) over blocks of scales up to 2^40 apart,
+    two blocks of which cancel: 2^-20 of the sum of magnitudes each, and the rounding to bf16."""
+    K, rows, N = 256, 300, 264
+    g = torch.Generator(device="cuda")
+    g.manual_seed(spread)
+    byte = dict(dtype=torch.uint8, device="cuda")
+    q = torch.randint(0, 256, (rows, K // 2), generator=g, **byte)
+    q[torch.rand(q.shape, generator=g, device="cuda") >= keep] = 0
+    wq = torch.randint(0, 256, (1, N, K // 2), generator=g, **byte)
+    s = 127 - torch.randint(0, spread + 1, (rows, 8), generator=g, **byte)
+    ws = torch.full((1, N, 8), 127, **byte)
+    q[:, 32:64], wq[..., 32:64], s[:, :4] = q[:, :32], wq[..., :32] ^ 0x88, 127
+    y = _run((q, s), (wq, ws), [0, rows], [rows], False, K).double()
+    a, w = mx_exact.decode(q, s, K), mx_exact.decode(wq[0], ws[0], K)
+    want = a @ w.T.contiguous()
+    off = 2 * 2.0 ** -20 * (a.abs() @ w.abs().T.contiguous())
+    assert torch.all((y - want).abs() <= 2.0 ** -8 * (want.abs() + off) + off)
+    if not spread:
+        assert torch.equal(y, want.float().bfloat16().double())
