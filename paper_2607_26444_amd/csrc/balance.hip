@@ -13,10 +13,11 @@
 // which adds the loss.  Sequences of one part need no second launch.
 //
 // The logits are read once, but exponentials, reciprocals and sums over lanes take longer than
-// that, not the waiting for loads (two rounds of tokens asked for ahead instead of one, 32768 x
-// 256: 17.7 for 15.5 us): 32768 x 256 float32 in 8 sequences 14.3 us (2.4 TB/s), the
-// gradient of 32768 x 128 bf16 with another added 10.4 (2.4 TB/s), of 32768 x 256 float32
-// 16.2 (4.1 TB/s).  Small batches are bound by the launches: 128 x 16 5.0 us.
+// that (vector instructions are issued in 7.6 of the first kernel's 12.4 us), not the waiting for
+// loads (two rounds of tokens asked for ahead instead of one were a seventh slower): 32768 x 256
+// float32 in 8 sequences 13.5 us by sigmoid (2.5 TB/s), 12.9 by softmax scores; the gradient of
+// 32768 x 128 bf16 with another added 10.0 (2.5 TB/s), of 32768 x 256 float32, sigmoid, 15.8 (4.2
+// TB/s).  Small batches are bound by the launches: 128 x 16 4.9 us.
 
 #include "logits.h"
 
@@ -71,7 +72,7 @@ __device__ __forceinline__ float exp_near(float x) {
 // Exponentials and reciprocals are as near as the routing's (expf, exactly rounded) in fewer
 // instructions: their arguments are clamped to where nothing overflows.  A rounded argument and
 // the bare reciprocal would save 0.4 us (softmax) and 1.2 us (sigmoid) of 32768 x 256 logits and
-// cost up to 44 units of a share.  REST: also 1 - s.
+// cost up to 63 units of a share, for 6.  REST: also 1 - s.
 template <int LANES, int VPL, bool SIGMOID, bool REST = false>
 __device__ __forceinline__ float scores(float (&x)[VPL], float (&rest)[REST ? VPL : 1]) {
   if constexpr (SIGMOID) {
@@ -518,9 +519,25 @@ unsigned unit_blocks(int64_t seqs, int parts) {
 // Tokens that a workgroup of `waves` wavefronts has at once.
 static int64_t tokens_at_once(int E, int waves) { return waves * (E <= 256 ? 4 : 1); }
 
-// A workgroup of 16 wavefronts for each compute unit: 32768 x 256 15.5 us, with twice or half
-// as many 21.0 and 16.8; 16384 x 512 14.9, with twice as many 19.1.  Up to eight rounds of
-// tokens one workgroup is quicker than two launches (256 x 64: 7.2 and 8.5 us).
+// Values that a lane has of a token (by_width).
+static int values_of_lane(int E) {
+  int n = E <= 256 ? 1 : E <= 512 ? 8 : 16;
+  while (E <= 256 && 16 * n < E) n *= 2;
+  return n;
+}
+
+// A workgroup of 16 wavefronts for each compute unit: 32768 x 256 in 8 sequences 13.5 us, with
+// twice or half as many 19.0 and 17.7; 16384 x 512 15.9, so 20.4 and 19.6.  A sequence of few rounds
+// of tokens has one workgroup, which saves the second launch: us by one and by two launches
+//   rounds            2             4             6             8
+//   16 experts     5.0 / 8.8     5.8 / 8.9     6.6 / 9.0     7.3 / 8.8
+//   64             6.2 / 8.5     7.7 / 9.0     9.3 / 9.1    10.7 / 8.8
+//   256            9.8 / 10.6   14.3 / 10.6   18.8 / 10.8   23.1 / 10.8
+//   512            7.4 / 9.4     9.9 / 9.5    12.4 / 9.6    15.1 / 9.8
+//   1000           9.4 / 10.2   14.0 / 10.4   18.5 / 10.9   23.0 / 11.0
+// where a round takes about as long as its values of a lane and two; up to 36 of that in one.
+// More than 128 sequences have one each whatever their length: 128 of 256 x 256 13.3, 129 15.1,
+// 255 16.9, 257, in two rounds, 28.9.
 BalanceShape balance_shape(int64_t T, int E, int64_t seq) {
   BalanceShape s;
   s.seq = seq ? seq : T;
@@ -529,7 +546,7 @@ BalanceShape balance_shape(int64_t T, int E, int64_t seq) {
   int64_t parts = (s.seq + step - 1) / step;
   const int64_t most = 256 / (s.seqs > 0 ? s.seqs : 1);
   parts = parts < most ? parts : most;
-  if (s.seq <= 8 * step || parts < 1) parts = 1;
+  if (s.seq <= 36 / (values_of_lane(E) + 2) * step || parts < 1) parts = 1;
   s.per = ((s.seq + parts - 1) / parts + step - 1) / step * step;
   s.parts = s.seq > 0 ? (int)((s.seq + s.per - 1) / s.per) : 1;
   const int64_t a_wave = step / kMaxWaves, longest = s.seq < s.per ? s.seq : s.per;
@@ -544,8 +561,9 @@ BalanceShape balance_shape(int64_t T, int E, int64_t seq) {
 }
 
 // The gradient's parts leave nothing behind: about 768 workgroups of four wavefronts, each
-// with up to eight rounds of tokens (us with one, two, four, eight rounds: 32768 x 128 bf16 14.7,
-// 10.7, 10.4, 14.0; 16384 x 512 18.2, 16.1, 13.8, 14.6; 2048 x 384 5.1, 5.3, 6.6, 9.2).
+// with up to eight rounds of tokens (us with one, two, four, eight rounds: 32768 x 128 bf16 13.0,
+// 9.8, 8.8, 10.5 and by the rule's three 9.7; 16384 x 512 17.0, 14.5, 13.1, 13.8, by its six 13.4;
+// 2048 x 384 4.3, 4.6, 6.2, 9.1).
 void balance_grad_parts(BalanceGradArgs& a) {
   const int64_t step = tokens_at_once(a.E, kWavesPerBlock);
   const int64_t all = a.seqs * ((a.seq + step - 1) / step), rounds = (all + 767) / 768;

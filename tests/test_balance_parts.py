@@ -18,3 +18,17 @@ def test_up_to_32_experts_one_workgroup_joins(E):
         assert bytes_ in (0, parts * 260 + 12) and parts * 32 <= 8192
         if T > 2 ** 20:
             assert parts > 128
+
+
+@pytest.mark.parametrize("E,rounds", [(1, 12), (16, 12), (17, 9), (32, 9), (60, 6), (128, 3), (129, 2),
+                                      (256, 2), (257, 3), (512, 3), (513, 2), (1024, 2)])
+def test_short_sequences_have_one_workgroup(E, rounds):
+    """Rounds of 64 tokens up to 256 experts, of 16 beyond; no workspace where one workgroup has the
+    whole sequence.  A longer one is cut, unless there are more than 128 of them."""
+    step = 64 if E <= 256 else 16
+    assert moe.moe_balance_workspace_bytes(rounds * step, E) == 0
+    assert moe.moe_balance_workspace_bytes(rounds * step + 1, E) > 0
+    for S in (2, 128):
+        assert moe.moe_balance_workspace_bytes(S * rounds * step, E, rounds * step) == 0
+        assert moe.moe_balance_workspace_bytes(S * (rounds + 1) * step, E, (rounds + 1) * step) > 0
+    assert moe.moe_balance_workspace_bytes(129 * 4096, E, 4096) == 0
