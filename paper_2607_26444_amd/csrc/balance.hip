@@ -583,8 +583,9 @@ hipError_t launch_balance(const BalanceArgs& a, const BalanceShape& shape, hipSt
   });
   if (err != hipSuccess || a.parts == 1) return err;
   // Up to 8192 sums a sequence one workgroup joins them sooner (us by one and by several: 16
-  // sequences of 16 parts of 256 experts 13.2 and 16.6, 8 of 32 14.3 and 16.0, one of 128 parts of
-  // 64 9.2 and 9.1, of 256 parts of 64 11.0 and 10.3).
+  // sequences of 16 parts of 256 experts 13.1 and 16.1, 8 of 32 13.2 and 14.7, one of 128 parts of
+  // 64 10.0 and 9.9, of 256 parts of 64 11.1 and 10.7; 4 of 64 parts of 256 13.6 and 14.5, one of
+  // 256 of them 18.4 and 14.7).
   if (a.parts * part_pitch(a.E) <= 8192) {
     hipLaunchKernelGGL(balance_join_one_kernel, dim3((unsigned)a.seqs), dim3(kJoinThreads), 0,
                        stream, a);

@@ -84,14 +84,17 @@ __device__ __forceinline__ void each(F&& f) {
 // row from there and puts them, by quarter and tile, where a lane finds its words of four tiles
 // in one read.
 //
-// 32768 rows, 16 experts, 7168 x 4096 with swiglu 477 us (4.0 PFLOP/s), and no unit is full: the
-// matrix units are busy 44% of the cycles within a layer, at 2.0 GHz (with all codes 0 7% less
-// time), reads of LDS a fifth, and the loads would come in a third of a stage (a loop of them
-// reaches 110 to 130 bytes a ns and compute unit, 70 from rows that lie across lines).  Two
-// wavefronts a SIMD that meet once a stage do not cover each other's waits: with the loads left out
-// 370, without those of the scales alone 445.  Shallow products also have their stores (32 experts,
-// 2048 x 7168 351 us, without stores 274; not waiting for them in the next tile's first stage
-// changes nothing).
+// 32768 rows, 16 experts, 7168 x 4096 with swiglu 472 to 480 us by card (4.0 PFLOP/s).  What bounds
+// it is that the two wavefronts of a SIMD are in the same phase of a stage and meet once in it, so
+// that both wait at a time: the matrix units are busy 44% of the cycles within a layer, at 2.0 GHz
+// (with all codes 0 7% less time), reads of LDS a fifth, and the loads would come in a third of a
+// stage (a loop of them reaches 110 to 130 bytes a ns and compute unit, 70 from rows that lie
+// across lines).  With the loads left out it takes 370, without those of the scales alone 445.  The
+// two in opposite phases, or instructions of 32 x 32 x 64, have not been tried.
+// Shallow products also have their stores: 32 experts, 2048 x 7168 349 to 359 us, without stores
+// 274; not waiting for them in the next tile's first stage changes nothing.
+// A window's last rows walk all of the depth again: 32 windows of 256 rows, 7168 x 4096, 152 us, of
+// 257 236, of 384 236, of 512 253.
 // On the way there: scales word by word and stage by stage 527; 16 bytes every second stage 495;
 // stages of half the depth, four of them, 510; four wavefronts with 128 x 128 each 523; lines asked
 // for earlier, to have them in the L2 cache, +4 to 8%; the windows' short last tiles behind all
@@ -111,7 +114,9 @@ struct MxTileLds {
   static constexpr int kScaleAt = kStages * kStageBytes;
   static constexpr bool kFourStages = HEIGHT == 256;   // scales come for four stages, else for two
   // Loads of a full tile's stage that are asked for during the first units of the stage before it,
-  // and not as soon as their place is free: 0 486 us, 4 482, 6 477, 8 484 at the size above.
+  // and not as soon as their place is free: 0 486 us, 4 482, 6 477, 8 484 at the size above.  8192
+  // rows over 32 experts, where half of the windows have a short tile besides, lost 2% (225 ->
+  // 230).
   static constexpr int kLate = HEIGHT == 256 ? 6 : 0;
   static constexpr int kRawAt = kScaleAt + kTileThreads * kPairScales;
   static constexpr int kListAt = kRawAt + (kFourStages ? kTileThreads * 2 * kPairScales : 0);

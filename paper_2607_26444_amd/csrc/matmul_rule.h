@@ -141,7 +141,10 @@ inline int choose_way(const MatmulShape& a) { return quickest_way(a, kWay); }
 //   64, 8, 2048 x 1024               7.3/8.7  5.8/6.4  5.6/5.5  4.5/4.4  4.7/4.4
 //   1, 1, 7168 x 4096                 16/23    10/14   8.2/10   7.5/7.7  5.9/5.9
 // The way chosen is the best of each line or within 3% of it, but for 8192 rows over 32
-// experts (230 for 212, 137 for 130).
+// experts (230 for 212, 137 for 130), where it depends on how many windows pass 256 rows: the model
+// knows their sum alone.  For the same reason fixed windows are taken as if they were full: 512
+// rows in 32 windows of 16 take what packed ones do (81 us, 7168 x 4096 with swiglu; 49, 2048 x
+// 7168), in windows of 32 91 and 52, of 64 92 and 60, of 128 to 512 102 and 63.
 constexpr Way kMxWay[kWays] = {
     {256, 256, 128, 256, 8.2, 1.73, 1.73, 11.5e6},     // matmul_mx_tile_kernel<256>
     {128, 256, 128, 256, 5.7, 1.17, 1.17, 8.0e6},      // matmul_mx_tile_kernel<128>

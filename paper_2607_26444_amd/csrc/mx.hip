@@ -6,6 +6,10 @@
 // that none is cut off by more than half a step; a power of two less for a in [7, 8), which
 // cuts off up to 2 of 8 units, has a 3% larger error over normal values (0.115 of their root
 // mean square for 0.112), one more from 6 on as well.
+//
+// Bound by memory: 16384 rows of 7168 48.8 us (6.1 TB/s), with values 79 (6.7 TB/s).  Rows of less
+// than a wavefront's 512 values leave lanes idle: as many values in rows of 512 take 58 us, of 256
+// 105, of 64 387.
 
 #include "layer.h"
 
